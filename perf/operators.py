@@ -7,7 +7,8 @@ A case is a dict of plain values. Its ``mode`` is the call that a program makes:
 * ``checkpoint``  omnimoe_checkpoint_store and omnimoe_checkpoint_load: an activation goes to 8 bits and comes back;
 * ``backward``    omnimoe_shared_mlp_backward: gradients of the shared SwiGLU branch from the checkpoint of its input;
 * ``adapters``    omnimoe_shared_mlp_adapters: the shared branch of a batch whose tokens belong to requests with
-                  adapters of their own (or with none), added to the routed branch's output;
+                  adapters of their own (or with none), added to the routed branch's output and
+                  rounded to the layer's type;
 * ``few``         omnimoe_layer_forward_few: Eq. 7 whole (routed and shared branch) for a decode step of a few tokens.
 
 ``listed()`` names the cases, ``draw(rng)`` gives others of the same ranges, ``prepare`` makes what the program holds
@@ -128,7 +129,7 @@ def _tensors(case, seed):
         return dict(codes=codes.view(torch.uint8), scales=scales, w_gu=_normal(case, seed, 3, (2 * c.d_ff, d), w),
                     w_down=_normal(case, seed, 4, (d, c.d_ff), 1.0 / math.sqrt(c.d_ff)),
                     # the loss's gradient at the layer's output, averaged over the batch's tokens, and the routed
-                    # branch's share of dL/dx
+                    # branch's share of dL/dx, to which the call adds its own
                     dy=_normal(case, seed, 5, (T, d), 1.0 / T, torch.float32),
                     dx_in=_normal(case, seed, 6, (T, d), 1.0 / T, torch.float32))
     if c.mode == "adapters":
@@ -193,7 +194,7 @@ def _plain_backward(s):
     da = s.dy @ w_down
     dh = torch.cat((da * u * (sg * (1 + g * (1 - sg))), da * g * sg), 1)
     dt = s.w_gu.dtype
-    return dict(dx=s.dx_in + dh @ w_gu, dw_gu=(dh.t() @ x).to(dt), dw_down=(s.dy.t() @ (g * sg * u)).to(dt))
+    return dict(dx=(s.dx_in + dh @ w_gu).to(dt), dw_gu=(dh.t() @ x).to(dt), dw_down=(s.dy.t() @ (g * sg * u)).to(dt))
 
 
 def _plain_adapters(s):
@@ -208,7 +209,8 @@ def _plain_adapters(s):
     u = u + (b_up @ low[:, r:, None])[:, :, 0]
     a = g * torch.sigmoid(g) * u
     low = scale * (s.a_down[ids].float() @ a[:, :, None])[:, :, 0]
-    return dict(y=s.y_in + (a @ s.w_down.float().t() + (s.b_down[ids].float() @ low[:, :, None])[:, :, 0]))
+    y = s.y_in + (a @ s.w_down.float().t() + (s.b_down[ids].float() @ low[:, :, None])[:, :, 0])
+    return dict(y=y.to(s.x.dtype))
 
 
 def _best_cells(c, row, col, K):
@@ -270,11 +272,11 @@ def _kept(s):
         k.codes, k.scales = new((T, d), torch.uint8), new((T, -(-d // 32)), torch.uint8)
         k.back = torch.empty_like(s.x)
     elif c["mode"] == "backward":
-        k.dx, k.dw_gu, k.dw_down = torch.empty_like(s.dx_in), torch.empty_like(s.w_gu), torch.empty_like(s.w_down)
+        k.dx, k.dw_gu, k.dw_down = new((T, d), s.w_gu.dtype), torch.empty_like(s.w_gu), torch.empty_like(s.w_down)
         k.ws = workspace(P.omnimoe_shared_mlp_backward_workspace_size(desc, c["d_ff"]))
     elif c["mode"] == "adapters":
         k.adapters = P.make_adapters(s.a_gu, s.b_gu, s.a_down, s.b_down, s.scale)
-        k.y = torch.empty_like(s.y_in)
+        k.y = torch.empty_like(s.x)
         k.ws = workspace(P.omnimoe_shared_mlp_adapters_workspace_size(desc, c["d_ff"], k.adapters))
     else:
         k.y = new((T, d), torch.float32)
@@ -323,13 +325,13 @@ def work(case):
     x, mlp = c.T * c.d, 3 * c.d * c.d_ff
     if c.mode == "backward":
         # in: codes, scales, weights, dy, dx_in; out: dx, weight gradients
-        return {"bytes": x + c.T * -(-c.d // 32) + 2 * mlp * size + 12 * x,
+        return {"bytes": x + c.T * -(-c.d // 32) + 2 * mlp * size + (8 + size) * x,
                 "flops": 16.0 * c.T * c.d * c.d_ff}
     if c.mode == "adapters":
         with_one = c.T * (2 / 3 if c.ids == "mixed" else 1)
         reached = min(c.n, c.T) if c.ids != "mixed" else c.n * -math.expm1(-with_one / c.n)
         per_token = 2 * c.r * c.d + 2 * c.r * c.d_ff + c.r * c.d_ff + c.r * c.d
-        return {"bytes": x * (size + 8) + mlp * size + reached * per_token * size + 4 * c.T + 4 * reached,
+        return {"bytes": x * (2 * size + 4) + mlp * size + reached * per_token * size + 4 * c.T + 4 * reached,
                 "flops": 2.0 * c.T * mlp + 2.0 * with_one * per_token}
     M, N = c.T * c.H * c.K, c.n_rows * c.n_cols
     keys = c.H * (c.n_rows + c.n_cols) * c.d_key
