@@ -1,0 +1,60 @@
+/*
+ * omnimoe_ffn.h - the feed-forward layer around the routed branch (libomnimoe.so): the shared branch's training step
+ * on 8-bit activation checkpoints.
+ *
+ * Conventions as in omnimoe.h: device pointers owned by the caller, row-major, contiguous, 16-byte aligned; nothing is
+ * allocated; every call is asynchronous on `stream`, checked on the host before anything is launched, and may run
+ * beside calls on other streams with other workspaces; the workspace and all outputs must not overlap the inputs or
+ * each other (but where a comment allows it), and the workspace's contents need not be initialised. `stream` belongs to
+ * the calling thread's current device, which holds the tensors. Of the descriptor the calls here use T, d and dtype
+ * unless stated otherwise; it is checked whole. Results are the same on every run.
+ */
+#ifndef OMNIMOE_FFN_H
+#define OMNIMOE_FFN_H
+
+#include "omnimoe.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Activation checkpoint in 8 bits. Every row of x is cut into blocks of 32 values (the last one may be shorter); a
+ * block is held as e4m3 codes (OCP: bias 7, largest 448) times a power of two.
+ *   x       [T, d]            dtype
+ *   codes   [T, d]            uint8
+ *   scales  [T, ceil(d/32)]   uint8   exponent + 127 of the block's power of two 2^s: the least s >= -127 with
+ *                                     max |x| <= 448 2^s
+ * store: code = x 2^-s rounded to the nearest e4m3 value, ties to even (so within 2^-4 of the value, relative, where
+ * |x| >= 2^(s-6), and within 2^(s-10) below). Values that are not finite are stored as NaN and take no part in the
+ * block's maximum.
+ * load: x = code 2^s in dtype (exact but where bf16 or fp32 has no such small value). */
+omnimoe_status omnimoe_checkpoint_store(const omnimoe_layer_desc* desc, const void* x, uint8_t* codes,
+                                        uint8_t* scales, void* stream);
+omnimoe_status omnimoe_checkpoint_load(const omnimoe_layer_desc* desc, const uint8_t* codes, const uint8_t* scales,
+                                       void* x, void* stream);
+
+/* Gradients of the shared branch (omnimoe_shared_mlp) for a loss L with dL/dy = dy, from the checkpoint of its input:
+ * with x = the checkpoint's values, g = W_g x, u = W_u x (recomputed), a = silu(g) u, da = W_down^T dy,
+ * dg = da u silu'(g), du = da silu(g):
+ *   codes, scales             the checkpoint of x [T, d]
+ *   w_gu     [2 d_ff, d], w_down [d, d_ff]   dtype, as in omnimoe_shared_mlp
+ *   dy       [T, d]  fp32
+ *   dx_in    [T, d]  fp32, may be NULL (zeros): the routed branch's share of dL/dx (omnimoe_expert_backward's with
+ *                    omnimoe_route_backward's added)
+ *   dx       [T, d]  dtype out   dx_in + W_g^T dg + W_u^T du, rounded once (fp32: may be dx_in itself)
+ *   dw_gu    [2 d_ff, d] dtype out   sums over the tokens of dg x^T, then of du x^T
+ *   dw_down  [d, d_ff]   dtype out   sum over the tokens of dy a^T
+ * Sums are fp32 (matrix cores). bf16 layers round dy, a, dg and du to bf16 between the products. T = 0 writes zeros to
+ * dw_gu and dw_down (the pointers to tokens and the workspace may then be NULL). d_ff as in omnimoe_shared_mlp.
+ * Workspace: omnimoe_shared_mlp_backward_workspace_size bytes. */
+omnimoe_status omnimoe_shared_mlp_backward_workspace_size(const omnimoe_layer_desc* desc, int32_t d_ff,
+                                                          size_t* bytes);
+omnimoe_status omnimoe_shared_mlp_backward(const omnimoe_layer_desc* desc, int32_t d_ff, const uint8_t* codes,
+                                           const uint8_t* scales, const void* w_gu, const void* w_down,
+                                           const float* dy, const float* dx_in, void* dx, void* dw_gu, void* dw_down,
+                                           void* workspace, size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* OMNIMOE_FFN_H */

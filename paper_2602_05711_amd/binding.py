@@ -1,4 +1,4 @@
-"""Python binding of libomnimoe.so (declared in include/omnimoe.h): argument marshalling only.
+"""Python binding of libomnimoe.so (declared in include/omnimoe.h and include/omnimoe_ffn.h): argument marshalling only.
 
 Every function has the name of the C entry point it calls and takes torch tensors on the GPU.
 torch provides device memory and the stream (the current stream unless one is given); all of
@@ -85,6 +85,10 @@ def load_library():
         "omnimoe_layer_path": [D, ctypes.POINTER(I32)],
         "omnimoe_layer_kernels": [D],
         "omnimoe_layer_forward_timed": [D, P, P, P, P, P, P, P, P, P, SZ, P, P],
+        "omnimoe_checkpoint_store": [D, P, P, P, P],
+        "omnimoe_checkpoint_load": [D, P, P, P, P],
+        "omnimoe_shared_mlp_backward_workspace_size": [D, I32, ctypes.POINTER(SZ)],
+        "omnimoe_shared_mlp_backward": [D, I32, P, P, P, P, P, P, P, P, P, P, SZ, P],
         "omnimoe_timer_create": [I32, ctypes.POINTER(P)],
         "omnimoe_timer_destroy": [P],
         "omnimoe_timer_read": [P, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(I32)],
@@ -327,3 +331,89 @@ class Timer:
             self.close()
         except Exception:
             pass
+
+
+# ------------------------------------------------------------------ include/omnimoe_ffn.h
+
+EXPORTED_FFN = (
+    "omnimoe_checkpoint_store", "omnimoe_checkpoint_load", "omnimoe_shared_mlp_backward_workspace_size",
+    "omnimoe_shared_mlp_backward",
+)
+
+
+def _ffn_call(fn, desc, tensors, call, stream):
+    """Checks `tensors`, a list of (name, tensor or None, dtype, elements), all contiguous and on one GPU, and runs
+    call(stream) with that GPU current; `stream` defaults to its current stream."""
+    import torch
+    dev = None
+    for name, t, dtype, n in tensors:
+        if t is None:
+            continue
+        if t.dtype is not dtype:
+            raise ValueError(f"{fn}: {name} is {t.dtype}, not {dtype}")
+        if t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{fn}: {name} must be contiguous with {n} elements, not {tuple(t.shape)}")
+        if dev is None:
+            dev = t.device
+            if dev.type != "cuda":
+                raise ValueError(f"{fn}: {name} is on {dev}, not on a GPU")
+        elif t.device != dev:
+            raise ValueError(f"{fn}: {name} is on {t.device}, others on {dev}")
+    if dev is None or dev.index == torch.cuda.current_device():
+        _check(fn, call(_stream(stream)))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn, call(_stream(stream)))
+
+
+def _layer_dtype(desc):
+    import torch
+    return torch.bfloat16 if desc.dtype == OMNIMOE_BF16 else torch.float32
+
+
+def _bytes_ws(ws, size, device):
+    """`ws` (a uint8 tensor of any size: the call checks it), or a new one of size() bytes."""
+    import torch
+    return torch.empty(max(256, size()), dtype=torch.uint8, device=device) if ws is None else ws
+
+
+def omnimoe_checkpoint_store(desc, x, codes, scales, stream=None):
+    import torch
+    n, u8 = desc.T * desc.d, torch.uint8
+    _ffn_call("omnimoe_checkpoint_store", desc, (
+        ("x", x, _layer_dtype(desc), n), ("codes", codes, u8, n),
+        ("scales", scales, u8, desc.T * ((desc.d + 31) // 32))),
+        lambda st: load_library().omnimoe_checkpoint_store(ctypes.byref(desc), _ptr(x), _ptr(codes), _ptr(scales), st),
+        stream)
+
+
+def omnimoe_checkpoint_load(desc, codes, scales, x, stream=None):
+    import torch
+    n, u8 = desc.T * desc.d, torch.uint8
+    _ffn_call("omnimoe_checkpoint_load", desc, (
+        ("x", x, _layer_dtype(desc), n), ("codes", codes, u8, n),
+        ("scales", scales, u8, desc.T * ((desc.d + 31) // 32))),
+        lambda st: load_library().omnimoe_checkpoint_load(ctypes.byref(desc), _ptr(codes), _ptr(scales), _ptr(x), st),
+        stream)
+
+
+def omnimoe_shared_mlp_backward_workspace_size(desc, d_ff: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check("omnimoe_shared_mlp_backward_workspace_size",
+           load_library().omnimoe_shared_mlp_backward_workspace_size(ctypes.byref(desc), d_ff, ctypes.byref(n)))
+    return n.value
+
+
+def omnimoe_shared_mlp_backward(desc, d_ff, codes, scales, w_gu, w_down, dy, dx_in, dx, dw_gu, dw_down, ws=None,
+                                stream=None):
+    """Gradients of the shared branch from the 8-bit checkpoint of its input; dx_in may be None."""
+    import torch
+    ws = _bytes_ws(ws, lambda: omnimoe_shared_mlp_backward_workspace_size(desc, d_ff), w_gu.device)
+    T, d, dt, f32, u8 = desc.T, desc.d, _layer_dtype(desc), torch.float32, torch.uint8
+    _ffn_call("omnimoe_shared_mlp_backward", desc, (
+        ("codes", codes, u8, T * d), ("scales", scales, u8, T * ((d + 31) // 32)), ("w_gu", w_gu, dt, 2 * d_ff * d),
+        ("w_down", w_down, dt, d * d_ff), ("dy", dy, f32, T * d), ("dx_in", dx_in, f32, T * d), ("dx", dx, dt, T * d),
+        ("dw_gu", dw_gu, dt, 2 * d_ff * d), ("dw_down", dw_down, dt, d * d_ff), ("ws", ws, u8, ws.numel())),
+        lambda st: load_library().omnimoe_shared_mlp_backward(
+            ctypes.byref(desc), d_ff, _ptr(codes), _ptr(scales), _ptr(w_gu), _ptr(w_down), _ptr(dy), _ptr(dx_in),
+            _ptr(dx), _ptr(dw_gu), _ptr(dw_down), _ptr(ws), ws.numel(), st), stream)

@@ -239,4 +239,17 @@ hipError_t launch_sweep_sorted_sum(const Shape& s, const void* v, float* y, void
 hipError_t launch_accumulate(const Shape& s, const void* v, const int32_t* idx, const float* a,
                              float* y, hipStream_t st);
 
+// Activation checkpoint in 8 bits (checkpoint.hip): codes [T, d], scales [T, ceil(d / 32)].
+hipError_t launch_checkpoint_store(int64_t T, int d, bool bf16, const void* x, uint8_t* codes, uint8_t* scales,
+                                   hipStream_t st);
+hipError_t launch_checkpoint_load(int64_t T, int d, bool bf16, const uint8_t* codes, const uint8_t* scales, void* x,
+                                  hipStream_t st);
+
+// The way back through the shared branch from the checkpoint of its input (shared_backward.hip). dx_in may be NULL.
+// Workspace: shared_backward_ws_bytes(s, d_ff).
+size_t shared_backward_ws_bytes(const Shape& s, int d_ff);
+hipError_t launch_shared_backward(const Shape& s, int d_ff, const uint8_t* codes, const uint8_t* scales,
+                                  const void* w_gu, const void* w_down, const float* dy, const float* dx_in, void* dx,
+                                  void* dw_gu, void* dw_down, void* ws, hipStream_t st);
+
 }  // namespace omnimoe

@@ -1,0 +1,340 @@
+// The way back through the shared branch MLP(x) = W_down (silu(W_g x) (.) (W_u x)) (Eq. 7's SwiGLU block) from the
+// 8-bit checkpoint of its input x~:
+//   g = W_g x~, u = W_u x~, p = 1 / (1 + exp(-g)), a = g p u, da = W_down^T dy
+//   dg = da u p (1 + g (1 - p)), du = da g p
+//   dx = dx_in + W_g^T dg + W_u^T du,  dW_g = dg x~^T, dW_u = du x~^T, dW_down = dy a^T (sums over the tokens)
+// Four launches: the checkpoint's and dy's values in the layer's type; the three products that a tile of dg, du and a
+// needs, whose sums meet in registers; dx; the weight gradients, split over the tokens into fp32 partial sums that are
+// added in order. No atomics: the result is the same on every run. Sums are fp32. bf16 layers round a, dg and du to bf16
+// (once each, to nearest) for the matrix cores, as the forward pass rounds a; dy, fp32 from the caller, enters as two
+// bf16 values, its rounding and what that leaves (2^-17 relative), for two products more: with dy rounded as well, three
+// roundings (dy, a or dg, the result) put the weight gradients 0.0029 of their norm from the exact ones instead of
+// 0.0024, the rounding of the result alone being 0.0017.
+#include "internal.hpp"
+#include "tile_gemm.hpp"
+
+namespace omnimoe {
+namespace {
+
+// hi = bf16(in), lo = bf16(in - hi), eight values a thread. Where hi is not finite, lo is zero.
+__global__ __launch_bounds__(256) void split_kernel(const float* __restrict__ in, uint16_t* __restrict__ hi,
+                                                    uint16_t* __restrict__ lo, int64_t n8) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (int64_t)gridDim.x * 256) {
+    const float4 a = *(const float4*)(in + i * 8), b = *(const float4*)(in + i * 8 + 4);
+    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      h[e] = (uint32_t)bf16_rne(v[2 * e]) | ((uint32_t)bf16_rne(v[2 * e + 1]) << 16);
+      const float r0 = v[2 * e] - bf16_lo(h[e]), r1 = v[2 * e + 1] - bf16_hi(h[e]);
+      l[e] = ((h[e] & 0x7F80u) == 0x7F80u ? 0u : (uint32_t)bf16_rne(r0)) |
+             ((h[e] & 0x7F800000u) == 0x7F800000u ? 0u : (uint32_t)bf16_rne(r1) << 16);
+    }
+    *(uint4*)(hi + i * 8) = make_uint4(h[0], h[1], h[2], h[3]);
+    *(uint4*)(lo + i * 8) = make_uint4(l[0], l[1], l[2], l[3]);
+  }
+}
+
+struct HiddenArgs {
+  const void *x, *dy, *dy_lo, *w_gu, *w_down;  // [T, d] three times (dy_lo: bf16 only), [2 F, d], [d, F]
+  void *dh, *act;                      // [T, 2 F] (dg then du), [T, F]
+  int64_t T;
+  int d, F;
+};
+
+// TM tokens x FN features a workgroup; a wave holds 32 MJ tokens x 32 FI features of each of g, u and da.
+template <class T, int TM, int FN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC) void hidden_kernel(HiddenArgs p) {
+  constexpr int NW = WR * WC, MJ = TM / WR / 32, FI = FN / WC / 32;
+  typedef typename T::elem elem;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, wr = wid / WC, wc = wid % WC;
+  const int F = p.F, tiles_f = (F + FN - 1) / FN;
+  const int64_t m0 = (int64_t)(blockIdx.x / (unsigned)tiles_f) * TM;
+  const int f0 = (int)(blockIdx.x % (unsigned)tiles_f) * FN;
+  const int mlast = (int)((p.T - 1 < m0 + TM - 1 ? p.T - 1 : m0 + TM - 1) - m0);
+  auto token = [&](int r) { return r < mlast ? r : mlast; };
+
+  int b0[MJ], a2[2 * FI], a1[FI];
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) b0[j] = (wr * MJ + j) * 32;
+#pragma unroll
+  for (int i = 0; i < FI; ++i) {
+    a1[i] = a2[2 * i] = (wc * FI + i) * 32;
+    a2[2 * i + 1] = FN + a1[i];
+  }
+  tg_f32x16 gu[2 * FI][MJ], da[FI][MJ];
+  tile_zero(gu);
+  tile_zero(da);
+  {
+    TileOperand<T, 2 * FN, false, NW> w;
+    TileOperand<T, TM, false, NW> x;
+    w.init((const elem*)p.w_gu, p.d, wid, lane, [&](int r) {
+      const int f = f0 + (r < FN ? r : r - FN);
+      return (f < F ? f : F - 1) + (r < FN ? 0 : F);
+    });
+    x.init((const elem*)p.x + m0 * p.d, p.d, wid, lane, token);
+    tile_sum<decltype(w), decltype(x), T>(w, x, p.d, a2, b0, smem, wid, lane, gu);
+  }
+  {
+    TileOperand<T, FN, true, NW> w;
+    TileOperand<T, TM, false, NW> y;
+    w.init((const elem*)p.w_down, F, wid, lane, [&](int r) { return f0 + r < F ? f0 + r : F - w.kPer; });
+    y.init((const elem*)p.dy + m0 * p.d, p.d, wid, lane, token);
+    tile_sum<decltype(w), decltype(y), T>(w, y, p.d, a1, b0, smem, wid, lane, da);
+    if constexpr (T::kSize == 2) {
+      y.base = (const char*)((const elem*)p.dy_lo + m0 * p.d);
+      tile_sum<decltype(w), decltype(y), T>(w, y, p.d, a1, b0, smem, wid, lane, da);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) {
+    const int64_t t = m0 + b0[j] + (lane & 31);
+    if (t >= p.T) continue;
+    elem* const dh = (elem*)p.dh + t * 2 * F;
+    elem* const act = (elem*)p.act + t * F;
+#pragma unroll
+    for (int i = 0; i < FI; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int f = f0 + a1[i] + 8 * q + 4 * (lane >> 5);
+        if (f >= F) continue;
+        float dg[4], du[4], a[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float g = gu[2 * i][j][4 * q + e], u = gu[2 * i + 1][j][4 * q + e], z = da[i][j][4 * q + e];
+          const float s = 1.0f / (1.0f + expf(-g));
+          a[e] = g * s * u;
+          du[e] = z * (g * s);
+          dg[e] = z * u * (s * (1.0f + g * (1.0f - s)));
+        }
+        store4(dh + f, dg[0], dg[1], dg[2], dg[3]);
+        store4(dh + F + f, du[0], du[1], du[2], du[3]);
+        store4(act + f, a[0], a[1], a[2], a[3]);
+      }
+  }
+}
+
+// C[m, n] = sum over k of B(m, k) A(n, k), a workgroup's tile TM x TN of one of up to two products and one part of the
+// summed range. Parts (parts > 1) go to part[z][m, n] in fp32, whole sums to out in the layer's type, with add[m, n].
+struct Product {
+  const void *a, *b, *b_lo;  // b_lo: NULL, or what is added to b
+  int64_t lda, ldb, M;
+  int N, K, tiles_n;
+  void* out;
+  const float* add;  // or NULL
+  float* part;
+};
+struct ProductArgs {
+  Product p[2];
+  int first;  // workgroups of the first product, per part
+  int parts, kpart;
+};
+
+template <class T, int TM, int TN, int WR, int WC, bool B_MNC>
+__global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args) {
+  constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
+  typedef typename T::elem elem;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, wr = wid / WC, wc = wid % WC;
+  const bool second = (int)blockIdx.x >= args.first;
+  const Product& p = args.p[second];
+  const int tile = (int)blockIdx.x - (second ? args.first : 0);
+  const int n0 = tile % p.tiles_n * TN;
+  const int64_t m0 = (int64_t)(tile / p.tiles_n) * TM;
+  const int k0 = blockIdx.y * args.kpart;
+  const int K = args.parts == 1 ? p.K : (p.K - k0 < args.kpart ? p.K - k0 : args.kpart);
+  const int mlast = (int)((p.M - 1 < m0 + TM - 1 ? p.M - 1 : m0 + TM - 1) - m0);
+
+  int a0[NI], b0[MJ];
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) b0[j] = (wr * MJ + j) * 32;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) a0[i] = (wc * NI + i) * 32;
+  tg_f32x16 acc[NI][MJ];
+  tile_zero(acc);
+  TileOperand<T, TN, true, NW> a;
+  TileOperand<T, TM, B_MNC, NW> b;
+  a.init((const elem*)p.a + (int64_t)k0 * p.lda, p.lda, wid, lane,
+         [&](int r) { return n0 + r < p.N ? n0 + r : p.N - a.kPer; });
+  if constexpr (B_MNC)
+    b.init((const elem*)p.b + (int64_t)k0 * p.ldb + m0, p.ldb, wid, lane,
+           [&](int r) { return r <= mlast ? r : mlast + 1 - b.kPer; });
+  else
+    b.init((const elem*)p.b + k0 + m0 * p.ldb, p.ldb, wid, lane, [&](int r) { return r < mlast ? r : mlast; });
+  tile_sum<decltype(a), decltype(b), T>(a, b, K, a0, b0, smem, wid, lane, acc);
+  if (p.b_lo) {
+    b.base += (const char*)p.b_lo - (const char*)p.b;
+    tile_sum<decltype(a), decltype(b), T>(a, b, K, a0, b0, smem, wid, lane, acc);
+  }
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) {
+    const int64_t m = m0 + b0[j] + (lane & 31);
+    if (m >= p.M) continue;
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int n = n0 + a0[i] + 8 * q + 4 * (lane >> 5);
+        if (n >= p.N) continue;
+        const int64_t at = m * p.N + n;
+        float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+        if (args.parts > 1) {
+          *(float4*)(p.part + blockIdx.y * (p.M * p.N) + at) = v;
+          continue;
+        }
+        if (p.add) {
+          const float4 s = *(const float4*)(p.add + at);
+          v.x += s.x;
+          v.y += s.y;
+          v.z += s.z;
+          v.w += s.w;
+        }
+        store4((elem*)p.out + at, v.x, v.y, v.z, v.w);
+      }
+  }
+}
+
+// out = the parts' sum, in order, of both products (n4 quads of the first, then the second's).
+template <class T>
+__global__ __launch_bounds__(256) void add_parts_kernel(ProductArgs args, int64_t n4_first, int64_t n4) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
+    const bool second = i >= n4_first;
+    const Product& p = args.p[second];
+    const int64_t at = (i - (second ? n4_first : 0)) * 4, size = p.M * p.N;
+    float4 v = *(const float4*)(p.part + at);
+    for (int z = 1; z < args.parts; ++z) {
+      const float4 s = *(const float4*)(p.part + z * size + at);
+      v.x += s.x;
+      v.y += s.y;
+      v.z += s.z;
+      v.w += s.w;
+    }
+    store4((typename T::elem*)p.out + at, v.x, v.y, v.z, v.w);
+  }
+}
+
+size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
+
+int64_t tiles(int64_t M, int64_t N, int tm, int tn) { return ((M + tm - 1) / tm) * ((N + tn - 1) / tn); }
+
+// Parts of the weight gradients' sums over the tokens.
+struct Parts {
+  int parts, kpart;
+};
+Parts weight_parts(int64_t T, int d, int F, int tile) {
+  if (T == 0) return {1, 64};
+  const int64_t t = tiles(2 * (int64_t)F, d, tile, tile) + tiles(d, F, tile, tile);
+  int64_t want = (768 + t - 1) / t;
+  const int64_t most = (T + 255) / 256;
+  if (want > most) want = most;
+  if (want < 1) want = 1;
+  const int64_t kpart = ((T + want - 1) / want + 63) / 64 * 64;
+  return {(int)((T + kpart - 1) / kpart), (int)kpart};
+}
+
+bool large_tiles(int64_t T, int d, int F, bool bf16) { return bf16 && tiles(T, F, 256, 128) >= 192; }
+
+template <class T>
+hipError_t run(const Shape& s, int F, const uint8_t* codes, const uint8_t* scales, const void* w_gu,
+               const void* w_down, const float* dy, const float* dx_in, void* dx, void* dw_gu, void* dw_down,
+               char* ws, hipStream_t st) {
+  constexpr bool kBf16 = T::kSize == 2;
+  constexpr int kSmallLds = 2 * (128 + 64) * 128, kProductLds = 2 * 128 * 128;
+  const int d = s.d;
+  char* xb = ws;
+  char* dyb = xb + up((size_t)s.T * d * T::kSize);
+  char* dyl = dyb + (kBf16 ? up((size_t)s.T * d * 2) : 0);
+  char* dh = dyl + (kBf16 ? up((size_t)s.T * d * 2) : 0);
+  char* act = dh + up((size_t)s.T * 2 * F * T::kSize);
+  char* part = act + up((size_t)s.T * F * T::kSize);
+  hipError_t e;
+  if (s.T > 0) {
+    if ((e = launch_checkpoint_load(s.T, d, kBf16, codes, scales, xb, st))) return e;
+    if (kBf16) {
+      const int64_t n8 = s.T * d / 8;
+      const int64_t blocks = (n8 + 255) / 256;
+      hipLaunchKernelGGL(split_kernel, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), 0, st, dy,
+                         (uint16_t*)dyb, (uint16_t*)dyl, n8);
+    }
+    HiddenArgs h{xb, kBf16 ? (const void*)dyb : dy, dyl, w_gu, w_down, dh, act, s.T, d, F};
+    bool done = false;
+    if constexpr (kBf16)
+      if (large_tiles(s.T, d, F, true)) {
+        done = true;
+        hipLaunchKernelGGL((hidden_kernel<T, 256, 128, 2, 2>),
+                           dim3((unsigned)tiles(s.T, F, 256, 128)), dim3(256), 2 * 512 * 128, st, h);
+      }
+    if (!done)
+      hipLaunchKernelGGL((hidden_kernel<T, 64, 64, 2, 2>),
+                         dim3((unsigned)tiles(s.T, F, 64, 64)), dim3(256), kSmallLds, st, h);
+    if ((e = hipGetLastError())) return e;
+  }
+  const void* dyk = kBf16 ? (const void*)dyb : dy;
+  ProductArgs g{};
+  g.parts = 1;
+  if (s.T > 0) {
+    g.p[0] = {w_gu, dh, nullptr, d, 2 * (int64_t)F, s.T, d, 2 * F, 0, dx, dx_in, nullptr};
+    bool done = false;
+    if constexpr (kBf16)
+      if (tiles(s.T, d, 256, 256) >= 192) {
+        done = true;
+        g.p[0].tiles_n = (d + 255) / 256;
+        g.first = (int)tiles(s.T, d, 256, 256);
+        hipLaunchKernelGGL((product_kernel<T, 256, 256, 2, 4, false>), dim3((unsigned)g.first), dim3(512),
+                           2 * 512 * 128, st, g);
+      }
+    if (!done) {
+      g.p[0].tiles_n = (d + 63) / 64;
+      g.first = (int)tiles(s.T, d, 64, 64);
+      hipLaunchKernelGGL((product_kernel<T, 64, 64, 2, 2, false>), dim3((unsigned)g.first), dim3(256), kProductLds,
+                         st, g);
+    }
+    if ((e = hipGetLastError())) return e;
+  }
+  const bool big = kBf16 && large_tiles(s.T, d, F, true);
+  const int tile = big ? 256 : 64;
+  const Parts z = weight_parts(s.T, d, F, tile);
+  g.parts = z.parts < 1 ? 1 : z.parts;
+  g.kpart = z.kpart;
+  g.p[0] = {xb, dh, nullptr, d, 2 * (int64_t)F, 2 * (int64_t)F, d, (int)s.T, (d + tile - 1) / tile, dw_gu, nullptr,
+            (float*)part};
+  g.p[1] = {act, dyk, kBf16 ? dyl : nullptr, F, d, d, F, (int)s.T, (F + tile - 1) / tile, dw_down, nullptr,
+            (float*)part + (size_t)g.parts * 2 * F * d};
+  g.first = (int)tiles(2 * (int64_t)F, d, tile, tile);
+  const unsigned n = (unsigned)(g.first + tiles(d, F, tile, tile));
+  bool done = false;
+  if constexpr (kBf16)
+    if (big) {
+      done = true;
+      hipLaunchKernelGGL((product_kernel<T, 256, 256, 2, 4, true>), dim3(n, g.parts), dim3(512), 2 * 512 * 128, st, g);
+    }
+  if (!done)
+    hipLaunchKernelGGL((product_kernel<T, 64, 64, 2, 2, true>), dim3(n, g.parts), dim3(256), kProductLds, st, g);
+  if ((e = hipGetLastError())) return e;
+  if (g.parts > 1) {
+    const int64_t n4 = (int64_t)F * d / 2, all = n4 + (int64_t)F * d / 4, blocks = (all + 255) / 256;
+    hipLaunchKernelGGL(add_parts_kernel<T>, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), 0, st, g,
+                       n4, all);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t shared_backward_ws_bytes(const Shape& s, int F) {
+  const size_t size = s.bf16 ? 2 : 4, T = (size_t)s.T;
+  const int tile = large_tiles(s.T, s.d, F, s.bf16) ? 256 : 64;
+  const Parts z = weight_parts(s.T, s.d, F, tile);
+  return up(T * s.d * size) + (s.bf16 ? 2 * up(T * s.d * 2) : 0) + up(T * 2 * F * size) + up(T * F * size) +
+         (z.parts > 1 ? up((size_t)z.parts * 3 * F * s.d * 4) : 0);
+}
+
+hipError_t launch_shared_backward(const Shape& s, int F, const uint8_t* codes, const uint8_t* scales,
+                                  const void* w_gu, const void* w_down, const float* dy, const float* dx_in, void* dx,
+                                  void* dw_gu, void* dw_down, void* ws, hipStream_t st) {
+  return s.bf16 ? run<BF16>(s, F, codes, scales, w_gu, w_down, dy, dx_in, dx, dw_gu, dw_down, (char*)ws, st)
+                : run<F32>(s, F, codes, scales, w_gu, w_down, dy, dx_in, dx, dw_gu, dw_down, (char*)ws, st);
+}
+
+}  // namespace omnimoe

@@ -1,0 +1,204 @@
+// Matrix products of the shared branch's training and adapter kernels: a workgroup's TM x TN tile of C = A B^T, the
+// operands copied global -> LDS without registers, two stages, products on the matrix cores with fp32 accumulation
+// (v_mfma_f32_32x32x16_bf16, or v_mfma_f32_32x32x2_f32 for fp32 layers).
+//
+// An operand is indexed (r, k): r a row of the product's result (its columns for B), k the summed index. It lies in
+// memory either with k contiguous (element (r, k) at p[r ld + k]) or, MNC, with r contiguous (p[k ld + r]), so that
+// the way back needs no transposed copies: the weights of the forward products are read as they are. A stage holds
+// kStep(T) values of k (64 bf16, 32 fp32): 128 bytes a row either way.
+//   k contiguous: rows of 128 bytes; the 16-byte chunk j of row r lies at j ^ ((r >> 1) & 7), so that the rows read by
+//     one operand load fall in distinct banks.
+//   MNC bf16: rows k of 2 R bytes; a lane's eight k values come from two ds_read_b64_tr_b16, each of which hands the
+//     lanes of a 16-lane group one column each of a 4 (k) x 16 (r) block; the 64-byte chunks of row k are permuted by
+//     its low bits, so that a block's four rows fall in distinct banks.
+//   MNC fp32: rows k of 4 R bytes, read value by value; the 128-byte chunks alternate with bit 2 of k.
+// The sum's last stage may be partial: chunks past K are stored as zeros. Rows past the operand's last one read that
+// row again (their results are not stored).
+#pragma once
+
+#include "device_common.hpp"
+
+namespace omnimoe {
+
+typedef __bf16 tg_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float tg_f32x4 __attribute__((ext_vector_type(4)));
+typedef float tg_f32x16 __attribute__((ext_vector_type(16)));
+typedef short tg_s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void* tg_lds_ptr;
+typedef __attribute__((address_space(3))) tg_s16x4* tg_lds_s16x4;
+
+struct BF16 {
+  typedef uint16_t elem;
+  typedef tg_bf16x8 frag;
+  static constexpr int kSize = 2, kStep = 64;
+};
+struct F32 {
+  typedef float elem;
+  typedef tg_f32x4 frag;
+  static constexpr int kSize = 4, kStep = 32;
+};
+
+// acc += (rows of a) x (rows of b): register q of lane l is a's row 8 (q / 4) + 4 (l / 32) + q % 4 and b's row
+// l % 32.
+__device__ __forceinline__ void tile_mma(tg_f32x16& acc, tg_bf16x8 a, tg_bf16x8 b) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
+}
+__device__ __forceinline__ void tile_mma(tg_f32x16& acc, tg_f32x4 a, tg_f32x4 b) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], acc, 0, 0, 0);
+}
+
+// One operand's R rows of a stage, copied by NW waves.
+template <class T, int R, bool MNC, int NW>
+struct TileOperand {
+  static constexpr int kBytes = R * 128;
+  static constexpr int kCopies = R / 8 / NW;  // 1 KiB each
+  static_assert(R % (8 * NW) == 0, "each wave copies whole KiB");
+  static constexpr int kPer = 16 / T::kSize;                 // elements per 16-byte chunk
+  static constexpr int kRowChunks = MNC ? R / kPer : 8;      // 16-byte chunks per LDS row
+  typedef typename T::elem elem;
+
+  // Copy i of stage kt reads from base + kt step + off[i] (bytes; base and step are the same on every lane, and a tile's
+  // rows lie within 4 GiB of its first: 256 rows, or 64 of the summed index, of at most 2^17 values).
+  const char* base;
+  int64_t step;
+  uint32_t off[kCopies];
+  int lds;  // this wave's first byte within the operand
+
+  // Position of chunk c in LDS row `row` (an involution in c).
+  static __device__ __forceinline__ int place(int row, int c) {
+    if constexpr (!MNC) return c ^ ((row >> 1) & 7);
+    else if constexpr (T::kSize == 4) return c ^ (((row >> 2) & 1) << 3);
+    else if constexpr (R >= 128) return c ^ ((row & 3) << 2);
+    else return c ^ (((row >> 1) & 1) << 2);
+  }
+
+  // row(r): the operand's row in memory of tile row r (0 <= r < R); for MNC it must keep groups of kPer together.
+  template <class Row>
+  __device__ __forceinline__ void init(const elem* p, int64_t ld, int wid, int lane, Row row) {
+    base = (const char*)p;
+    step = (MNC ? (int64_t)T::kStep * ld : T::kStep) * T::kSize;
+    lds = wid * kCopies * 1024;
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int at = (wid * kCopies + i) * 64 + lane;  // 16-byte position within the operand
+      const int lrow = at / kRowChunks, c = place(lrow, at % kRowChunks);
+      const int64_t e = MNC ? (int64_t)lrow * ld + row(c * kPer) : (int64_t)row(lrow) * ld + c * kPer;
+      off[i] = (uint32_t)(e * T::kSize);
+    }
+  }
+  // k of this lane's chunk in copy i, within the stage
+  static __device__ __forceinline__ int chunk_k(int i, int lane, int wid) {
+    const int at = (wid * kCopies + i) * 64 + lane;
+    const int lrow = at / kRowChunks;
+    return MNC ? lrow : place(lrow, at % kRowChunks) * kPer;
+  }
+  __device__ __forceinline__ void copy(unsigned char* st, int kt, int K, int wid, int lane) const {
+    unsigned char* const to = st + lds;
+    const char* const from = base + kt * step;
+    if ((kt + 1) * T::kStep <= K) {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i)
+        __builtin_amdgcn_global_load_lds((const void*)(from + off[i]), (tg_lds_ptr)(to + i * 1024), 16, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) {
+        if (kt * T::kStep + chunk_k(i, lane, wid) < K)
+          __builtin_amdgcn_global_load_lds((const void*)(from + off[i]), (tg_lds_ptr)(to + i * 1024), 16, 0, 0);
+        else
+          *(uint4*)(to + i * 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
+      }
+    }
+  }
+  // Rows r0 .. r0 + 31 (r0 a multiple of 32), quarter ks of the stage.
+  static __device__ __forceinline__ typename T::frag frag(const unsigned char* st, int r0, int ks, int lane) {
+    if constexpr (!MNC) {
+      const int r = r0 + (lane & 31);
+      return *(const typename T::frag*)(st + r * 128 + (((ks * 2 + (lane >> 5)) ^ ((r >> 1) & 7)) << 4));
+    } else if constexpr (T::kSize == 2) {
+      const int g = lane >> 4, i = lane & 15;
+      const int k = ks * 16 + (g >> 1) * 8 + (i >> 2);
+      const unsigned char* a = st + k * (2 * R) + place(k, r0 / 8 + (g & 1) * 2 + ((i & 3) >> 1)) * 16 + (i & 1) * 8;
+      const tg_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tg_lds_s16x4)a);
+      const tg_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tg_lds_s16x4)(a + 4 * (2 * R)));
+      typedef short s16x8 __attribute__((ext_vector_type(8)));
+      const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      return __builtin_bit_cast(tg_bf16x8, v);
+    } else {
+      const int k = ks * 8 + (lane >> 5) * 4, r = r0 + (lane & 31);
+      const unsigned char* a = st + k * (4 * R) + place(k, r / 4) * 16 + (r & 3) * 4;
+      tg_f32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *(const float*)(a + e * (4 * R));
+      return v;
+    }
+  }
+};
+
+// The workgroup's sum over K into acc[i][j]: a's rows a0[i] .. + 31 and b's rows b0[j] .. + 31 of the tile. smem holds two stages of both operands. Every thread of the workgroup takes part; on return the LDS is free.
+template <class OA, class OB, class T, int MI, int NJ>
+__device__ __forceinline__ void tile_sum(const OA& a, const OB& b, int K, const int (&a0)[MI], const int (&b0)[NJ],
+                                         unsigned char* smem, int wid, int lane, tg_f32x16 (&acc)[MI][NJ]) {
+  constexpr int kStage = OA::kBytes + OB::kBytes;
+  const int KT = (K + T::kStep - 1) / T::kStep;
+  if (KT == 0) return;
+  a.copy(smem, 0, K, wid, lane);
+  b.copy(smem + OA::kBytes, 0, K, wid, lane);
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  __syncthreads();
+  for (int kt = 0; kt < KT; ++kt) {
+    const unsigned char* st = smem + (kt & 1) * kStage;
+    if (kt + 1 < KT) {
+      unsigned char* nx = smem + ((kt & 1) ^ 1) * kStage;
+      a.copy(nx, kt + 1, K, wid, lane);
+      b.copy(nx + OA::kBytes, kt + 1, K, wid, lane);
+    }
+    typename T::frag fa[2][MI], fb[2][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) fa[0][i] = OA::frag(st, a0[i], 0, lane);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) fb[0][j] = OB::frag(st + OA::kBytes, b0[j], 0, lane);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      const int c = ks & 1;
+      if (ks + 1 < 4) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[c ^ 1][i] = OA::frag(st, a0[i], ks + 1, lane);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) fb[c ^ 1][j] = OB::frag(st + OA::kBytes, b0[j], ks + 1, lane);
+      }
+      // the next quarter's reads are issued before this one's products
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) tile_mma(acc[i][j], fa[c][i], fb[c][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
+  }
+}
+
+template <int MI, int NJ>
+__device__ __forceinline__ void tile_zero(tg_f32x16 (&acc)[MI][NJ]) {
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+}
+
+// Four neighbouring values in the layer's type.
+__device__ __forceinline__ void store4(uint16_t* p, float a, float b, float c, float d) {
+  uint2 o;
+  o.x = (uint32_t)bf16_rne(a) | ((uint32_t)bf16_rne(b) << 16);
+  o.y = (uint32_t)bf16_rne(c) | ((uint32_t)bf16_rne(d) << 16);
+  *(uint2*)p = o;
+}
+__device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) {
+  *(float4*)p = make_float4(a, b, c, d);
+}
+
+}  // namespace omnimoe
