@@ -47,8 +47,8 @@ template <class T, int TM, int FN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC) void hidden_kernel(HiddenArgs p) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, FI = FN / WC / 32;
   typedef typename T::elem elem;
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, wr = wid / WC, wc = wid % WC;
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[(2 * FN + TM) * 128], st1[(2 * FN + TM) * 128];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
   const int F = p.F, tiles_f = (F + FN - 1) / FN;
   const int64_t m0 = (int64_t)(blockIdx.x / (unsigned)tiles_f) * TM;
   const int f0 = (int)(blockIdx.x % (unsigned)tiles_f) * FN;
@@ -74,18 +74,16 @@ __global__ __launch_bounds__(64 * WR * WC) void hidden_kernel(HiddenArgs p) {
       return (f < F ? f : F - 1) + (r < FN ? 0 : F);
     });
     x.init((const elem*)p.x + m0 * p.d, p.d, wid, lane, token);
-    tile_sum<decltype(w), decltype(x), T>(w, x, p.d, a2, b0, smem, wid, lane, gu);
+    const TileRange all[2] = {{p.d, 0, 0}, {0, 0, 0}};
+    tile_sum<T>(w, x, all, a2, b0, st0, st1, wid, lane, gu);
   }
   {
     TileOperand<T, FN, true, NW> w;
     TileOperand<T, TM, false, NW> y;
     w.init((const elem*)p.w_down, F, wid, lane, [&](int r) { return f0 + r < F ? f0 + r : F - w.kPer; });
     y.init((const elem*)p.dy + m0 * p.d, p.d, wid, lane, token);
-    tile_sum<decltype(w), decltype(y), T>(w, y, p.d, a1, b0, smem, wid, lane, da);
-    if constexpr (T::kSize == 2) {
-      y.base = (const char*)((const elem*)p.dy_lo + m0 * p.d);
-      tile_sum<decltype(w), decltype(y), T>(w, y, p.d, a1, b0, smem, wid, lane, da);
-    }
+    const TileRange both[2] = {{p.d, 0, 0}, {T::kSize == 2 ? p.d : 0, 0, (const char*)p.dy_lo - (const char*)p.dy}};
+    tile_sum<T>(w, y, both, a1, b0, st0, st1, wid, lane, da);
   }
 #pragma unroll
   for (int j = 0; j < MJ; ++j) {
@@ -117,34 +115,43 @@ __global__ __launch_bounds__(64 * WR * WC) void hidden_kernel(HiddenArgs p) {
 
 // C[m, n] = sum over k of B(m, k) A(n, k), a workgroup's tile TM x TN of one of up to two products and one part of the
 // summed range. Parts (parts > 1) go to part[z][m, n] in fp32, whole sums to out in the layer's type, with add[m, n].
+// With b_lo, B is b + b_lo: the range is run through twice, k in [K, 2 K) being b_lo's.
 struct Product {
-  const void *a, *b, *b_lo;  // b_lo: NULL, or what is added to b
+  const void *a, *b, *b_lo;
   int64_t lda, ldb, M;
-  int N, K, tiles_n;
+  int N, K, tiles_n, parts;
+  int first;  // workgroup of the product's first tile
   void* out;
   const float* add;  // or NULL
   float* part;
 };
 struct ProductArgs {
   Product p[2];
-  int first;  // workgroups of the first product, per part
-  int parts, kpart;
+  int kpart;
 };
 
 template <class T, int TM, int TN, int WR, int WC, bool B_MNC>
 __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
   typedef typename T::elem elem;
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, wr = wid / WC, wc = wid % WC;
-  const bool second = (int)blockIdx.x >= args.first;
-  const Product& p = args.p[second];
-  const int tile = (int)blockIdx.x - (second ? args.first : 0);
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
+  const int wg = (int)xcd_contiguous(blockIdx.x, gridDim.x);
+  const Product& p = args.p[wg >= args.p[1].first];
+  const int part = (wg - p.first) % p.parts, tile = (wg - p.first) / p.parts;
   const int n0 = tile % p.tiles_n * TN;
   const int64_t m0 = (int64_t)(tile / p.tiles_n) * TM;
-  const int k0 = blockIdx.y * args.kpart;
-  const int K = args.parts == 1 ? p.K : (p.K - k0 < args.kpart ? p.K - k0 : args.kpart);
   const int mlast = (int)((p.M - 1 < m0 + TM - 1 ? p.M - 1 : m0 + TM - 1) - m0);
+  TileRange range[2];
+  {
+    const int64_t ka = p.lda * T::kSize, kb = (B_MNC ? p.ldb : 1) * T::kSize;
+    const int64_t lo = (const char*)p.b_lo - (const char*)p.b;
+    const int64_t k0 = (int64_t)part * args.kpart, k1 = p.parts == 1 ? 2 * (int64_t)p.K : k0 + args.kpart;
+    auto cut = [&](int64_t v) { return (int)(v < 0 ? 0 : v > p.K ? p.K : v); };
+    const int h0 = cut(k0), h1 = cut(k1), l0 = cut(k0 - p.K), l1 = p.b_lo ? cut(k1 - p.K) : l0;
+    range[0] = {h1 - h0, h0 * ka, h0 * kb};
+    range[1] = {l1 - l0, l0 * ka, l0 * kb + lo};
+  }
 
   int a0[NI], b0[MJ];
 #pragma unroll
@@ -155,18 +162,12 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args)
   tile_zero(acc);
   TileOperand<T, TN, true, NW> a;
   TileOperand<T, TM, B_MNC, NW> b;
-  a.init((const elem*)p.a + (int64_t)k0 * p.lda, p.lda, wid, lane,
-         [&](int r) { return n0 + r < p.N ? n0 + r : p.N - a.kPer; });
+  a.init((const elem*)p.a, p.lda, wid, lane, [&](int r) { return n0 + r < p.N ? n0 + r : p.N - a.kPer; });
   if constexpr (B_MNC)
-    b.init((const elem*)p.b + (int64_t)k0 * p.ldb + m0, p.ldb, wid, lane,
-           [&](int r) { return r <= mlast ? r : mlast + 1 - b.kPer; });
+    b.init((const elem*)p.b + m0, p.ldb, wid, lane, [&](int r) { return r <= mlast ? r : mlast + 1 - b.kPer; });
   else
-    b.init((const elem*)p.b + k0 + m0 * p.ldb, p.ldb, wid, lane, [&](int r) { return r < mlast ? r : mlast; });
-  tile_sum<decltype(a), decltype(b), T>(a, b, K, a0, b0, smem, wid, lane, acc);
-  if (p.b_lo) {
-    b.base += (const char*)p.b_lo - (const char*)p.b;
-    tile_sum<decltype(a), decltype(b), T>(a, b, K, a0, b0, smem, wid, lane, acc);
-  }
+    b.init((const elem*)p.b + m0 * p.ldb, p.ldb, wid, lane, [&](int r) { return r < mlast ? r : mlast; });
+  tile_sum<T>(a, b, range, a0, b0, st0, st1, wid, lane, acc);
 #pragma unroll
   for (int j = 0; j < MJ; ++j) {
     const int64_t m = m0 + b0[j] + (lane & 31);
@@ -179,8 +180,8 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args)
         if (n >= p.N) continue;
         const int64_t at = m * p.N + n;
         float4 v = make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-        if (args.parts > 1) {
-          *(float4*)(p.part + blockIdx.y * (p.M * p.N) + at) = v;
+        if (p.parts > 1) {
+          *(float4*)(p.part + part * (p.M * p.N) + at) = v;
           continue;
         }
         if (p.add) {
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args)
   }
 }
 
-// out = the parts' sum, in order, of both products (n4 quads of the first, then the second's).
+// out = the parts' sum, in order, of one or both products (n4 quads of p[0], then n4_second of p[1]).
 template <class T>
 __global__ __launch_bounds__(256) void add_parts_kernel(ProductArgs args, int64_t n4_first, int64_t n4) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(256) void add_parts_kernel(ProductArgs args, int64_
     const Product& p = args.p[second];
     const int64_t at = (i - (second ? n4_first : 0)) * 4, size = p.M * p.N;
     float4 v = *(const float4*)(p.part + at);
-    for (int z = 1; z < args.parts; ++z) {
+    for (int z = 1; z < p.parts; ++z) {
       const float4 s = *(const float4*)(p.part + z * size + at);
       v.x += s.x;
       v.y += s.y;
@@ -218,29 +219,54 @@ size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 
 int64_t tiles(int64_t M, int64_t N, int tm, int tn) { return ((M + tm - 1) / tm) * ((N + tn - 1) / tn); }
 
-// Parts of the weight gradients' sums over the tokens.
+// How the weight gradients' sums over the tokens are split: parts of kpart values of k, dW_gu's range being the tokens
+// and dW_down's twice those for bf16 (dy's two halves). Of the splits into 1 to 64 parts the one is taken that the
+// workgroups' rounds over the compute units and the parts' way through memory make the shortest.
 struct Parts {
-  int parts, kpart;
+  int gu, down, kpart;
 };
-Parts weight_parts(int64_t T, int d, int F, int tile) {
-  if (T == 0) return {1, 64};
-  const int64_t t = tiles(2 * (int64_t)F, d, tile, tile) + tiles(d, F, tile, tile);
-  int64_t want = (768 + t - 1) / t;
-  const int64_t most = (T + 255) / 256;
-  if (want > most) want = most;
-  if (want < 1) want = 1;
-  const int64_t kpart = ((T + want - 1) / want + 63) / 64 * 64;
-  return {(int)((T + kpart - 1) / kpart), (int)kpart};
+Parts weight_parts(const Shape& s, int F, int tile) {
+  if (s.T == 0) return {1, 1, 64};
+  const int64_t tg = tiles(2 * (int64_t)F, s.d, tile, tile), td = tiles(s.d, F, tile, tile);
+  const int64_t range = (s.bf16 ? 2 : 1) * s.T;
+  // 256 compute units; the small tiles' workgroups share one, four at a time
+  const int64_t slots = tile == 256 ? 256 : 1024;
+  // ns of a value of k in a tile, of a tile's start and end, of a KiB of a part written and read
+  const double per_k = tile == 256 ? 55.0 : 12.0, fixed = 4000.0, per_kib = 0.5;
+  Parts best{1, 1, 64};
+  double least = 0;
+  for (int n = 1; n <= 64; ++n) {
+    const int64_t kpart = ((range + n - 1) / n + 63) / 64 * 64;
+    const int pg = (int)((s.T + kpart - 1) / kpart), pd = (int)((range + kpart - 1) / kpart);
+    const int64_t rounds = (tg * pg + td * pd + slots - 1) / slots;
+    const double elems = (pg > 1 ? 2.0 * pg : 0.0) * F * s.d + (pd > 1 ? 1.0 * pd : 0.0) * F * s.d;
+    const double ns = rounds * (kpart * per_k + fixed) + elems * 4 / 1024 * per_kib;
+    if (n == 1 || ns < least) {
+      least = ns;
+      best = {pg, pd, (int)kpart};
+    }
+  }
+  return best;
 }
 
 bool large_tiles(int64_t T, int d, int F, bool bf16) { return bf16 && tiles(T, F, 256, 128) >= 192; }
+
+template <class T, bool B_MNC>
+void launch_product(bool big, const ProductArgs& g, int workgroups, hipStream_t st) {
+  if constexpr (T::kSize == 2)
+    if (big) {
+      hipLaunchKernelGGL((product_kernel<T, 256, 256, 2, 4, B_MNC>), dim3((unsigned)workgroups), dim3(512), 0, st,
+                         g);
+      return;
+    }
+  hipLaunchKernelGGL((product_kernel<T, 64, 64, 2, 2, B_MNC>), dim3((unsigned)workgroups), dim3(256), 0, st, g);
+}
 
 template <class T>
 hipError_t run(const Shape& s, int F, const uint8_t* codes, const uint8_t* scales, const void* w_gu,
                const void* w_down, const float* dy, const float* dx_in, void* dx, void* dw_gu, void* dw_down,
                char* ws, hipStream_t st) {
   constexpr bool kBf16 = T::kSize == 2;
-  constexpr int kSmallLds = 2 * (128 + 64) * 128, kProductLds = 2 * 128 * 128;
   const int d = s.d;
   char* xb = ws;
   char* dyb = xb + up((size_t)s.T * d * T::kSize);
@@ -262,60 +288,41 @@ hipError_t run(const Shape& s, int F, const uint8_t* codes, const uint8_t* scale
     if constexpr (kBf16)
       if (large_tiles(s.T, d, F, true)) {
         done = true;
-        hipLaunchKernelGGL((hidden_kernel<T, 256, 128, 2, 2>),
-                           dim3((unsigned)tiles(s.T, F, 256, 128)), dim3(256), 2 * 512 * 128, st, h);
+        hipLaunchKernelGGL((hidden_kernel<T, 256, 128, 4, 2>),
+                           dim3((unsigned)tiles(s.T, F, 256, 128)), dim3(512), 0, st, h);
       }
     if (!done)
       hipLaunchKernelGGL((hidden_kernel<T, 64, 64, 2, 2>),
-                         dim3((unsigned)tiles(s.T, F, 64, 64)), dim3(256), kSmallLds, st, h);
+                         dim3((unsigned)tiles(s.T, F, 64, 64)), dim3(256), 0, st, h);
     if ((e = hipGetLastError())) return e;
   }
   const void* dyk = kBf16 ? (const void*)dyb : dy;
   ProductArgs g{};
-  g.parts = 1;
   if (s.T > 0) {
-    g.p[0] = {w_gu, dh, nullptr, d, 2 * (int64_t)F, s.T, d, 2 * F, 0, dx, dx_in, nullptr};
-    bool done = false;
-    if constexpr (kBf16)
-      if (tiles(s.T, d, 256, 256) >= 192) {
-        done = true;
-        g.p[0].tiles_n = (d + 255) / 256;
-        g.first = (int)tiles(s.T, d, 256, 256);
-        hipLaunchKernelGGL((product_kernel<T, 256, 256, 2, 4, false>), dim3((unsigned)g.first), dim3(512),
-                           2 * 512 * 128, st, g);
-      }
-    if (!done) {
-      g.p[0].tiles_n = (d + 63) / 64;
-      g.first = (int)tiles(s.T, d, 64, 64);
-      hipLaunchKernelGGL((product_kernel<T, 64, 64, 2, 2, false>), dim3((unsigned)g.first), dim3(256), kProductLds,
-                         st, g);
-    }
+    const bool big = kBf16 && tiles(s.T, d, 256, 256) >= 192;
+    const int tile = big ? 256 : 64;
+    const int n = (int)tiles(s.T, d, tile, tile);
+    g.p[0] = {w_gu, dh, nullptr, d, 2 * (int64_t)F, s.T, d, 2 * F, (d + tile - 1) / tile, 1, 0, dx, dx_in, nullptr};
+    g.p[1].first = n;
+    launch_product<T, false>(big, g, n, st);
     if ((e = hipGetLastError())) return e;
   }
-  const bool big = kBf16 && large_tiles(s.T, d, F, true);
+  const bool big = large_tiles(s.T, d, F, kBf16);
   const int tile = big ? 256 : 64;
-  const Parts z = weight_parts(s.T, d, F, tile);
-  g.parts = z.parts < 1 ? 1 : z.parts;
+  const Parts z = weight_parts(s, F, tile);
+  const int n0 = (int)tiles(2 * (int64_t)F, d, tile, tile) * z.gu, n1 = (int)tiles(d, F, tile, tile) * z.down;
   g.kpart = z.kpart;
-  g.p[0] = {xb, dh, nullptr, d, 2 * (int64_t)F, 2 * (int64_t)F, d, (int)s.T, (d + tile - 1) / tile, dw_gu, nullptr,
-            (float*)part};
-  g.p[1] = {act, dyk, kBf16 ? dyl : nullptr, F, d, d, F, (int)s.T, (F + tile - 1) / tile, dw_down, nullptr,
-            (float*)part + (size_t)g.parts * 2 * F * d};
-  g.first = (int)tiles(2 * (int64_t)F, d, tile, tile);
-  const unsigned n = (unsigned)(g.first + tiles(d, F, tile, tile));
-  bool done = false;
-  if constexpr (kBf16)
-    if (big) {
-      done = true;
-      hipLaunchKernelGGL((product_kernel<T, 256, 256, 2, 4, true>), dim3(n, g.parts), dim3(512), 2 * 512 * 128, st, g);
-    }
-  if (!done)
-    hipLaunchKernelGGL((product_kernel<T, 64, 64, 2, 2, true>), dim3(n, g.parts), dim3(256), kProductLds, st, g);
+  g.p[0] = {xb, dh, nullptr, d, 2 * (int64_t)F, 2 * (int64_t)F, d, (int)s.T, (d + tile - 1) / tile, z.gu, 0, dw_gu,
+            nullptr, (float*)part};
+  g.p[1] = {act, dyk, kBf16 ? dyl : nullptr, F, d, d, F, (int)s.T, (F + tile - 1) / tile, z.down, n0, dw_down, nullptr,
+            (float*)part + (z.gu > 1 ? (size_t)z.gu * 2 * F * d : 0)};
+  launch_product<T, true>(big, g, n0 + n1, st);
   if ((e = hipGetLastError())) return e;
-  if (g.parts > 1) {
-    const int64_t n4 = (int64_t)F * d / 2, all = n4 + (int64_t)F * d / 4, blocks = (all + 255) / 256;
+  if (z.down > 1) {  // (and with it perhaps z.gu: dW_down has as many parts as dW_gu or more)
+    const int64_t first = z.gu > 1 ? (int64_t)F * d / 2 : 0, all = first + (int64_t)F * d / 4;
+    const int64_t blocks = (all + 255) / 256;
     hipLaunchKernelGGL(add_parts_kernel<T>, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), 0, st, g,
-                       n4, all);
+                       first, all);
   }
   return hipGetLastError();
 }
@@ -325,9 +332,9 @@ hipError_t run(const Shape& s, int F, const uint8_t* codes, const uint8_t* scale
 size_t shared_backward_ws_bytes(const Shape& s, int F) {
   const size_t size = s.bf16 ? 2 : 4, T = (size_t)s.T;
   const int tile = large_tiles(s.T, s.d, F, s.bf16) ? 256 : 64;
-  const Parts z = weight_parts(s.T, s.d, F, tile);
+  const Parts z = weight_parts(s, F, tile);
   return up(T * s.d * size) + (s.bf16 ? 2 * up(T * s.d * 2) : 0) + up(T * 2 * F * size) + up(T * F * size) +
-         (z.parts > 1 ? up((size_t)z.parts * 3 * F * s.d * 4) : 0);
+         up(((z.gu > 1 ? 2 * (size_t)z.gu : 0) + (z.down > 1 ? (size_t)z.down : 0)) * F * s.d * 4);
 }
 
 hipError_t launch_shared_backward(const Shape& s, int F, const uint8_t* codes, const uint8_t* scales,
