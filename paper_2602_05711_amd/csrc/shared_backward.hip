@@ -66,24 +66,23 @@ __global__ __launch_bounds__(64 * WR * WC) void hidden_kernel(HiddenArgs p) {
   tg_f32x16 gu[2 * FI][MJ], da[FI][MJ];
   tile_zero(gu);
   tile_zero(da);
+  TileOperand<T, TM, false, NW> x;  // rows of x~, then of dy: both [T, d]
+  x.init((const elem*)p.x + m0 * p.d, p.d, wid, lane, token);
   {
     TileOperand<T, 2 * FN, false, NW> w;
-    TileOperand<T, TM, false, NW> x;
     w.init((const elem*)p.w_gu, p.d, wid, lane, [&](int r) {
       const int f = f0 + (r < FN ? r : r - FN);
       return (f < F ? f : F - 1) + (r < FN ? 0 : F);
     });
-    x.init((const elem*)p.x + m0 * p.d, p.d, wid, lane, token);
     const TileRange all[2] = {{p.d, 0, 0}, {0, 0, 0}};
     tile_sum<T>(w, x, all, a2, b0, st0, st1, wid, lane, gu);
   }
   {
     TileOperand<T, FN, true, NW> w;
-    TileOperand<T, TM, false, NW> y;
     w.init((const elem*)p.w_down, F, wid, lane, [&](int r) { return f0 + r < F ? f0 + r : F - w.kPer; });
-    y.init((const elem*)p.dy + m0 * p.d, p.d, wid, lane, token);
+    x.base = (const char*)((const elem*)p.dy + m0 * p.d);
     const TileRange both[2] = {{p.d, 0, 0}, {T::kSize == 2 ? p.d : 0, 0, (const char*)p.dy_lo - (const char*)p.dy}};
-    tile_sum<T>(w, y, both, a1, b0, st0, st1, wid, lane, da);
+    tile_sum<T>(w, x, both, a1, b0, st0, st1, wid, lane, da);
   }
 #pragma unroll
   for (int j = 0; j < MJ; ++j) {

@@ -112,7 +112,9 @@ struct TileOperand {
       asm volatile("" : "+v"(l));  // nothing of this branch is worth a register in the loop
 #pragma unroll
       for (int i = 0; i < kCopies; ++i) {
-        const char* const p = kt * T::kStep + chunk_k(i, l, wid) < K ? from + off[i] : (const char*)&tile_zeros;
+        uint32_t o = off[i];
+        asm volatile("" : "+v"(o));
+        const char* const p = kt * T::kStep + chunk_k(i, l, wid) < K ? from + o : (const char*)&tile_zeros;
         __builtin_amdgcn_global_load_lds((const void*)p, (tg_lds_ptr)(st + (to + i * 1024)), 16, 0, 0);
       }
     }
