@@ -1,6 +1,6 @@
 /*
  * omnimoe_ffn.h - the feed-forward layer around the routed branch (libomnimoe.so): the shared branch's training step
- * on 8-bit activation checkpoints.
+ * on 8-bit activation checkpoints, and the whole layer for a few tokens.
  *
  * Conventions as in omnimoe.h: device pointers owned by the caller, row-major, contiguous, 16-byte aligned; nothing is
  * allocated; every call is asynchronous on `stream`, checked on the host before anything is launched, and may run
@@ -53,6 +53,24 @@ omnimoe_status omnimoe_shared_mlp_backward(const omnimoe_layer_desc* desc, int32
                                            const uint8_t* scales, const void* w_gu, const void* w_down,
                                            const float* dy, const float* dx_in, void* dx, void* dw_gu, void* dw_down,
                                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* The whole feed-forward layer (Eq. 7) for a decode step of a few tokens, in two kernels: omnimoe_layer_forward's routed
+ * branch and, with d_ff > 0, omnimoe_shared_mlp's shared branch added to it.
+ *   x, keys_row, keys_col, u, v   as in omnimoe_layer_forward (the whole descriptor counts; group_size is not used)
+ *   w_gu, w_down                  as in omnimoe_shared_mlp; not used with d_ff = 0, and may then be NULL
+ *   y [T, d] fp32 out;  idx_out, gates_out [T, H, K] out, as omnimoe_route's, may be NULL
+ * The selection is exact on the fp32 logits, ties to the lower id. Routed sums are fp32 in (head, slot) order, each head's
+ * by itself; the shared branch's hidden values enter the down projection unrounded, so that y has fp32's accuracy for
+ * both types. Results agree with omnimoe_layer_forward's and omnimoe_shared_mlp's to the
+ * rounding of their sums (and, for bf16 layers, of the hidden values there); logits summed in another order can put
+ * near-ties the other way. T <= OMNIMOE_FEW_TOKENS and K <= 64, else OMNIMOE_ERR_UNSUPPORTED. T = 0 is a no-op.
+ * Workspace: omnimoe_layer_few_workspace_size bytes. */
+#define OMNIMOE_FEW_TOKENS 16
+omnimoe_status omnimoe_layer_few_workspace_size(const omnimoe_layer_desc* desc, int32_t d_ff, size_t* bytes);
+omnimoe_status omnimoe_layer_forward_few(const omnimoe_layer_desc* desc, int32_t d_ff, const void* x,
+                                         const void* keys_row, const void* keys_col, const void* u, const void* v,
+                                         const void* w_gu, const void* w_down, float* y, int32_t* idx_out,
+                                         float* gates_out, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -89,6 +89,8 @@ def load_library():
         "omnimoe_checkpoint_load": [D, P, P, P, P],
         "omnimoe_shared_mlp_backward_workspace_size": [D, I32, ctypes.POINTER(SZ)],
         "omnimoe_shared_mlp_backward": [D, I32, P, P, P, P, P, P, P, P, P, P, SZ, P],
+        "omnimoe_layer_few_workspace_size": [D, I32, ctypes.POINTER(SZ)],
+        "omnimoe_layer_forward_few": [D, I32, P, P, P, P, P, P, P, P, P, P, P, SZ, P],
         "omnimoe_timer_create": [I32, ctypes.POINTER(P)],
         "omnimoe_timer_destroy": [P],
         "omnimoe_timer_read": [P, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(I32)],
@@ -337,8 +339,9 @@ class Timer:
 
 EXPORTED_FFN = (
     "omnimoe_checkpoint_store", "omnimoe_checkpoint_load", "omnimoe_shared_mlp_backward_workspace_size",
-    "omnimoe_shared_mlp_backward",
+    "omnimoe_shared_mlp_backward", "omnimoe_layer_few_workspace_size", "omnimoe_layer_forward_few",
 )
+FEW_TOKENS = 16  # OMNIMOE_FEW_TOKENS
 
 
 def _ffn_call(fn, desc, tensors, call, stream):
@@ -417,3 +420,28 @@ def omnimoe_shared_mlp_backward(desc, d_ff, codes, scales, w_gu, w_down, dy, dx_
         lambda st: load_library().omnimoe_shared_mlp_backward(
             ctypes.byref(desc), d_ff, _ptr(codes), _ptr(scales), _ptr(w_gu), _ptr(w_down), _ptr(dy), _ptr(dx_in),
             _ptr(dx), _ptr(dw_gu), _ptr(dw_down), _ptr(ws), ws.numel(), st), stream)
+
+
+def omnimoe_layer_few_workspace_size(desc, d_ff: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check("omnimoe_layer_few_workspace_size",
+           load_library().omnimoe_layer_few_workspace_size(ctypes.byref(desc), d_ff, ctypes.byref(n)))
+    return n.value
+
+
+def omnimoe_layer_forward_few(desc, d_ff, x, keys_row, keys_col, u, v, w_gu, w_down, y, idx_out=None, gates_out=None,
+                              ws=None, stream=None):
+    """The whole feed-forward layer for up to FEW_TOKENS tokens; without a shared branch d_ff is 0 and its weights None."""
+    import torch
+    ws = _bytes_ws(ws, lambda: omnimoe_layer_few_workspace_size(desc, d_ff), x.device)
+    T, d, H, K, dt = desc.T, desc.d, desc.H, desc.K, _layer_dtype(desc)
+    N = desc.n_rows * desc.n_cols
+    _ffn_call("omnimoe_layer_forward_few", desc, (
+        ("x", x, dt, T * d), ("keys_row", keys_row, dt, H * desc.n_rows * desc.d_key),
+        ("keys_col", keys_col, dt, H * desc.n_cols * desc.d_key), ("u", u, dt, N * d), ("v", v, dt, N * d),
+        ("w_gu", w_gu, dt, 2 * d_ff * d), ("w_down", w_down, dt, d * d_ff), ("y", y, torch.float32, T * d),
+        ("idx_out", idx_out, torch.int32, T * H * K), ("gates_out", gates_out, torch.float32, T * H * K),
+        ("ws", ws, torch.uint8, ws.numel())),
+        lambda st: load_library().omnimoe_layer_forward_few(
+            ctypes.byref(desc), d_ff, _ptr(x), _ptr(keys_row), _ptr(keys_col), _ptr(u), _ptr(v), _ptr(w_gu),
+            _ptr(w_down), _ptr(y), _ptr(idx_out), _ptr(gates_out), _ptr(ws), ws.numel(), st), stream)

@@ -1,0 +1,544 @@
+// The whole feed-forward layer (Eq. 7: routed and shared branch) for up to sixteen tokens in two kernels.
+//
+//   few_products  every product that needs only x: the row and column logits (Eq. 9) and the shared branch's hidden
+//                 values a = silu(W_g x) (.) (W_u x). Reading the sub-keys and W_g, W_u once is its cost.
+//   few_finish    a workgroup per (token, head) selects (Eq. 11, 1, 2), forms g act(x . u) of its K picks and adds their
+//                 a v rows; further workgroups form the down projection of all tokens beside it. Whoever finishes a
+//                 token last (a counter) adds the token's partial rows, heads in order, then the shared branch's.
+//
+// Few tokens leave the matrix cores idle, so that a tile of sixteen weight rows x sixteen tokens (v_mfma 16x16) costs
+// nothing beside the loads, whatever T is. A lane reads 32 neighbouring bytes of a row in two loads, so that two
+// instructions cover sixteen whole 128-byte lines; the sum runs over k in that permuted order, the same for both
+// operands. A workgroup's waves split k and their tiles are added in wave order through LDS.
+//
+// The partial rows and the counters cross XCDs inside one kernel, whose L2s are not coherent with each other: partial
+// rows are stored and loaded at agent scope (past L2), every thread waits for its stores (vmcnt) before the barrier
+// behind which one thread counts the workgroup in, and nothing waits for another workgroup.
+#include <type_traits>
+
+#include "cand_table.hpp"
+#include "device_common.hpp"
+#include "internal.hpp"
+
+namespace omnimoe {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kTokens = 16;
+constexpr int kSplit = 3;  // bf16 values of a hidden value
+
+struct FewArgs {
+  const void *x, *keys[2], *u, *v, *w_gu, *w_down;
+  float* y;
+  int32_t* idx;   // or NULL
+  float* gates;   // or NULL
+  float* logits;  // [T H, npad[0] + npad[1]]
+  void* act;      // bf16: [kSplit][kTokens, F]; fp32: [kTokens, F]
+  float* part;    // [T H, d] the heads' sums
+  float* shared;  // [T, d] the down projection
+  int* count;     // [kTokens] workgroups that are done with the token
+  int64_t N;
+  int T, d, F, H, K, act_kind, dk, col0;
+  int n[2], npad[2];
+  int key_groups[2];  // workgroups of sixteen sub-keys per half
+  int down_groups;    // workgroups of sixteen output columns
+};
+
+// 16 rows x 16 tokens: acc of lane l, register q is row 4 (l / 16) + q, token l % 16.
+template <bool BF16>
+struct Chunk;  // 16 bytes of a row
+template <>
+struct Chunk<true> {
+  static constexpr int kElems = 8;
+  static __device__ __forceinline__ void mma(f32x4& acc, const uint4& a, const uint4& b) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc,
+                                                  0, 0, 0);
+  }
+};
+template <>
+struct Chunk<false> {
+  static constexpr int kElems = 4;
+  static __device__ __forceinline__ void mma(f32x4& acc, const uint4& a, const uint4& b) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+  }
+};
+
+// Steps of four lanes x 32 bytes (128 bytes of every row) of wave w among W: the rows' chunks in units of 16 bytes.
+// row: this lane's weight row; tok: this lane's token row in each of NB token operands (lanes past the last token have
+// that one's: their columns of the tile are not used). The loads are unconditional; chunks past the row's end read its
+// last one, and the weights' are then zeros.
+template <bool BF16, int NB, int W>
+__device__ __forceinline__ f32x4 wave_tile(const uint4* row, const uint4* const (&tok)[NB], int chunks, int w) {
+  const int quad = (threadIdx.x & 63) >> 4;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 4;  // steps in flight: 8 + 8 NB loads a lane
+  auto steps = [&](int s0, auto whole) {
+    uint4 a[U][2], b[U][2][NB];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        int c = (s0 + i) * 8 + quad * 2 + e;
+        if constexpr (!decltype(whole)::value) c = c < chunks ? c : chunks - 1;
+        a[i][e] = row[c];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) b[i][e][n] = tok[n][c];
+      }
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if constexpr (!decltype(whole)::value)
+          if ((s0 + i) * 8 + quad * 2 + e >= chunks) a[i][e] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) Chunk<BF16>::mma(acc, a[i][e], b[i][e][n]);
+      }
+  };
+  int s0 = w * U;
+  for (; (s0 + U) * 8 <= chunks; s0 += W * U) steps(s0, std::true_type{});
+  if (s0 * 8 < chunks) steps(s0, std::false_type{});
+  return acc;
+}
+
+// Sum of the W waves' tiles in wave order, on wave 0.
+template <int W>
+__device__ __forceinline__ f32x4 add_tiles(f32x4 acc, f32x4 (&lds)[W][64], int w, int l) {
+  lds[w][l] = acc;
+  __syncthreads();
+  if (w == 0)
+#pragma unroll
+    for (int i = 1; i < W; ++i) acc += lds[i][l];
+  return acc;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void few_products(FewArgs p) {
+  constexpr int W = 4, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
+  __shared__ f32x4 tiles[W][64];
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, t = l & 15;
+  if (blockIdx.x == 0 && threadIdx.x < kTokens) p.count[threadIdx.x] = 0;
+  const char* const x = (const char*)p.x + (int64_t)(t < p.T ? t : p.T - 1) * p.d * kSize;
+  int g = blockIdx.x;
+  const int half = g < p.key_groups[0] ? 0 : 1;
+  if (half) g -= p.key_groups[0];
+  if (g < (half ? p.key_groups[1] : p.key_groups[0])) {
+    const int n = half ? p.n[1] : p.n[0], rows = p.H * n, r0 = g * 16, r = r0 + t < rows ? r0 + t : rows - 1;
+    const uint4* const tok[1] = {(const uint4*)(x + (half ? p.col0 * kSize : 0))};
+    const uint4* const row = (const uint4*)((const char*)(half ? p.keys[1] : p.keys[0]) + (int64_t)r * p.dk * kSize);
+    const f32x4 acc = add_tiles<W>(wave_tile<BF16, 1, W>(row, tok, p.dk / E, w), tiles, w, l);
+    if (w == 0 && t < p.T)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int key = r0 + 4 * (l >> 4) + q;
+        if (key >= rows) break;
+        const int h = key / n, i = key - h * n;
+        p.logits[((int64_t)t * p.H + h) * (p.npad[0] + p.npad[1]) + (half ? p.npad[0] : 0) + i] = acc[q];
+      }
+    return;
+  }
+  // eight features: a lane's four accumulators are the gate and up values of two of them
+  const int f0 = (g - p.key_groups[1]) * 8, f = f0 + 2 * (t >> 2) + (t & 1);
+  const int r = (f < p.F ? f : p.F - 1) + (t & 2 ? p.F : 0);
+  const uint4* const tok[1] = {(const uint4*)x};
+  const uint4* const row = (const uint4*)((const char*)p.w_gu + (int64_t)r * p.d * kSize);
+  const f32x4 acc = add_tiles<W>(wave_tile<BF16, 1, W>(row, tok, p.d / E, w), tiles, w, l);
+  if (w == 0) {
+    const int fo = f0 + 2 * (l >> 4);
+    const float a0 = activation(1, acc[0]) * acc[2], a1 = activation(1, acc[1]) * acc[3];
+    if constexpr (BF16) {
+      // three bf16 values a feature, their sum a itself: the down projection keeps fp32's accuracy
+      float r0 = a0, r1 = a1;
+#pragma unroll
+      for (int n = 0; n < kSplit; ++n) {
+        const uint32_t h0 = bf16_rne(r0), h1 = bf16_rne(r1);
+        *(uint32_t*)((uint16_t*)p.act + (n * kTokens + t) * p.F + fo) = h0 | (h1 << 16);
+        r0 -= __uint_as_float(h0 << 16);
+        r1 -= __uint_as_float(h1 << 16);
+      }
+    } else {
+      *(float2*)((float*)p.act + t * p.F + fo) = make_float2(a0, a1);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- few_finish
+
+__device__ __forceinline__ void store_agent(float* p, float a, float b) {
+  __hip_atomic_store((uint64_t*)p, ((uint64_t)__float_as_uint(b) << 32) | __float_as_uint(a), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float4 load_agent4(const float* p) {
+  const uint64_t a = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const uint64_t b = __hip_atomic_load((const uint64_t*)(p + 2), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float4(__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)(a >> 32)), __uint_as_float((uint32_t)b),
+                     __uint_as_float((uint32_t)(b >> 32)));
+}
+
+constexpr int kThreads = 512, kWaves = 8;
+
+// y of token t from its heads' sums and the down projection's, by the whole workgroup.
+__device__ __forceinline__ void add_token(const FewArgs& p, int t) {
+  for (int c = threadIdx.x * 4; c < p.d; c += kThreads * 4) {
+    const float* part = p.part + (int64_t)t * p.H * p.d + c;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int h0 = 0; h0 < p.H; h0 += 8) {
+      float4 r[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (h0 + i < p.H) r[i] = load_agent4(part + (int64_t)(h0 + i) * p.d);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (h0 + i < p.H) {
+          s.x += r[i].x;
+          s.y += r[i].y;
+          s.z += r[i].z;
+          s.w += r[i].w;
+        }
+    }
+    if (p.F) {
+      const float4 r = load_agent4(p.shared + (int64_t)t * p.d + c);
+      s.x += r.x;
+      s.y += r.y;
+      s.z += r.z;
+      s.w += r.w;
+    }
+    *(float4*)(p.y + (int64_t)t * p.d + c) = s;
+  }
+}
+
+// This wave's half of a row: its best kh of n logits, best first (logit descending, index ascending), as keys (value
+// order high, ~index low) in out[0 .. kh). The logits that reach a threshold that at least kh of them reach (the kh-th
+// largest of the lanes' maxima, its low bits cleared) are ranked by counting; more than 64 of them (ties) are taken one
+// after the other instead.
+template <int R>
+__device__ __forceinline__ void half_best(const float* __restrict__ logits, int n, int kh, uint64_t* __restrict__ cand,
+                                          uint64_t* __restrict__ out) {
+  const int l = lane_id();
+  uint32_t o[R];
+  uint32_t most = 0u;
+#pragma unroll
+  for (int c = 0; c < R / 4; ++c) {
+    const float4 v = *(const float4*)(logits + 256 * c + 4 * l < logits + n ? logits + 256 * c + 4 * l : logits);
+    const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o[4 * c + q] = 256 * c + 4 * l + q < n ? ord_f32(e[q]) : 0u;
+  }
+#pragma unroll
+  for (int k = 0; k < R; ++k) most = o[k] > most ? o[k] : most;
+  uint32_t th = 0u;
+#pragma unroll
+  for (int b = 31; b >= 8; --b) {
+    const uint32_t c = th | (1u << b);
+    if (__popcll(__ballot(most >= c)) >= kh) th = c;
+  }
+  auto index = [&](int k) { return 256 * (k >> 2) + 4 * l + (k & 3); };
+  auto key = [&](int k) { return ((uint64_t)o[k] << 32) | (0xFFFFFFFFu - (uint32_t)index(k)); };
+  int total = 0;
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    const bool in = o[k] >= th && index(k) < n;
+    const uint64_t m = __ballot(in);
+    const int at = total + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32),
+                                                          __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+    if (in && at < 64) cand[at] = key(k);
+    total += __popcll(m);
+  }
+  if (l >= total) cand[l] = 0ull;
+  wave_lds_sync();
+  if (total <= 64) {
+    const uint64_t mine = cand[l];
+    int rank = 0;
+    for (int j = 0; j < total; j += 8) {
+      ulonglong2 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = *(const ulonglong2*)(cand + j + 2 * i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rank += (v[i].x > mine ? 1 : 0) + (v[i].y > mine ? 1 : 0);
+    }
+    if (l < total && rank < kh) out[rank] = mine;
+  } else {
+    uint64_t last = ~0ull;
+    for (int j = 0; j < kh; ++j) {
+      uint64_t m = 0ull;
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const uint64_t v = index(k) < n ? key(k) : 0ull;
+        m = v < last && v > m ? v : m;
+      }
+#pragma unroll
+      for (int b = 32; b >= 1; b >>= 1) {
+        const uint64_t v = shfl_xor_u64(m, b);
+        m = v > m ? v : m;
+      }
+      if (l == 0) out[j] = m;
+      last = m;
+    }
+  }
+}
+
+struct FinishShared {
+  union {
+    f32x4 tiles[kWaves][64];
+    struct {
+      uint64_t cand[2][64], best[2][64];
+      uint4 cell[288];  // score (order map of the double), id
+      uint64_t pick_score[64];
+      uint32_t pick_id[64];
+      float a[64];
+    };
+  };
+  int last;
+};
+
+template <bool BF16>
+__device__ __forceinline__ void down_group(const FewArgs& p, FinishShared& sh, int g) {
+  constexpr int E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4, NB = BF16 ? kSplit : 1;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, t = l & 15;
+  const int r = g * 16 + t < p.d ? g * 16 + t : p.d - 1;
+  const uint4* const row = (const uint4*)((const char*)p.w_down + (int64_t)r * p.F * kSize);
+  // (the hidden values of lanes past the last token are that token's again)
+  auto act = [&](int n) { return (const uint4*)((const char*)p.act + (int64_t)(n * kTokens + t) * p.F * kSize); };
+  f32x4 acc;
+  if constexpr (BF16) {
+    const uint4* const tok[NB] = {act(0), act(1), act(2)};
+    acc = wave_tile<BF16, NB, kWaves>(row, tok, p.F / E, w);
+  } else {
+    const uint4* const tok[NB] = {act(0)};
+    acc = wave_tile<BF16, NB, kWaves>(row, tok, p.F / E, w);
+  }
+  acc = add_tiles<kWaves>(acc, sh.tiles, w, l);
+  int mine = 0;
+  if (w == 0) {
+    const int c = g * 16 + 4 * (l >> 4);
+    if (t < p.T && c < p.d) {
+      float* const o = p.shared + (int64_t)t * p.d + c;
+      store_agent(o, acc[0], acc[1]);
+      store_agent(o + 2, acc[2], acc[3]);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the wave's stores are past L2
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");
+    if (l < p.T)
+      mine = __hip_atomic_fetch_add(p.count + l, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+             p.H + p.down_groups - 1;
+    const uint64_t m = __ballot(mine);
+    if (l == 0) sh.last = (int)m;
+  }
+  __syncthreads();
+  for (int m = sh.last; m; m &= m - 1) add_token(p, __builtin_ctz(m));
+}
+
+template <bool BF16, int R>
+__global__ __launch_bounds__(kThreads) void few_finish(FewArgs p) {
+  __shared__ FinishShared sh;
+  if ((int)blockIdx.x >= p.T * p.H) {
+    down_group<BF16>(p, sh, (int)blockIdx.x - p.T * p.H);
+    return;
+  }
+  constexpr int E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
+  const int row = blockIdx.x, t = row / p.H, K = p.K;
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kr = K < p.n[0] ? K : p.n[0], kc = K < p.n[1] ? K : p.n[1];
+  if (w < 2)
+    half_best<R>(p.logits + (int64_t)row * (p.npad[0] + p.npad[1]) + (w ? p.npad[0] : 0), w ? p.n[1] : p.n[0],
+                 w ? kc : kr, sh.cand[w], sh.best[w]);
+  __syncthreads();
+  // The candidate cells, ranked by counting (score descending, id ascending).
+  const int first = kCand.first[K], cells = kCand.first[K + 1] - first;
+  uint64_t score = 0ull;
+  uint32_t id = 0u;
+  bool cell = false;
+  if ((int)threadIdx.x < cells) {
+    const int ab = kCand.cell[first + threadIdx.x], a = ab >> 8, b = ab & 0xFF;
+    cell = a < kr && b < kc;
+    if (cell) {
+      const uint64_t ka = sh.best[0][a], kb = sh.best[1][b];
+      score = ord_f64((double)f32_from_ord((uint32_t)(ka >> 32)) + (double)f32_from_ord((uint32_t)(kb >> 32)));
+      id = (0xFFFFFFFFu - (uint32_t)ka) * (uint32_t)p.n[1] + (0xFFFFFFFFu - (uint32_t)kb);
+    }
+  }
+  if (threadIdx.x < 288)  // (no cell: below every score)
+    sh.cell[threadIdx.x] = make_uint4((uint32_t)score, (uint32_t)(score >> 32), cell ? id : 0xFFFFFFFFu, 0u);
+  __syncthreads();
+  if (cell) {
+    int rank = 0;
+    for (int j = 0; j < cells; j += 8) {  // at most 280 of them
+      uint4 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = sh.cell[j + i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint64_t s = ((uint64_t)v[i].y << 32) | v[i].x;
+        rank += s > score || (s == score && v[i].z < id) ? 1 : 0;
+      }
+    }
+    if (rank < K) {
+      sh.pick_score[rank] = score;
+      sh.pick_id[rank] = id;
+    }
+  }
+  __syncthreads();
+  // Gates, on every wave: lane k has pick k's.
+  const uint32_t eid = sh.pick_id[l < K ? l : 0];
+  const double s0 = f64_from_ord(sh.pick_score[0]);
+  const float e = l < K ? expf((float)(f64_from_ord(sh.pick_score[l < K ? l : 0]) - s0)) : 0.0f;
+  const float gate = e / wave_sum_f32(e);
+  if (w == 0 && l < K) {
+    if (p.idx) p.idx[(int64_t)row * K + l] = (int32_t)eid;
+    if (p.gates) p.gates[(int64_t)row * K + l] = gate;
+  }
+  // x . u of picks w, w + 8, ..., two at a time; the first v rows are requested right after the first u rows.
+  // (Loads are unconditional: a chunk past the row's end reads its last one and counts as zeros.)
+  constexpr int kAhead = 16;
+  typedef typename std::conditional<BF16, uint2, uint4>::type Raw;  // four values
+  Raw vr[kAhead];
+  const int c0 = threadIdx.x * 4;
+  auto load_v = [&](int k0, int c) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const uint32_t pick = sh.pick_id[k0 + k < K ? k0 + k : K - 1];
+      vr[k] = *(const Raw*)((const char*)p.v + ((int64_t)pick * p.d + (c < p.d ? c : 0)) * kSize);
+    }
+  };
+  {
+    const uint4* const x = (const uint4*)((const char*)p.x + (int64_t)t * p.d * kSize);
+    const int chunks = p.d / E;
+    uint4 xr[4], ur[2][4];
+    auto load_u = [&](int k, int q) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xr[i] = x[q + 64 * i < chunks ? q + 64 * i : chunks - 1];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const uint32_t pick = (uint32_t)readlane_i32((int)eid, k + n * kWaves < K ? k + n * kWaves : k);
+        const uint4* const u = (const uint4*)((const char*)p.u + (int64_t)pick * p.d * kSize);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ur[n][i] = u[q + 64 * i < chunks ? q + 64 * i : chunks - 1];
+      }
+    };
+    if (w < K) load_u(w, l);
+    load_v(0, c0);
+    for (int k = w; k < K; k += 2 * kWaves) {
+      float acc[2] = {0.0f, 0.0f};
+      for (int q = 0; q < chunks; q += 256) {
+        if (k != w || q) load_u(k, q + l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (q + l + 64 * i >= chunks) xr[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) acc[n] = chunk_dot<BF16>(ur[n][i], xr[i], acc[n]);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const float h = wave_sum_uniform(acc[n]);
+        if (l == k + n * kWaves && l < K) sh.a[l] = gate * activation(p.act_kind, h);
+      }
+    }
+  }
+  __syncthreads();
+  float* const out = p.part + (int64_t)row * p.d;
+  for (int c = c0; c < p.d; c += kThreads * 4) {
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = 0; k0 < K; k0 += kAhead) {
+      if (c != c0 || k0) load_v(k0, c);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (k0 + k < K) {
+          const float a = sh.a[k0 + k];
+          float4 r;
+          if constexpr (BF16) r = make_float4(bf16_lo(vr[k].x), bf16_hi(vr[k].x), bf16_lo(vr[k].y), bf16_hi(vr[k].y));
+          else r = __builtin_bit_cast(float4, vr[k]);
+          s.x = fmaf(a, r.x, s.x);
+          s.y = fmaf(a, r.y, s.y);
+          s.z = fmaf(a, r.z, s.z);
+          s.w = fmaf(a, r.w, s.w);
+        }
+    }
+    store_agent(out + c, s.x, s.y);
+    store_agent(out + c + 2, s.z, s.w);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's stores are past L2
+  __syncthreads();
+  if (threadIdx.x == 0)
+    sh.last = __hip_atomic_fetch_add(p.count + t, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+              p.H + p.down_groups - 1;
+  __syncthreads();
+  if (sh.last) add_token(p, t);
+}
+
+size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
+int pad(int n) { return (n + 3) / 4 * 4; }
+
+}  // namespace
+
+bool few_fits(const Shape& s) { return s.T <= kTokens && s.K <= kCandK; }
+
+size_t few_ws_bytes(const Shape& s, int F) {
+  return up((size_t)s.rows * (pad(s.nr) + pad(s.nc)) * 4) + up((size_t)kTokens * F * (s.bf16 ? 2 * kSplit : 4)) +
+         up((size_t)s.rows * s.d * 4) + up(F ? (size_t)s.T * s.d * 4 : 0) + 256;
+}
+
+hipError_t launch_few(const Shape& s, int F, const void* x, const void* keys_row, const void* keys_col, const void* u,
+                      const void* v, const void* w_gu, const void* w_down, float* y, int32_t* idx, float* gates,
+                      void* ws, hipStream_t st) {
+  FewArgs p;
+  p.x = x;
+  p.keys[0] = keys_row;
+  p.keys[1] = keys_col;
+  p.u = u;
+  p.v = v;
+  p.w_gu = w_gu;
+  p.w_down = w_down;
+  p.y = y;
+  p.idx = idx;
+  p.gates = gates;
+  p.N = s.N;
+  p.T = (int)s.T;
+  p.d = s.d;
+  p.F = F;
+  p.H = s.H;
+  p.K = s.K;
+  p.act_kind = s.act;
+  p.dk = s.dk;
+  p.col0 = s.col0;
+  p.n[0] = s.nr;
+  p.n[1] = s.nc;
+  for (int i = 0; i < 2; ++i) {
+    p.npad[i] = pad(p.n[i]);
+    p.key_groups[i] = (int)(((int64_t)s.H * p.n[i] + 15) / 16);
+  }
+  p.down_groups = F ? (s.d + 15) / 16 : 0;
+  char* w = (char*)ws;
+  p.count = (int*)w;
+  w += 256;
+  p.logits = (float*)w;
+  w += up((size_t)s.rows * (p.npad[0] + p.npad[1]) * 4);
+  p.act = w;
+  w += up((size_t)kTokens * F * (s.bf16 ? 2 * kSplit : 4));
+  p.part = (float*)w;
+  w += up((size_t)s.rows * s.d * 4);
+  p.shared = (float*)w;
+  const dim3 products((unsigned)(p.key_groups[0] + p.key_groups[1] + F / 8));
+  if (s.bf16) hipLaunchKernelGGL(few_products<true>, products, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL(few_products<false>, products, dim3(256), 0, st, p);
+  const dim3 finish((unsigned)(s.rows + p.down_groups));
+  const int n = s.nr > s.nc ? s.nr : s.nc;
+#define OMNIMOE_FEW(R_)                                                                         \
+  do {                                                                                          \
+    if (s.bf16) hipLaunchKernelGGL((few_finish<true, R_>), finish, dim3(kThreads), 0, st, p);   \
+    else hipLaunchKernelGGL((few_finish<false, R_>), finish, dim3(kThreads), 0, st, p);         \
+  } while (0)
+  if (n <= 256) OMNIMOE_FEW(4);
+  else if (n <= 512) OMNIMOE_FEW(8);
+  else if (n <= 1024) OMNIMOE_FEW(16);
+  else if (n <= 2048) OMNIMOE_FEW(32);
+  else OMNIMOE_FEW(64);
+#undef OMNIMOE_FEW
+  return hipGetLastError();
+}
+
+}  // namespace omnimoe

@@ -252,4 +252,12 @@ hipError_t launch_shared_backward(const Shape& s, int d_ff, const uint8_t* codes
                                   const void* w_gu, const void* w_down, const float* dy, const float* dx_in, void* dx,
                                   void* dw_gu, void* dw_down, void* ws, hipStream_t st);
 
+// The whole feed-forward layer for a few tokens (few.hip), where few_fits(s): T <= 16, K <= 64. d_ff = 0: no shared
+// branch (w_gu and w_down unused). idx and gates may be NULL. Workspace: few_ws_bytes(s, d_ff).
+bool few_fits(const Shape& s);
+size_t few_ws_bytes(const Shape& s, int d_ff);
+hipError_t launch_few(const Shape& s, int d_ff, const void* x, const void* keys_row, const void* keys_col,
+                      const void* u, const void* v, const void* w_gu, const void* w_down, float* y, int32_t* idx,
+                      float* gates, void* ws, hipStream_t st);
+
 }  // namespace omnimoe
