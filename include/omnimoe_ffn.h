@@ -1,6 +1,6 @@
 /*
  * omnimoe_ffn.h - the feed-forward layer around the routed branch (libomnimoe.so): the shared branch's training step
- * on 8-bit activation checkpoints, and the whole layer for a few tokens.
+ * on 8-bit activation checkpoints, the shared branch with low-rank adapters, and the whole layer for a few tokens.
  *
  * Conventions as in omnimoe.h: device pointers owned by the caller, row-major, contiguous, 16-byte aligned; nothing is
  * allocated; every call is asynchronous on `stream`, checked on the host before anything is launched, and may run
@@ -71,6 +71,44 @@ omnimoe_status omnimoe_layer_forward_few(const omnimoe_layer_desc* desc, int32_t
                                          const void* keys_row, const void* keys_col, const void* u, const void* v,
                                          const void* w_gu, const void* w_down, float* y, int32_t* idx_out,
                                          float* gates_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Low-rank adapters of the shared branch's projections, side by side in tables of n slots. All of a table's slots have the
+ * same rank (a smaller one is filled up with zeros). Only slots that a token names are read.
+ *   n       slots, 0 <= n <= 8192 (else OMNIMOE_ERR_UNSUPPORTED); with n = 0 the tables may be NULL
+ *   rank    8 <= rank <= 256, rank % 8 == 0
+ *   a_gu    [n, 2 rank, d]      dtype   the gate projection's A, then the up projection's
+ *   b_gu    [n, 2 d_ff, rank]   dtype   rows as w_gu's: the gate rows' B, then the up rows'
+ *   a_down  [n, rank, d_ff]     dtype
+ *   b_down  [n, d, rank]        dtype
+ *   scale   [n] fp32, may be NULL (ones) */
+typedef struct {
+  int32_t n;
+  int32_t rank;
+  const void* a_gu;
+  const void* b_gu;
+  const void* a_down;
+  const void* b_down;
+  const float* scale;
+} omnimoe_adapters;
+
+/* The shared branch of a batch whose tokens belong to requests with adapters of their own. With e = ids[t]:
+ *   g = W_g x + scale_e B_gate (A_gate x),  u = W_u x + scale_e B_up (A_up x),  a = silu(g) u,
+ *   y = y_in + W_down a + scale_e B_down (A_down a)
+ *   x [T, d], w_gu [2 d_ff, d], w_down [d, d_ff]   dtype, as in omnimoe_shared_mlp
+ *   ids   [T] int32   the token's slot; a value outside [0, n): no adapter
+ *   y_in  [T, d] fp32, may be NULL (zeros): e.g. omnimoe_layer_forward's y
+ *   y     [T, d] dtype out, rounded once (fp32 layers: may be y_in itself)
+ * Tokens of any adapters may come in any order; a token's result does not depend on the others in the batch but for the
+ * rounding of sums, whose order differs between calls of up to 64 and of more tokens, and no value of another slot
+ * enters it. Sums are fp32; bf16 layers round a (as omnimoe_shared_mlp does) and, from 65 tokens on, the rank-wide
+ * values to bf16 for the matrix cores. T = 0 is a no-op. Workspace: omnimoe_shared_mlp_adapters_workspace_size bytes
+ * (the tables' pointers and scale do not count there). */
+omnimoe_status omnimoe_shared_mlp_adapters_workspace_size(const omnimoe_layer_desc* desc, int32_t d_ff,
+                                                          const omnimoe_adapters* adapters, size_t* bytes);
+omnimoe_status omnimoe_shared_mlp_adapters(const omnimoe_layer_desc* desc, int32_t d_ff,
+                                           const omnimoe_adapters* adapters, const void* x, const void* w_gu,
+                                           const void* w_down, const int32_t* ids, const float* y_in, void* y,
+                                           void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -45,6 +45,11 @@ class OmnimoeLayerDesc(ctypes.Structure):
                 ("query_mode", ctypes.c_int32), ("group_size", ctypes.c_int32)]
 
 
+class OmnimoeAdapters(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("rank", ctypes.c_int32), ("a_gu", ctypes.c_void_p), ("b_gu", ctypes.c_void_p),
+                ("a_down", ctypes.c_void_p), ("b_down", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
 class OmnimoeError(RuntimeError):
     def __init__(self, fn: str, status: int, text: str):
         super().__init__(f"{fn} failed: {text} (status {status})")
@@ -91,6 +96,8 @@ def load_library():
         "omnimoe_shared_mlp_backward": [D, I32, P, P, P, P, P, P, P, P, P, P, SZ, P],
         "omnimoe_layer_few_workspace_size": [D, I32, ctypes.POINTER(SZ)],
         "omnimoe_layer_forward_few": [D, I32, P, P, P, P, P, P, P, P, P, P, P, SZ, P],
+        "omnimoe_shared_mlp_adapters_workspace_size": [D, I32, ctypes.POINTER(OmnimoeAdapters), ctypes.POINTER(SZ)],
+        "omnimoe_shared_mlp_adapters": [D, I32, ctypes.POINTER(OmnimoeAdapters), P, P, P, P, P, P, P, SZ, P],
         "omnimoe_timer_create": [I32, ctypes.POINTER(P)],
         "omnimoe_timer_destroy": [P],
         "omnimoe_timer_read": [P, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(I32)],
@@ -340,6 +347,7 @@ class Timer:
 EXPORTED_FFN = (
     "omnimoe_checkpoint_store", "omnimoe_checkpoint_load", "omnimoe_shared_mlp_backward_workspace_size",
     "omnimoe_shared_mlp_backward", "omnimoe_layer_few_workspace_size", "omnimoe_layer_forward_few",
+    "omnimoe_shared_mlp_adapters_workspace_size", "omnimoe_shared_mlp_adapters",
 )
 FEW_TOKENS = 16  # OMNIMOE_FEW_TOKENS
 
@@ -445,3 +453,37 @@ def omnimoe_layer_forward_few(desc, d_ff, x, keys_row, keys_col, u, v, w_gu, w_d
         lambda st: load_library().omnimoe_layer_forward_few(
             ctypes.byref(desc), d_ff, _ptr(x), _ptr(keys_row), _ptr(keys_col), _ptr(u), _ptr(v), _ptr(w_gu),
             _ptr(w_down), _ptr(y), _ptr(idx_out), _ptr(gates_out), _ptr(ws), ws.numel(), st), stream)
+
+
+def make_adapters(a_gu, b_gu, a_down, b_down, scale=None) -> OmnimoeAdapters:
+    """The adapter tables' descriptor, which keeps the tensors: a_gu [n, 2 rank, d], b_gu [n, 2 d_ff, rank],
+    a_down [n, rank, d_ff], b_down [n, d, rank], scale [n] fp32 or None."""
+    n, rank, d_ff = a_down.shape
+    a = OmnimoeAdapters(n=n, rank=rank, a_gu=a_gu.data_ptr(), b_gu=b_gu.data_ptr(), a_down=a_down.data_ptr(),
+                        b_down=b_down.data_ptr(), scale=None if scale is None else scale.data_ptr())
+    a.tensors = (a_gu, b_gu, a_down, b_down, scale)
+    return a
+
+
+def omnimoe_shared_mlp_adapters_workspace_size(desc, d_ff: int, adapters) -> int:
+    n = ctypes.c_size_t(0)
+    _check("omnimoe_shared_mlp_adapters_workspace_size",
+           load_library().omnimoe_shared_mlp_adapters_workspace_size(ctypes.byref(desc), d_ff, ctypes.byref(adapters),
+                                                                     ctypes.byref(n)))
+    return n.value
+
+
+def omnimoe_shared_mlp_adapters(desc, d_ff, adapters, x, w_gu, w_down, ids, y_in, y, ws=None, stream=None):
+    """The shared branch with the tokens' adapters (make_adapters), added to y_in (None: zeros) into y."""
+    import torch
+    ws = _bytes_ws(ws, lambda: omnimoe_shared_mlp_adapters_workspace_size(desc, d_ff, adapters), x.device)
+    T, d, dt, f32, n, r = desc.T, desc.d, _layer_dtype(desc), torch.float32, adapters.n, adapters.rank
+    a_gu, b_gu, a_down, b_down, scale = adapters.tensors
+    _ffn_call("omnimoe_shared_mlp_adapters", desc, (
+        ("x", x, dt, T * d), ("w_gu", w_gu, dt, 2 * d_ff * d), ("w_down", w_down, dt, d * d_ff),
+        ("ids", ids, torch.int32, T), ("y_in", y_in, f32, T * d), ("y", y, dt, T * d),
+        ("a_gu", a_gu, dt, n * 2 * r * d), ("b_gu", b_gu, dt, n * 2 * d_ff * r), ("a_down", a_down, dt, n * r * d_ff),
+        ("b_down", b_down, dt, n * d * r), ("scale", scale, f32, n), ("ws", ws, torch.uint8, ws.numel())),
+        lambda st: load_library().omnimoe_shared_mlp_adapters(
+            ctypes.byref(desc), d_ff, ctypes.byref(adapters), _ptr(x), _ptr(w_gu), _ptr(w_down), _ptr(ids), _ptr(y_in),
+            _ptr(y), _ptr(ws), ws.numel(), st), stream)

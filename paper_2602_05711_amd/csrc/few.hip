@@ -6,25 +6,17 @@
 //                 a v rows; further workgroups form the down projection of all tokens beside it. Whoever finishes a
 //                 token last (a counter) adds the token's partial rows, heads in order, then the shared branch's.
 //
-// Few tokens leave the matrix cores idle, so that a tile of sixteen weight rows x sixteen tokens (v_mfma 16x16) costs
-// nothing beside the loads, whatever T is. A lane reads 32 neighbouring bytes of a row in two loads, so that two
-// instructions cover sixteen whole 128-byte lines; the sum runs over k in that permuted order, the same for both
-// operands. A workgroup's waves split k and their tiles are added in wave order through LDS.
-//
 // The partial rows and the counters cross XCDs inside one kernel, whose L2s are not coherent with each other: partial
 // rows are stored and loaded at agent scope (past L2), every thread waits for its stores (vmcnt) before the barrier
 // behind which one thread counts the workgroup in, and nothing waits for another workgroup.
 #include <type_traits>
 
 #include "cand_table.hpp"
-#include "device_common.hpp"
+#include "few_tile.hpp"
 #include "internal.hpp"
 
 namespace omnimoe {
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTokens = 16;
 constexpr int kSplit = 3;  // bf16 values of a hidden value
@@ -46,80 +38,10 @@ struct FewArgs {
   int down_groups;    // workgroups of sixteen output columns
 };
 
-// 16 rows x 16 tokens: acc of lane l, register q is row 4 (l / 16) + q, token l % 16.
-template <bool BF16>
-struct Chunk;  // 16 bytes of a row
-template <>
-struct Chunk<true> {
-  static constexpr int kElems = 8;
-  static __device__ __forceinline__ void mma(f32x4& acc, const uint4& a, const uint4& b) {
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc,
-                                                  0, 0, 0);
-  }
-};
-template <>
-struct Chunk<false> {
-  static constexpr int kElems = 4;
-  static __device__ __forceinline__ void mma(f32x4& acc, const uint4& a, const uint4& b) {
-    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
-  }
-};
-
-// Steps of four lanes x 32 bytes (128 bytes of every row) of wave w among W: the rows' chunks in units of 16 bytes.
-// row: this lane's weight row; tok: this lane's token row in each of NB token operands (lanes past the last token have
-// that one's: their columns of the tile are not used). The loads are unconditional; chunks past the row's end read its
-// last one, and the weights' are then zeros.
-template <bool BF16, int NB, int W>
-__device__ __forceinline__ f32x4 wave_tile(const uint4* row, const uint4* const (&tok)[NB], int chunks, int w) {
-  const int quad = (threadIdx.x & 63) >> 4;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  constexpr int U = 4;  // steps in flight: 8 + 8 NB loads a lane
-  auto steps = [&](int s0, auto whole) {
-    uint4 a[U][2], b[U][2][NB];
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        int c = (s0 + i) * 8 + quad * 2 + e;
-        if constexpr (!decltype(whole)::value) c = c < chunks ? c : chunks - 1;
-        a[i][e] = row[c];
-#pragma unroll
-        for (int n = 0; n < NB; ++n) b[i][e][n] = tok[n][c];
-      }
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if constexpr (!decltype(whole)::value)
-          if ((s0 + i) * 8 + quad * 2 + e >= chunks) a[i][e] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int n = 0; n < NB; ++n) Chunk<BF16>::mma(acc, a[i][e], b[i][e][n]);
-      }
-  };
-  int s0 = w * U;
-  for (; (s0 + U) * 8 <= chunks; s0 += W * U) steps(s0, std::true_type{});
-  if (s0 * 8 < chunks) steps(s0, std::false_type{});
-  return acc;
-}
-
-// Sum of the W waves' tiles in wave order, on wave 0.
-template <int W>
-__device__ __forceinline__ f32x4 add_tiles(f32x4 acc, f32x4 (&lds)[W][64], int w, int l) {
-  lds[w][l] = acc;
-  __syncthreads();
-  if (w == 0)
-#pragma unroll
-    for (int i = 1; i < W; ++i) acc += lds[i][l];
-  return acc;
-}
-
 template <bool BF16>
 __global__ __launch_bounds__(256) void few_products(FewArgs p) {
   constexpr int W = 4, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
-  __shared__ f32x4 tiles[W][64];
+  __shared__ f32x4 tiles[W][1][64];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, t = l & 15;
   if (blockIdx.x == 0 && threadIdx.x < kTokens) p.count[threadIdx.x] = 0;
   const char* const x = (const char*)p.x + (int64_t)(t < p.T ? t : p.T - 1) * p.d * kSize;
@@ -130,14 +52,16 @@ __global__ __launch_bounds__(256) void few_products(FewArgs p) {
     const int n = half ? p.n[1] : p.n[0], rows = p.H * n, r0 = g * 16, r = r0 + t < rows ? r0 + t : rows - 1;
     const uint4* const tok[1] = {(const uint4*)(x + (half ? p.col0 * kSize : 0))};
     const uint4* const row = (const uint4*)((const char*)(half ? p.keys[1] : p.keys[0]) + (int64_t)r * p.dk * kSize);
-    const f32x4 acc = add_tiles<W>(wave_tile<BF16, 1, W>(row, tok, p.dk / E, w), tiles, w, l);
+    f32x4 acc[1];
+    wave_tile<BF16, 1, 1, W>(row, tok, p.dk / E, w, acc);
+    add_tiles(acc, tiles, w, l);
     if (w == 0 && t < p.T)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int key = r0 + 4 * (l >> 4) + q;
         if (key >= rows) break;
         const int h = key / n, i = key - h * n;
-        p.logits[((int64_t)t * p.H + h) * (p.npad[0] + p.npad[1]) + (half ? p.npad[0] : 0) + i] = acc[q];
+        p.logits[((int64_t)t * p.H + h) * (p.npad[0] + p.npad[1]) + (half ? p.npad[0] : 0) + i] = acc[0][q];
       }
     return;
   }
@@ -146,10 +70,12 @@ __global__ __launch_bounds__(256) void few_products(FewArgs p) {
   const int r = (f < p.F ? f : p.F - 1) + (t & 2 ? p.F : 0);
   const uint4* const tok[1] = {(const uint4*)x};
   const uint4* const row = (const uint4*)((const char*)p.w_gu + (int64_t)r * p.d * kSize);
-  const f32x4 acc = add_tiles<W>(wave_tile<BF16, 1, W>(row, tok, p.d / E, w), tiles, w, l);
+  f32x4 acc[1];
+  wave_tile<BF16, 1, 1, W>(row, tok, p.d / E, w, acc);
+  add_tiles(acc, tiles, w, l);
   if (w == 0) {
     const int fo = f0 + 2 * (l >> 4);
-    const float a0 = activation(1, acc[0]) * acc[2], a1 = activation(1, acc[1]) * acc[3];
+    const float a0 = activation(1, acc[0][0]) * acc[0][2], a1 = activation(1, acc[0][1]) * acc[0][3];
     if constexpr (BF16) {
       // three bf16 values a feature, their sum a itself: the down projection keeps fp32's accuracy
       float r0 = a0, r1 = a1;
@@ -283,7 +209,7 @@ __device__ __forceinline__ void half_best(const float* __restrict__ logits, int 
 
 struct FinishShared {
   union {
-    f32x4 tiles[kWaves][64];
+    f32x4 tiles[kWaves][1][64];
     struct {
       uint64_t cand[2][64], best[2][64];
       uint4 cell[288];  // score (order map of the double), id
@@ -303,22 +229,22 @@ __device__ __forceinline__ void down_group(const FewArgs& p, FinishShared& sh, i
   const uint4* const row = (const uint4*)((const char*)p.w_down + (int64_t)r * p.F * kSize);
   // (the hidden values of lanes past the last token are that token's again)
   auto act = [&](int n) { return (const uint4*)((const char*)p.act + (int64_t)(n * kTokens + t) * p.F * kSize); };
-  f32x4 acc;
+  f32x4 acc[1];
   if constexpr (BF16) {
     const uint4* const tok[NB] = {act(0), act(1), act(2)};
-    acc = wave_tile<BF16, NB, kWaves>(row, tok, p.F / E, w);
+    wave_tile<BF16, NB, 1, kWaves>(row, tok, p.F / E, w, acc);
   } else {
     const uint4* const tok[NB] = {act(0)};
-    acc = wave_tile<BF16, NB, kWaves>(row, tok, p.F / E, w);
+    wave_tile<BF16, NB, 1, kWaves>(row, tok, p.F / E, w, acc);
   }
-  acc = add_tiles<kWaves>(acc, sh.tiles, w, l);
+  add_tiles(acc, sh.tiles, w, l);
   int mine = 0;
   if (w == 0) {
     const int c = g * 16 + 4 * (l >> 4);
     if (t < p.T && c < p.d) {
       float* const o = p.shared + (int64_t)t * p.d + c;
-      store_agent(o, acc[0], acc[1]);
-      store_agent(o + 2, acc[2], acc[3]);
+      store_agent(o, acc[0][0], acc[0][1]);
+      store_agent(o + 2, acc[0][2], acc[0][3]);
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the wave's stores are past L2
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");

@@ -1,0 +1,91 @@
+// Products of weight rows with a few tokens, bound by reading the weights once (few.hip, adapters.hip).
+//
+// Few tokens leave the matrix cores idle, so that a tile of sixteen weight rows x sixteen tokens (v_mfma 16x16) costs
+// nothing beside the loads, however many of the sixteen there are. A lane reads 32 neighbouring bytes of a row in two
+// loads, so that two instructions cover sixteen whole 128-byte lines; the sum runs over k in that permuted order, the
+// same for both operands. A workgroup's waves split k and their tiles are added in wave order through LDS.
+#pragma once
+
+#include <type_traits>
+
+#include "device_common.hpp"
+
+namespace omnimoe {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// 16 rows x 16 tokens: acc of lane l, register q is row 4 (l / 16) + q, token l % 16.
+template <bool BF16>
+struct Chunk;  // 16 bytes of a row
+template <>
+struct Chunk<true> {
+  static constexpr int kElems = 8;
+  static __device__ __forceinline__ void mma(f32x4& acc, const uint4& a, const uint4& b) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc,
+                                                  0, 0, 0);
+  }
+};
+template <>
+struct Chunk<false> {
+  static constexpr int kElems = 4;
+  static __device__ __forceinline__ void mma(f32x4& acc, const uint4& a, const uint4& b) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+  }
+};
+
+// Steps of four lanes x 32 bytes (128 bytes of every row) of wave w among W: the rows' chunks in units of 16 bytes.
+// row: this lane's weight row; tok: this lane's token row in each of NB token operands (lanes past the last token have
+// that one's: their columns of the tile are not used), which have a tile each (NACC = NB) or are summed (NACC = 1). The loads are unconditional; chunks past the row's end read its
+// last one, and the weights' are then zeros.
+template <bool BF16, int NB, int NACC, int W>
+__device__ __forceinline__ void wave_tile(const uint4* row, const uint4* const (&tok)[NB], int chunks, int w,
+                                          f32x4 (&acc)[NACC]) {
+  const int quad = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int n = 0; n < NACC; ++n) acc[n] = {0.f, 0.f, 0.f, 0.f};
+  constexpr int U = NB <= 3 ? 4 : 2;  // steps in flight: 2 U (1 + NB) loads a lane
+  auto steps = [&](int s0, auto whole) {
+    uint4 a[U][2], b[U][2][NB];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        int c = (s0 + i) * 8 + quad * 2 + e;
+        if constexpr (!decltype(whole)::value) c = c < chunks ? c : chunks - 1;
+        a[i][e] = row[c];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) b[i][e][n] = tok[n][c];
+      }
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if constexpr (!decltype(whole)::value)
+          if ((s0 + i) * 8 + quad * 2 + e >= chunks) a[i][e] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) Chunk<BF16>::mma(acc[NACC == NB ? n : 0], a[i][e], b[i][e][n]);
+      }
+  };
+  int s0 = w * U;
+  for (; (s0 + U) * 8 <= chunks; s0 += W * U) steps(s0, std::true_type{});
+  if (s0 * 8 < chunks) steps(s0, std::false_type{});
+}
+
+// Sum of the W waves' tiles in wave order, on wave 0.
+template <int W, int N>
+__device__ __forceinline__ void add_tiles(f32x4 (&acc)[N], f32x4 (&lds)[W][N][64], int w, int l) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) lds[w][n][l] = acc[n];
+  __syncthreads();
+  if (w == 0)
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 1; i < W; ++i) acc[n] += lds[i][n][l];
+}
+
+}  // namespace omnimoe

@@ -6,6 +6,15 @@
 
 using namespace omnimoe;
 
+namespace {
+
+omnimoe_status check_adapters(const omnimoe_adapters* a) {
+  if (!a || a->n < 0 || a->rank < 8 || a->rank > 256 || a->rank % 8) return OMNIMOE_ERR_INVALID_ARG;
+  return a->n > 8192 ? OMNIMOE_ERR_UNSUPPORTED : OMNIMOE_OK;
+}
+
+}  // namespace
+
 extern "C" {
 
 omnimoe_status omnimoe_checkpoint_store(const omnimoe_layer_desc* desc, const void* x, uint8_t* codes,
@@ -81,6 +90,33 @@ omnimoe_status omnimoe_layer_forward_few(const omnimoe_layer_desc* desc, int32_t
   if (ws_bytes < few_ws_bytes(s, d_ff)) return OMNIMOE_ERR_WORKSPACE;
   return hip_status(launch_few(s, d_ff, x, keys_row, keys_col, u, v, w_gu, w_down, y, idx_out, gates_out, ws,
                                (hipStream_t)stream));
+}
+
+omnimoe_status omnimoe_shared_mlp_adapters_workspace_size(const omnimoe_layer_desc* desc, int32_t d_ff,
+                                                          const omnimoe_adapters* adapters, size_t* bytes) {
+  if (!bytes || !valid_d_ff(d_ff)) return OMNIMOE_ERR_INVALID_ARG;
+  Shape s;
+  omnimoe_status st = check_desc(desc, &s);
+  if (st || (st = check_adapters(adapters))) return st;
+  *bytes = adapters_ws_bytes(s, d_ff, adapters->n, adapters->rank);
+  return OMNIMOE_OK;
+}
+
+omnimoe_status omnimoe_shared_mlp_adapters(const omnimoe_layer_desc* desc, int32_t d_ff,
+                                           const omnimoe_adapters* adapters, const void* x, const void* w_gu,
+                                           const void* w_down, const int32_t* ids, const float* y_in, void* y,
+                                           void* ws, size_t ws_bytes, void* stream) {
+  if (!valid_d_ff(d_ff)) return OMNIMOE_ERR_INVALID_ARG;
+  Shape s;
+  omnimoe_status st = check_desc(desc, &s);
+  if (st || (st = check_adapters(adapters))) return st;
+  if (s.T == 0) return OMNIMOE_OK;
+  const omnimoe_adapters& a = *adapters;
+  if ((st = check_ptrs({x, w_gu, w_down, ids, y, ws})) || (st = check_opt(y_in)) || (st = check_opt(a.scale))) return st;
+  if (a.n && (st = check_ptrs({a.a_gu, a.b_gu, a.a_down, a.b_down}))) return st;
+  if (ws_bytes < adapters_ws_bytes(s, d_ff, a.n, a.rank)) return OMNIMOE_ERR_WORKSPACE;
+  const AdapterTables t{a.n, a.rank, a.a_gu, a.b_gu, a.a_down, a.b_down, a.scale};
+  return hip_status(launch_adapters(s, d_ff, t, x, w_gu, w_down, ids, y_in, y, ws, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -260,4 +260,17 @@ hipError_t launch_few(const Shape& s, int d_ff, const void* x, const void* keys_
                       const void* u, const void* v, const void* w_gu, const void* w_down, float* y, int32_t* idx,
                       float* gates, void* ws, hipStream_t st);
 
+// The shared branch with low-rank adapters (adapters.hip): a_gu [n, 2 rank, d], b_gu [n, 2 d_ff, rank],
+// a_down [n, rank, d_ff], b_down [n, d, rank] in the layer's type, scale [n] fp32 or NULL; ids [T], y_in may be NULL.
+// Workspace: adapters_ws_bytes(s, d_ff, n, rank).
+struct AdapterTables {
+  int n, rank;
+  const void *a_gu, *b_gu, *a_down, *b_down;
+  const float* scale;
+};
+size_t adapters_ws_bytes(const Shape& s, int d_ff, int n, int rank);
+hipError_t launch_adapters(const Shape& s, int d_ff, const AdapterTables& t, const void* x, const void* w_gu,
+                           const void* w_down, const int32_t* ids, const float* y_in, void* y, void* ws,
+                           hipStream_t st);
+
 }  // namespace omnimoe
