@@ -27,7 +27,8 @@ extern "C" {
  * store: code = x 2^-s rounded to the nearest e4m3 value, ties to even (so within 2^-4 of the value, relative, where
  * |x| >= 2^(s-6), and within 2^(s-10) below). Values that are not finite are stored as NaN and take no part in the
  * block's maximum.
- * load: x = code 2^s in dtype (exact but where bf16 or fp32 has no such small value). */
+ * load: x = code 2^s in dtype, exact but where the type has no such small value; one past its largest finite value
+ * (the rounding of a neighbour of that) becomes that. */
 omnimoe_status omnimoe_checkpoint_store(const omnimoe_layer_desc* desc, const void* x, uint8_t* codes,
                                         uint8_t* scales, void* stream);
 omnimoe_status omnimoe_checkpoint_load(const omnimoe_layer_desc* desc, const uint8_t* codes, const uint8_t* scales,

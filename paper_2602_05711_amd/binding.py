@@ -352,29 +352,35 @@ EXPORTED_FFN = (
 FEW_TOKENS = 16  # OMNIMOE_FEW_TOKENS
 
 
-def _ffn_call(fn, desc, tensors, call, stream):
-    """Checks `tensors`, a list of (name, tensor or None, dtype, elements), all contiguous and on one GPU, and runs
-    call(stream) with that GPU current; `stream` defaults to its current stream."""
+def _ffn_refuse(fn, dev, name, t, dtype, n):
+    if t.dtype is not dtype:
+        raise ValueError(f"{fn}: {name} is {t.dtype}, not {dtype}")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{fn}: {name} must be contiguous with {n} elements, not {tuple(t.shape)}")
+    raise ValueError(f"{fn}: {name} is on {t.device}, " + ("others on another GPU" if dev >= 0 else "not on a GPU"))
+
+
+def _ffn_call(fn, desc, tensors, args, stream):
+    """Runs fn(desc, *args, stream) on the tensors' GPU; `stream` defaults to its current stream. `tensors`: (name, tensor
+    or None, dtype, elements) of each, which must be contiguous and on one GPU. Tensors in args stand for their address."""
     import torch
-    dev = None
+    dev = -1
     for name, t, dtype, n in tensors:
         if t is None:
             continue
-        if t.dtype is not dtype:
-            raise ValueError(f"{fn}: {name} is {t.dtype}, not {dtype}")
-        if t.numel() != n or not t.is_contiguous():
-            raise ValueError(f"{fn}: {name} must be contiguous with {n} elements, not {tuple(t.shape)}")
-        if dev is None:
-            dev = t.device
-            if dev.type != "cuda":
-                raise ValueError(f"{fn}: {name} is on {dev}, not on a GPU")
-        elif t.device != dev:
-            raise ValueError(f"{fn}: {name} is on {t.device}, others on {dev}")
-    if dev is None or dev.index == torch.cuda.current_device():
-        _check(fn, call(_stream(stream)))
-    else:
+        at = t.get_device()
+        if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or at < 0 or (at != dev and dev >= 0):
+            _ffn_refuse(fn, dev, name, t, dtype, n)
+        dev = at
+    call = getattr(load_library(), fn)
+    args = [a.data_ptr() if isinstance(a, torch.Tensor) else a for a in args]
+    if dev >= 0 and dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
-            _check(fn, call(_stream(stream)))
+            st = stream if stream is not None else torch.cuda.current_stream()
+            _check(fn, call(ctypes.byref(desc), *args, st.cuda_stream))
+    else:
+        st = stream if stream is not None else torch.cuda.current_stream()
+        _check(fn, call(ctypes.byref(desc), *args, st.cuda_stream))
 
 
 def _layer_dtype(desc):
@@ -382,83 +388,73 @@ def _layer_dtype(desc):
     return torch.bfloat16 if desc.dtype == OMNIMOE_BF16 else torch.float32
 
 
-def _bytes_ws(ws, size, device):
-    """`ws` (a uint8 tensor of any size: the call checks it), or a new one of size() bytes."""
+def _ffn_size(fn, *args) -> int:
+    n = ctypes.c_size_t(0)
+    _check(fn, getattr(load_library(), fn)(*args, ctypes.byref(n)))
+    return n.value
+
+
+def _ffn_workspace(ws, size, device):
+    """`ws` (a uint8 tensor: the call checks its size), or a new one of size() bytes."""
     import torch
     return torch.empty(max(256, size()), dtype=torch.uint8, device=device) if ws is None else ws
 
 
-def omnimoe_checkpoint_store(desc, x, codes, scales, stream=None):
+def _checkpoint_tensors(desc, x, codes, scales):
     import torch
-    n, u8 = desc.T * desc.d, torch.uint8
-    _ffn_call("omnimoe_checkpoint_store", desc, (
-        ("x", x, _layer_dtype(desc), n), ("codes", codes, u8, n),
-        ("scales", scales, u8, desc.T * ((desc.d + 31) // 32))),
-        lambda st: load_library().omnimoe_checkpoint_store(ctypes.byref(desc), _ptr(x), _ptr(codes), _ptr(scales), st),
-        stream)
+    T, d, u8 = desc.T, desc.d, torch.uint8
+    return (("x", x, _layer_dtype(desc), T * d), ("codes", codes, u8, T * d), ("scales", scales, u8, T * ((d + 31) // 32)))
+
+
+def omnimoe_checkpoint_store(desc, x, codes, scales, stream=None):
+    _ffn_call("omnimoe_checkpoint_store", desc, _checkpoint_tensors(desc, x, codes, scales), (x, codes, scales), stream)
 
 
 def omnimoe_checkpoint_load(desc, codes, scales, x, stream=None):
-    import torch
-    n, u8 = desc.T * desc.d, torch.uint8
-    _ffn_call("omnimoe_checkpoint_load", desc, (
-        ("x", x, _layer_dtype(desc), n), ("codes", codes, u8, n),
-        ("scales", scales, u8, desc.T * ((desc.d + 31) // 32))),
-        lambda st: load_library().omnimoe_checkpoint_load(ctypes.byref(desc), _ptr(codes), _ptr(scales), _ptr(x), st),
-        stream)
+    _ffn_call("omnimoe_checkpoint_load", desc, _checkpoint_tensors(desc, x, codes, scales), (codes, scales, x), stream)
 
 
 def omnimoe_shared_mlp_backward_workspace_size(desc, d_ff: int) -> int:
-    n = ctypes.c_size_t(0)
-    _check("omnimoe_shared_mlp_backward_workspace_size",
-           load_library().omnimoe_shared_mlp_backward_workspace_size(ctypes.byref(desc), d_ff, ctypes.byref(n)))
-    return n.value
+    return _ffn_size("omnimoe_shared_mlp_backward_workspace_size", ctypes.byref(desc), d_ff)
 
 
 def omnimoe_shared_mlp_backward(desc, d_ff, codes, scales, w_gu, w_down, dy, dx_in, dx, dw_gu, dw_down, ws=None,
                                 stream=None):
     """Gradients of the shared branch from the 8-bit checkpoint of its input; dx_in may be None."""
     import torch
-    ws = _bytes_ws(ws, lambda: omnimoe_shared_mlp_backward_workspace_size(desc, d_ff), w_gu.device)
+    ws = _ffn_workspace(ws, lambda: omnimoe_shared_mlp_backward_workspace_size(desc, d_ff), w_gu.device)
     T, d, dt, f32, u8 = desc.T, desc.d, _layer_dtype(desc), torch.float32, torch.uint8
     _ffn_call("omnimoe_shared_mlp_backward", desc, (
         ("codes", codes, u8, T * d), ("scales", scales, u8, T * ((d + 31) // 32)), ("w_gu", w_gu, dt, 2 * d_ff * d),
         ("w_down", w_down, dt, d * d_ff), ("dy", dy, f32, T * d), ("dx_in", dx_in, f32, T * d), ("dx", dx, dt, T * d),
         ("dw_gu", dw_gu, dt, 2 * d_ff * d), ("dw_down", dw_down, dt, d * d_ff), ("ws", ws, u8, ws.numel())),
-        lambda st: load_library().omnimoe_shared_mlp_backward(
-            ctypes.byref(desc), d_ff, _ptr(codes), _ptr(scales), _ptr(w_gu), _ptr(w_down), _ptr(dy), _ptr(dx_in),
-            _ptr(dx), _ptr(dw_gu), _ptr(dw_down), _ptr(ws), ws.numel(), st), stream)
+        (d_ff, codes, scales, w_gu, w_down, dy, dx_in, dx, dw_gu, dw_down, ws, ws.numel()), stream)
 
 
 def omnimoe_layer_few_workspace_size(desc, d_ff: int) -> int:
-    n = ctypes.c_size_t(0)
-    _check("omnimoe_layer_few_workspace_size",
-           load_library().omnimoe_layer_few_workspace_size(ctypes.byref(desc), d_ff, ctypes.byref(n)))
-    return n.value
+    return _ffn_size("omnimoe_layer_few_workspace_size", ctypes.byref(desc), d_ff)
 
 
 def omnimoe_layer_forward_few(desc, d_ff, x, keys_row, keys_col, u, v, w_gu, w_down, y, idx_out=None, gates_out=None,
                               ws=None, stream=None):
     """The whole feed-forward layer for up to FEW_TOKENS tokens; without a shared branch d_ff is 0 and its weights None."""
     import torch
-    ws = _bytes_ws(ws, lambda: omnimoe_layer_few_workspace_size(desc, d_ff), x.device)
-    T, d, H, K, dt = desc.T, desc.d, desc.H, desc.K, _layer_dtype(desc)
+    ws = _ffn_workspace(ws, lambda: omnimoe_layer_few_workspace_size(desc, d_ff), x.device)
+    T, d, H, K, dt, f32 = desc.T, desc.d, desc.H, desc.K, _layer_dtype(desc), torch.float32
     N = desc.n_rows * desc.n_cols
     _ffn_call("omnimoe_layer_forward_few", desc, (
         ("x", x, dt, T * d), ("keys_row", keys_row, dt, H * desc.n_rows * desc.d_key),
         ("keys_col", keys_col, dt, H * desc.n_cols * desc.d_key), ("u", u, dt, N * d), ("v", v, dt, N * d),
-        ("w_gu", w_gu, dt, 2 * d_ff * d), ("w_down", w_down, dt, d * d_ff), ("y", y, torch.float32, T * d),
-        ("idx_out", idx_out, torch.int32, T * H * K), ("gates_out", gates_out, torch.float32, T * H * K),
+        ("w_gu", w_gu, dt, 2 * d_ff * d), ("w_down", w_down, dt, d * d_ff), ("y", y, f32, T * d),
+        ("idx_out", idx_out, torch.int32, T * H * K), ("gates_out", gates_out, f32, T * H * K),
         ("ws", ws, torch.uint8, ws.numel())),
-        lambda st: load_library().omnimoe_layer_forward_few(
-            ctypes.byref(desc), d_ff, _ptr(x), _ptr(keys_row), _ptr(keys_col), _ptr(u), _ptr(v), _ptr(w_gu),
-            _ptr(w_down), _ptr(y), _ptr(idx_out), _ptr(gates_out), _ptr(ws), ws.numel(), st), stream)
+        (d_ff, x, keys_row, keys_col, u, v, w_gu, w_down, y, idx_out, gates_out, ws, ws.numel()), stream)
 
 
 def make_adapters(a_gu, b_gu, a_down, b_down, scale=None) -> OmnimoeAdapters:
     """The adapter tables' descriptor, which keeps the tensors: a_gu [n, 2 rank, d], b_gu [n, 2 d_ff, rank],
     a_down [n, rank, d_ff], b_down [n, d, rank], scale [n] fp32 or None."""
-    n, rank, d_ff = a_down.shape
+    n, rank, _ = a_down.shape
     a = OmnimoeAdapters(n=n, rank=rank, a_gu=a_gu.data_ptr(), b_gu=b_gu.data_ptr(), a_down=a_down.data_ptr(),
                         b_down=b_down.data_ptr(), scale=None if scale is None else scale.data_ptr())
     a.tensors = (a_gu, b_gu, a_down, b_down, scale)
@@ -466,17 +462,13 @@ def make_adapters(a_gu, b_gu, a_down, b_down, scale=None) -> OmnimoeAdapters:
 
 
 def omnimoe_shared_mlp_adapters_workspace_size(desc, d_ff: int, adapters) -> int:
-    n = ctypes.c_size_t(0)
-    _check("omnimoe_shared_mlp_adapters_workspace_size",
-           load_library().omnimoe_shared_mlp_adapters_workspace_size(ctypes.byref(desc), d_ff, ctypes.byref(adapters),
-                                                                     ctypes.byref(n)))
-    return n.value
+    return _ffn_size("omnimoe_shared_mlp_adapters_workspace_size", ctypes.byref(desc), d_ff, ctypes.byref(adapters))
 
 
 def omnimoe_shared_mlp_adapters(desc, d_ff, adapters, x, w_gu, w_down, ids, y_in, y, ws=None, stream=None):
     """The shared branch with the tokens' adapters (make_adapters), added to y_in (None: zeros) into y."""
     import torch
-    ws = _bytes_ws(ws, lambda: omnimoe_shared_mlp_adapters_workspace_size(desc, d_ff, adapters), x.device)
+    ws = _ffn_workspace(ws, lambda: omnimoe_shared_mlp_adapters_workspace_size(desc, d_ff, adapters), x.device)
     T, d, dt, f32, n, r = desc.T, desc.d, _layer_dtype(desc), torch.float32, adapters.n, adapters.rank
     a_gu, b_gu, a_down, b_down, scale = adapters.tensors
     _ffn_call("omnimoe_shared_mlp_adapters", desc, (
@@ -484,6 +476,4 @@ def omnimoe_shared_mlp_adapters(desc, d_ff, adapters, x, w_gu, w_down, ids, y_in
         ("ids", ids, torch.int32, T), ("y_in", y_in, f32, T * d), ("y", y, dt, T * d),
         ("a_gu", a_gu, dt, n * 2 * r * d), ("b_gu", b_gu, dt, n * 2 * d_ff * r), ("a_down", a_down, dt, n * r * d_ff),
         ("b_down", b_down, dt, n * d * r), ("scale", scale, f32, n), ("ws", ws, torch.uint8, ws.numel())),
-        lambda st: load_library().omnimoe_shared_mlp_adapters(
-            ctypes.byref(desc), d_ff, ctypes.byref(adapters), _ptr(x), _ptr(w_gu), _ptr(w_down), _ptr(ids), _ptr(y_in),
-            _ptr(y), _ptr(ws), ws.numel(), st), stream)
+        (d_ff, ctypes.byref(adapters), x, w_gu, w_down, ids, y_in, y, ws, ws.numel()), stream)

@@ -79,6 +79,7 @@ template <bool BF16>
 __global__ __launch_bounds__(256) void load_kernel(const uint8_t* __restrict__ codes,
                                                    const uint8_t* __restrict__ scales, void* __restrict__ x,
                                                    int64_t T, int d, int nblk) {
+  const float kLargest = __uint_as_float(BF16 ? 0x7F7F0000u : 0x7F7FFFFFu);
   const int q8 = d / 8;
   const int64_t n = T * q8;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
@@ -91,10 +92,13 @@ __global__ __launch_bounds__(256) void load_kernel(const uint8_t* __restrict__ c
     for (int h = 0; h < 2; ++h) {
       const int p = (int)(h ? w.y : w.x);
       const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(p, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(p, true);
-      v[4 * h] = ldexpf(lo[0], s);
-      v[4 * h + 1] = ldexpf(lo[1], s);
-      v[4 * h + 2] = ldexpf(hi[0], s);
-      v[4 * h + 3] = ldexpf(hi[1], s);
+      const float q[4] = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float y = ldexpf(q[e], s);
+        // a value next to the type's largest may have been rounded up past it
+        v[4 * h + e] = fabsf(y) > kLargest ? copysignf(kLargest, y) : y;
+      }
     }
     if constexpr (BF16) {
       uint32_t o[4];
