@@ -398,18 +398,25 @@ void launch_rows(const AdapterArgs& p, hipStream_t st) {
 #undef OMNIMOE_ROWS
 }
 
+// The largest tile that leaves few compute units without one: a 4096-token batch, d = d_ff = 2048, down projection (128
+// tiles of 256 x 256) 68 us on 64 x 128, 65 on 128 x 256; fp32, 333 tokens, 520 wide: 29 and 31 us on 64 x 128 (54 and 30
+// tiles), 15 and 20 on 32 x 128.
+template <class T, int TM, int TN, int WR, int WC, bool DOWN>
+bool try_tile(const AdapterArgs& p, int64_t least, hipStream_t st) {
+  const int64_t width = DOWN ? p.d : p.F, step = DOWN ? TN : TN / 2;
+  const int64_t tiles = ((int64_t)p.T + TM - 1) / TM * ((width + step - 1) / step);
+  if (tiles < least) return false;
+  hipLaunchKernelGGL((adapter_tile_kernel<T, TM, TN, WR, WC, DOWN>), dim3((unsigned)tiles), dim3(64 * WR * WC), 0, st, p);
+  return true;
+}
 template <class T, bool DOWN>
 void launch_tiles(const AdapterArgs& p, hipStream_t st) {
-  const int64_t width = DOWN ? p.d : p.F;
-  auto tiles = [&](int tm, int tn) { return ((int64_t)p.T + tm - 1) / tm * ((width + tn - 1) / tn); };
-  if constexpr (T::kSize == 2)
-    if (tiles(256, DOWN ? 256 : 128) >= 192) {
-      hipLaunchKernelGGL((adapter_tile_kernel<T, 256, 256, 2, 4, DOWN>), dim3((unsigned)tiles(256, DOWN ? 256 : 128)),
-                         dim3(512), 0, st, p);
-      return;
-    }
-  hipLaunchKernelGGL((adapter_tile_kernel<T, 64, 128, 2, 2, DOWN>), dim3((unsigned)tiles(64, DOWN ? 128 : 64)),
-                     dim3(256), 0, st, p);
+  if constexpr (T::kSize == 2) {
+    if (try_tile<T, 256, 256, 2, 4, DOWN>(p, 192, st)) return;
+    if (try_tile<T, 128, 256, 2, 4, DOWN>(p, 192, st)) return;
+  }
+  if (try_tile<T, 64, 128, 2, 2, DOWN>(p, 192, st)) return;
+  try_tile<T, 32, 128, 1, 4, DOWN>(p, 0, st);
 }
 
 template <class T>
