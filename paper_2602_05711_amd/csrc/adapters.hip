@@ -51,9 +51,12 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& p, int t) {
 // Workgroups of the weights' rows (sixteen a workgroup, all tokens), then of the A rows: sixteen rows for up to sixteen
 // tokens of one adapter, the workgroup of a token that is the first of such a group (others leave). TB: blocks of
 // sixteen tokens. DOWN: the second projection.
+#ifndef PW
+#define PW 4
+#endif
 template <bool BF16, int TB, bool DOWN>
-__global__ __launch_bounds__(256) void few_rows_kernel(AdapterArgs p, int weight_groups, int a_groups) {
-  constexpr int W = 4, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
+__global__ __launch_bounds__(64 * PW) void few_rows_kernel(AdapterArgs p, int weight_groups, int a_groups) {
+  constexpr int W = PW, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
   __shared__ f32x4 tiles[W][TB][64];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int K = DOWN ? p.F : p.d, chunks = K / E;
@@ -390,7 +393,7 @@ void launch_rows(const AdapterArgs& p, hipStream_t st) {
   const dim3 grid((unsigned)(weights + p.T * a_groups));
   const int tb = (p.T + 15) / 16;
 #define OMNIMOE_ROWS(TB_) \
-  hipLaunchKernelGGL((few_rows_kernel<BF16, TB_, DOWN>), grid, dim3(256), 0, st, p, weights, a_groups)
+  hipLaunchKernelGGL((few_rows_kernel<BF16, TB_, DOWN>), grid, dim3(64 * PW), 0, st, p, weights, a_groups)
   if (tb == 1) OMNIMOE_ROWS(1);
   else if (tb == 2) OMNIMOE_ROWS(2);
   else if (tb == 3) OMNIMOE_ROWS(3);

@@ -38,9 +38,12 @@ struct FewArgs {
   int down_groups;    // workgroups of sixteen output columns
 };
 
+#ifndef PW
+#define PW 4
+#endif
 template <bool BF16>
-__global__ __launch_bounds__(256) void few_products(FewArgs p) {
-  constexpr int W = 4, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
+__global__ __launch_bounds__(64 * PW) void few_products(FewArgs p) {
+  constexpr int W = PW, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
   __shared__ f32x4 tiles[W][1][64];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, t = l & 15;
   if (blockIdx.x == 0 && threadIdx.x < kTokens) p.count[threadIdx.x] = 0;
@@ -207,12 +210,14 @@ __device__ __forceinline__ void half_best(const float* __restrict__ logits, int 
   }
 }
 
+constexpr int kCells = 288;  // at least the 280 cells of K = 64, and what the last wave's share runs past them
 struct FinishShared {
   union {
     f32x4 tiles[kWaves][1][64];
     struct {
       uint64_t cand[2][64], best[2][64];
-      uint4 cell[288];  // score (order map of the double), id
+      uint4 cell[kCells];  // score (order map of the double), id
+      int rank[kCells];
       uint64_t pick_score[64];
       uint32_t pick_id[64];
       float a[64];
@@ -269,54 +274,57 @@ __global__ __launch_bounds__(kThreads) void few_finish(FewArgs p) {
   const int row = blockIdx.x, t = row / p.H, K = p.K;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kr = K < p.n[0] ? K : p.n[0], kc = K < p.n[1] ? K : p.n[1];
+  // The candidate cells (a, b), (a + 1)(b + 1) <= K: at most 280, one a thread.
+  const int first = kCand.first[K], cells = kCand.first[K + 1] - first;
+  const int ab = kCand.cell[first + ((int)threadIdx.x < cells ? threadIdx.x : 0)];
   if (w < 2)
     half_best<R>(p.logits + (int64_t)row * (p.npad[0] + p.npad[1]) + (w ? p.npad[0] : 0), w ? p.n[1] : p.n[0],
                  w ? kc : kr, sh.cand[w], sh.best[w]);
   __syncthreads();
-  // The candidate cells, ranked by counting (score descending, id ascending).
-  const int first = kCand.first[K], cells = kCand.first[K + 1] - first;
-  uint64_t score = 0ull;
-  uint32_t id = 0u;
-  bool cell = false;
-  if ((int)threadIdx.x < cells) {
-    const int ab = kCand.cell[first + threadIdx.x], a = ab >> 8, b = ab & 0xFF;
-    cell = a < kr && b < kc;
-    if (cell) {
+  if (threadIdx.x < kCells) {
+    const int a = ab >> 8, b = ab & 0xFF;
+    uint64_t score = 0ull;  // (no cell: below every score)
+    uint32_t id = 0xFFFFFFFFu;
+    if ((int)threadIdx.x < cells && a < kr && b < kc) {
       const uint64_t ka = sh.best[0][a], kb = sh.best[1][b];
       score = ord_f64((double)f32_from_ord((uint32_t)(ka >> 32)) + (double)f32_from_ord((uint32_t)(kb >> 32)));
       id = (0xFFFFFFFFu - (uint32_t)ka) * (uint32_t)p.n[1] + (0xFFFFFFFFu - (uint32_t)kb);
     }
+    sh.cell[threadIdx.x] = make_uint4((uint32_t)score, (uint32_t)(score >> 32), id, 0u);
+    sh.rank[threadIdx.x] = 0;
   }
-  if (threadIdx.x < 288)  // (no cell: below every score)
-    sh.cell[threadIdx.x] = make_uint4((uint32_t)score, (uint32_t)(score >> 32), cell ? id : 0xFFFFFFFFu, 0u);
   __syncthreads();
-  if (cell) {
+  // Their ranks by counting (score descending, id ascending): a lane has a cell, a wave an eighth of those that it is
+  // compared with. (On one wave the 50 cells of K = 16 took 6600 of the kernel's 27000 cycles.)
+  const int share = (cells + kWaves - 1) / kWaves;
+  for (int c = l; c < cells; c += 64) {
+    const uint4 m = sh.cell[c];
+    const uint64_t mine = ((uint64_t)m.y << 32) | m.x;
     int rank = 0;
-    for (int j = 0; j < cells; j += 8) {  // at most 280 of them
-      uint4 v[8];
+    for (int j0 = w * share; j0 < (w + 1) * share; j0 += 4) {
+      uint4 v[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = sh.cell[j + i];
+      for (int i = 0; i < 4; ++i) v[i] = sh.cell[j0 + i];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 4; ++i) {
         const uint64_t s = ((uint64_t)v[i].y << 32) | v[i].x;
-        rank += s > score || (s == score && v[i].z < id) ? 1 : 0;
+        const bool above = (s > mine) | ((s == mine) & (v[i].z < m.z));
+        rank += above & (j0 + i < (w + 1) * share) ? 1 : 0;
       }
     }
-    if (rank < K) {
-      sh.pick_score[rank] = score;
-      sh.pick_id[rank] = id;
+    atomicAdd(&sh.rank[c], rank);
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < cells) {
+    const uint4 m = sh.cell[threadIdx.x];
+    const int rank = sh.rank[threadIdx.x];
+    if (m.z != 0xFFFFFFFFu && rank < K) {
+      sh.pick_score[rank] = ((uint64_t)m.y << 32) | m.x;
+      sh.pick_id[rank] = m.z;
     }
   }
   __syncthreads();
-  // Gates, on every wave: lane k has pick k's.
-  const uint32_t eid = sh.pick_id[l < K ? l : 0];
-  const double s0 = f64_from_ord(sh.pick_score[0]);
-  const float e = l < K ? expf((float)(f64_from_ord(sh.pick_score[l < K ? l : 0]) - s0)) : 0.0f;
-  const float gate = e / wave_sum_f32(e);
-  if (w == 0 && l < K) {
-    if (p.idx) p.idx[(int64_t)row * K + l] = (int32_t)eid;
-    if (p.gates) p.gates[(int64_t)row * K + l] = gate;
-  }
+  const uint32_t eid = sh.pick_id[l < K ? l : 0];  // lane k: pick k's expert
   // x . u of picks w, w + 8, ..., two at a time; the first v rows are requested right after the first u rows.
   // (Loads are unconditional: a chunk past the row's end reads its last one and counts as zeros.)
   constexpr int kAhead = 16;
@@ -347,6 +355,14 @@ __global__ __launch_bounds__(kThreads) void few_finish(FewArgs p) {
     };
     if (w < K) load_u(w, l);
     load_v(0, c0);
+    // Gates, on every wave, while the rows are under way: lane k has pick k's.
+    const double s0 = f64_from_ord(sh.pick_score[0]);
+    const float e = l < K ? expf((float)(f64_from_ord(sh.pick_score[l < K ? l : 0]) - s0)) : 0.0f;
+    const float gate = e / wave_sum_uniform(e);
+    if (w == 0 && l < K) {
+      if (p.idx) p.idx[(int64_t)row * K + l] = (int32_t)eid;
+      if (p.gates) p.gates[(int64_t)row * K + l] = gate;
+    }
     for (int k = w; k < K; k += 2 * kWaves) {
       float acc[2] = {0.0f, 0.0f};
       for (int q = 0; q < chunks; q += 256) {
@@ -449,8 +465,8 @@ hipError_t launch_few(const Shape& s, int F, const void* x, const void* keys_row
   w += up((size_t)s.rows * s.d * 4);
   p.shared = (float*)w;
   const dim3 products((unsigned)(p.key_groups[0] + p.key_groups[1] + F / 8));
-  if (s.bf16) hipLaunchKernelGGL(few_products<true>, products, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL(few_products<false>, products, dim3(256), 0, st, p);
+  if (s.bf16) hipLaunchKernelGGL(few_products<true>, products, dim3(64 * PW), 0, st, p);
+  else hipLaunchKernelGGL(few_products<false>, products, dim3(64 * PW), 0, st, p);
   const dim3 finish((unsigned)(s.rows + p.down_groups));
   const int n = s.nr > s.nc ? s.nr : s.nc;
 #define OMNIMOE_FEW(R_)                                                                         \

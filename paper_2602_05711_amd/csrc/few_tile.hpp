@@ -37,42 +37,55 @@ struct Chunk<false> {
   }
 };
 
-// Steps of four lanes x 32 bytes (128 bytes of every row) of wave w among W: the rows' chunks in units of 16 bytes.
-// row: this lane's weight row; tok: this lane's token row in each of NB token operands (lanes past the last token have
-// that one's: their columns of the tile are not used), which have a tile each (NACC = NB) or are summed (NACC = 1). The loads are unconditional; chunks past the row's end read its
-// last one, and the weights' are then zeros.
-template <bool BF16, int NB, int NACC, int W>
-__device__ __forceinline__ void wave_tile(const uint4* row, const uint4* const (&tok)[NB], int chunks, int w,
-                                          f32x4 (&acc)[NACC]) {
+// The weights' rows against NB token operands, summed over this wave's steps (w of W): a step is four lanes x 32 bytes
+// (128 bytes of every row), a wave takes U neighbouring ones at a time and has their weights in flight together, U as
+// large as leaves every wave some.
+// row: this lane's weight row, of `chunks` times 16 bytes; tok: this lane's token row in each of the operands (lanes past
+// the last token have that one's: their columns of the tile are not used), which have a tile each (NACC = NB) or are
+// summed (NACC = 1). The loads are unconditional; chunks past the row's end read its last one, and the weights' are then
+// zeros.
+template <bool BF16, int NB, int NACC, int W, int U>
+__device__ __forceinline__ void wave_steps(const uint4* row, const uint4* const (&tok)[NB], int chunks, int w,
+                                           f32x4 (&acc)[NACC]) {
   const int quad = (threadIdx.x & 63) >> 4;
-#pragma unroll
-  for (int n = 0; n < NACC; ++n) acc[n] = {0.f, 0.f, 0.f, 0.f};
-  constexpr int U = NB <= 3 ? 4 : 2;  // steps in flight: 2 U (1 + NB) loads a lane
   auto steps = [&](int s0, auto whole) {
-    uint4 a[U][2], b[U][2][NB];
+    constexpr bool kWhole = decltype(whole)::value;
+    auto chunk = [&](int i, int e) {
+      const int c = (s0 + i) * 8 + quad * 2 + e;
+      return kWhole || c < chunks ? c : chunks - 1;
+    };
+    uint4 a[U][2];
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
+      for (int e = 0; e < 2; ++e) a[i][e] = row[chunk(i, e)];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      uint4 b[2][NB];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) b[e][n] = tok[n][chunk(i, e)];
+#pragma unroll
       for (int e = 0; e < 2; ++e) {
-        int c = (s0 + i) * 8 + quad * 2 + e;
-        if constexpr (!decltype(whole)::value) c = c < chunks ? c : chunks - 1;
-        a[i][e] = row[c];
+        if (!kWhole && (s0 + i) * 8 + quad * 2 + e >= chunks) a[i][e] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int n = 0; n < NB; ++n) b[i][e][n] = tok[n][c];
+        for (int n = 0; n < NB; ++n) Chunk<BF16>::mma(acc[NACC == NB ? n : 0], a[i][e], b[e][n]);
       }
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if constexpr (!decltype(whole)::value)
-          if ((s0 + i) * 8 + quad * 2 + e >= chunks) a[i][e] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int n = 0; n < NB; ++n) Chunk<BF16>::mma(acc[NACC == NB ? n : 0], a[i][e], b[i][e][n]);
-      }
+    }
   };
   int s0 = w * U;
   for (; (s0 + U) * 8 <= chunks; s0 += W * U) steps(s0, std::true_type{});
   if (s0 * 8 < chunks) steps(s0, std::false_type{});
+}
+template <bool BF16, int NB, int NACC, int W>
+__device__ __forceinline__ void wave_tile(const uint4* row, const uint4* const (&tok)[NB], int chunks, int w,
+                                          f32x4 (&acc)[NACC]) {
+#pragma unroll
+  for (int n = 0; n < NACC; ++n) acc[n] = {0.f, 0.f, 0.f, 0.f};
+  if (chunks >= 32 * W) wave_steps<BF16, NB, NACC, W, 4>(row, tok, chunks, w, acc);
+  else if (chunks >= 16 * W) wave_steps<BF16, NB, NACC, W, 2>(row, tok, chunks, w, acc);
+  else wave_steps<BF16, NB, NACC, W, 1>(row, tok, chunks, w, acc);
 }
 
 // Sum of the W waves' tiles in wave order, on wave 0.
