@@ -22,6 +22,7 @@ namespace omnimoe {
 namespace {
 
 constexpr int kFewTokens = 64;
+constexpr int kMaxParts = 4;  // of a few-token projection's summed index
 
 struct AdapterArgs {
   const void *x, *w_gu, *w_down;  // [T, d], [2 F, d], [d, F]
@@ -31,7 +32,7 @@ struct AdapterArgs {
   const float* y_in;   // [T, d], or NULL
   void* y;
   int T, d, F, n, r;
-  float* raw;      // few tokens: [T, 2 F] W_gu x, later [T, d] W_down a
+  float* raw;      // few tokens: [parts, T, 2 F] W_gu x, later [parts, T, d] W_down a
   float* low;      // few tokens: [T, 2 r], later [T, r]
   void* lowt;      // in the layer's type and in sorted order: [T, 2 r], later [T, r]
   void* act;       // [T, F], in sorted order
@@ -48,42 +49,55 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& p, int t) {
 
 // ---------------------------------------------------------------- up to 64 tokens
 
-// Workgroups of the weights' rows (sixteen a workgroup, all tokens), then of the A rows: sixteen rows for up to sixteen
-// tokens of one adapter, the workgroup of a token that is the first of such a group (others leave). TB: blocks of
-// sixteen tokens. DOWN: the second projection.
-#ifndef PW
-#define PW 4
-#endif
-template <bool BF16, int TB, bool DOWN>
-__global__ __launch_bounds__(64 * PW) void few_rows_kernel(AdapterArgs p, int weight_groups, int a_groups) {
-  constexpr int W = PW, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
-  __shared__ f32x4 tiles[W][TB][64];
+// Workgroups of the weights' rows (16 RB rows a workgroup and one of `splits` parts of the summed index, all tokens),
+// then of the A rows: sixteen rows for up to sixteen tokens of one adapter, the workgroup of a token that is the first of
+// such a group (others leave). TB: blocks of sixteen tokens. DOWN: the second projection.
+// With many tokens it is their rows that a workgroup reads most of (64 tokens: 128 KiB for 64 KiB of weights even so);
+// hence two row blocks and a part of the index instead of one block and the whole: 64 tokens, d = 2048, F = 2048: 12.0
+// and 9.0 us instead of 14.6 and 12.5. With sixteen or fewer the parts cost more than they give (5.9 us instead of 5.2).
+struct RowSplit {
+  int weight_groups, splits, chunks, a_groups;  // chunks: 16-byte chunks of a row in a part
+};
+template <bool BF16, int RB, int TB, bool DOWN>
+__global__ __launch_bounds__(256) void few_rows_kernel(AdapterArgs p, RowSplit split) {
+  constexpr int W = 4, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
+  __shared__ f32x4 tiles[W][RB * TB][64];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int K = DOWN ? p.F : p.d, chunks = K / E;
   const char* const in = (const char*)(DOWN ? p.act : p.x);
-  if ((int)blockIdx.x < weight_groups) {
-    const int rows = DOWN ? p.d : 2 * p.F, r0 = blockIdx.x * 16, r = r0 + (l & 15) < rows ? r0 + (l & 15) : rows - 1;
+  if ((int)blockIdx.x < split.weight_groups) {
+    const int group = blockIdx.x / split.splits, part = blockIdx.x - group * split.splits;
+    const int rows = DOWN ? p.d : 2 * p.F, r0 = group * 16 * RB, c0 = part * split.chunks;
+    const uint4* row[RB];
     const uint4* tok[TB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      const int r = r0 + 16 * b + (l & 15) < rows ? r0 + 16 * b + (l & 15) : rows - 1;
+      row[b] = (const uint4*)((const char*)(DOWN ? p.w_down : p.w_gu) + (int64_t)r * K * kSize) + c0;
+    }
 #pragma unroll
     for (int b = 0; b < TB; ++b) {
       const int t = 16 * b + (l & 15) < p.T ? 16 * b + (l & 15) : p.T - 1;
-      tok[b] = (const uint4*)(in + (int64_t)t * K * kSize);
+      tok[b] = (const uint4*)(in + (int64_t)t * K * kSize) + c0;
     }
-    f32x4 acc[TB];
-    wave_tile<BF16, TB, TB, W>((const uint4*)((const char*)(DOWN ? p.w_down : p.w_gu) + (int64_t)r * K * kSize), tok,
-                               chunks, w, acc);
+    f32x4 acc[RB * TB];
+    wave_tile<BF16, RB, TB, TB, W>(row, tok, chunks - c0 < split.chunks ? chunks - c0 : split.chunks, w, acc);
     add_tiles(acc, tiles, w, l);
-    const int o = r0 + 4 * (l >> 4);
-    if (w == 0 && o < rows)
+    if (w == 0)
 #pragma unroll
-      for (int b = 0; b < TB; ++b) {
-        const int t = 16 * b + (l & 15);
-        if (t < p.T) *(f32x4*)(p.raw + (int64_t)t * rows + o) = acc[b];
+      for (int b = 0; b < RB; ++b) {
+        const int o = r0 + 16 * b + 4 * (l >> 4);
+        if (o >= rows) break;
+#pragma unroll
+        for (int n = 0; n < TB; ++n) {
+          const int t = 16 * n + (l & 15);
+          if (t < p.T) *(f32x4*)(p.raw + ((int64_t)part * p.T + t) * rows + o) = acc[b * TB + n];
+        }
       }
     return;
   }
-  const int g = (int)blockIdx.x - weight_groups, t = g / a_groups, rows = DOWN ? p.r : 2 * p.r;
-  const int r0 = (g - t * a_groups) * 16;
+  const int g = (int)blockIdx.x - split.weight_groups, t = g / split.a_groups, rows = DOWN ? p.r : 2 * p.r;
+  const int r0 = (g - t * split.a_groups) * 16;
   const int mine = l < p.T ? adapter_of(p, l) : -1;
   const int e = readlane_i32(mine, t);
   uint64_t same = __ballot(mine == e);
@@ -101,9 +115,10 @@ __global__ __launch_bounds__(64 * PW) void few_rows_kernel(AdapterArgs p, int we
   }
   const int r = r0 + (l & 15) < rows ? r0 + (l & 15) : rows - 1;
   const uint4* const tok[1] = {(const uint4*)(in + (int64_t)token * K * kSize)};
+  const uint4* const row[1] = {
+      (const uint4*)((const char*)(DOWN ? p.a_down : p.a_gu) + ((int64_t)e * rows + r) * K * kSize)};
   f32x4 acc[1];
-  wave_tile<BF16, 1, 1, W>(
-      (const uint4*)((const char*)(DOWN ? p.a_down : p.a_gu) + ((int64_t)e * rows + r) * K * kSize), tok, chunks, w, acc);
+  wave_tile<BF16, 1, 1, 1, W>(row, tok, chunks, w, acc);
   f32x4(&one)[W][1][64] = *(f32x4(*)[W][1][64])tiles;
   add_tiles(acc, one, w, l);
   const int o = r0 + 4 * (l >> 4);
@@ -127,7 +142,8 @@ __device__ __forceinline__ float low_dot(const void* b, int64_t row, const float
         s = fmaf(bf16_hi(q[i]), low[k + 2 * i + 1], s);
       }
     } else {
-      const float4 v = *(const float4*)((const float*)b + row * r + k), u = *(const float4*)((const float*)b + row * r + k + 4);
+      const float* const b4 = (const float*)b + row * r + k;
+      const float4 v = *(const float4*)b4, u = *(const float4*)(b4 + 4);
       s = fmaf(v.x, low[k], s);
       s = fmaf(v.y, low[k + 1], s);
       s = fmaf(v.z, low[k + 2], s);
@@ -146,7 +162,7 @@ __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 
 // B's rows of one token: a value of a (or of y) a thread.
 template <bool BF16, bool DOWN>
-__global__ __launch_bounds__(256) void few_expand_kernel(AdapterArgs p) {
+__global__ __launch_bounds__(256) void few_expand_kernel(AdapterArgs p, int splits) {
   typedef typename std::conditional<BF16, uint16_t, float>::type elem;
   extern __shared__ float low[];
   const int t = blockIdx.y, e = adapter_of(p, t), width = DOWN ? p.d : p.F, rows = DOWN ? p.r : 2 * p.r;
@@ -157,11 +173,17 @@ __global__ __launch_bounds__(256) void few_expand_kernel(AdapterArgs p) {
   if (c >= width) return;
   if constexpr (DOWN) {
     float v = p.raw[(int64_t)t * p.d + c];
+    for (int k = 1; k < splits; ++k) v += p.raw[((int64_t)k * p.T + t) * p.d + c];
     if (e >= 0) v += low_dot<BF16>(p.b_down, (int64_t)e * p.d + c, low, p.r);
     if (p.y_in) v += p.y_in[(int64_t)t * p.d + c];
     store1((elem*)p.y + (int64_t)t * p.d + c, v);
   } else {
-    float g = p.raw[(int64_t)t * 2 * p.F + c], u = p.raw[(int64_t)t * 2 * p.F + p.F + c];
+    float g = 0.0f, u = 0.0f;
+    for (int k = 0; k < splits; ++k) {
+      const float* const raw = p.raw + ((int64_t)k * p.T + t) * 2 * p.F + c;
+      g += raw[0];
+      u += raw[p.F];
+    }
     if (e >= 0) {
       g += low_dot<BF16>(p.b_gu, (int64_t)e * 2 * p.F + c, low, p.r);
       u += low_dot<BF16>(p.b_gu, (int64_t)e * 2 * p.F + p.F + c, low + p.r, p.r);
@@ -172,6 +194,28 @@ __global__ __launch_bounds__(256) void few_expand_kernel(AdapterArgs p) {
 
 // ---------------------------------------------------------------- more tokens
 
+// Counts this lane's token into its bin: its place there. Neighbouring tokens are often of one request, so that the
+// first four bins met in a wave take one LDS atomic each (4096 tokens of 16 adapters: 7.3 us; an atomic a token 10).
+__device__ __forceinline__ int place_in(int* bins, int bin) {  // bin < 0: no token
+  int at = 0;
+  bool open = bin >= 0;
+  for (int k = 0; k < 4; ++k) {
+    const uint64_t todo = __ballot(open);
+    if (!todo) return at;
+    const int lead = __builtin_ctzll(todo), b = readlane_i32(bin, lead);
+    const uint64_t same = __ballot(open && bin == b);
+    int base = 0;
+    if (lane_id() == lead) base = atomicAdd(bins + b, __popcll(same));
+    base = readlane_i32(base, lead);
+    if (open && bin == b) {
+      at = base + __popcll(same & lanemask_lt());
+      open = false;
+    }
+  }
+  if (open) at = atomicAdd(bins + bin, 1);
+  return at;
+}
+
 // Tokens by adapter (bin n: none), and the runs of up to sixteen places of one adapter. One workgroup.
 constexpr int kPlanThreads = 1024;
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AdapterArgs p) {
@@ -180,9 +224,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AdapterArgs p) {
   const int tid = threadIdx.x, l = tid & 63, w = tid >> 6, nb = p.n + 1;
   for (int i = tid; i < nb; i += kPlanThreads) bins[i] = 0;
   __syncthreads();
-  for (int t = tid; t < p.T; t += kPlanThreads) {
-    const int e = adapter_of(p, t);
-    atomicAdd(bins + (e < 0 ? p.n : e), 1);
+  for (int t0 = 0; t0 < p.T; t0 += kPlanThreads) {
+    const int e = t0 + tid < p.T ? adapter_of(p, t0 + tid) : 0;
+    place_in(bins, t0 + tid >= p.T ? -1 : e < 0 ? p.n : e);
   }
   __syncthreads();
   // A thread's bins are neighbours; exclusive sums of tokens and of runs over the threads.
@@ -211,14 +255,18 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AdapterArgs p) {
     at += count;
   }
   __syncthreads();
-  for (int t = tid; t < p.T; t += kPlanThreads) {
-    const int e = adapter_of(p, t), place = atomicAdd(bins + (e < 0 ? p.n : e), 1);
-    p.order[place] = t;
-    p.ident[place] = e;
+  for (int t0 = 0; t0 < p.T; t0 += kPlanThreads) {
+    const int t = t0 + tid, e = t < p.T ? adapter_of(p, t) : 0;
+    const int place = place_in(bins, t >= p.T ? -1 : e < 0 ? p.n : e);
+    if (t < p.T) {
+      p.order[place] = t;
+      p.ident[place] = e;
+    }
   }
 }
 
-// low values of a run's tokens: sixteen A rows a workgroup.
+// low values of a run's tokens: sixteen A rows a workgroup (32: 17.0 us instead of 19.6 for 4096 tokens of 16 adapters,
+// rank 32, but 7.8 instead of 6.9 for a few hundred).
 template <bool BF16, bool DOWN>
 __global__ __launch_bounds__(256) void run_low_kernel(AdapterArgs p) {
   constexpr int W = 4, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
@@ -232,10 +280,10 @@ __global__ __launch_bounds__(256) void run_low_kernel(AdapterArgs p) {
   const char* const in = DOWN ? (const char*)p.act + (int64_t)place * K * kSize
                               : (const char*)p.x + (int64_t)p.order[place] * K * kSize;
   const uint4* const tok[1] = {(const uint4*)in};
+  const uint4* const row[1] = {
+      (const uint4*)((const char*)(DOWN ? p.a_down : p.a_gu) + ((int64_t)run.z * rows + r) * K * kSize)};
   f32x4 acc[1];
-  wave_tile<BF16, 1, 1, W>(
-      (const uint4*)((const char*)(DOWN ? p.a_down : p.a_gu) + ((int64_t)run.z * rows + r) * K * kSize), tok, K / E, w,
-      acc);
+  wave_tile<BF16, 1, 1, 1, W>(row, tok, K / E, w, acc);
   add_tiles(acc, tiles, w, l);
   const int o = r0 + 4 * (l >> 4);
   if (w == 0 && (l & 15) < run.y && o < rows) {
@@ -259,6 +307,7 @@ __device__ __forceinline__ typename T::frag low_frag(const typename T::elem* row
 template <class T, int TM, int TN, int WR, int WC, bool DOWN>
 __global__ __launch_bounds__(64 * WR * WC) void adapter_tile_kernel(AdapterArgs p) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32, FN = TN / 2;
+  static_assert(DOWN || NI % 2 == 0, "a wave holds gate rows and their up rows");
   typedef typename T::elem elem;
   __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
@@ -373,7 +422,7 @@ Layout layout(const Shape& s, int F, int n, int r) {
   };
   o.act = take(T * F * size);
   if (s.T <= kFewTokens) {
-    o.raw = take(T * (2 * (size_t)F > (size_t)s.d ? 2 * (size_t)F : (size_t)s.d) * 4);
+    o.raw = take(kMaxParts * T * (2 * (size_t)F > (size_t)s.d ? 2 * (size_t)F : (size_t)s.d) * 4);
     o.low = take(T * 2 * r * 4);
   } else {
     o.max_runs = (int64_t)(T / 16 + (T < (size_t)n ? T : (size_t)n));
@@ -386,24 +435,40 @@ Layout layout(const Shape& s, int F, int n, int r) {
   return o;
 }
 
+// Parts of a few-token projection with more than sixteen tokens: of at least 512 bytes a row, as many as bring the
+// weights' workgroups to one per compute unit, four at most.
+RowSplit row_split(int rows, int K, int size, int rb, int a_groups) {
+  RowSplit o;
+  const int groups = (rows + 16 * rb - 1) / (16 * rb), chunks = K * size / 16;
+  int parts = 1;
+  while (rb > 1 && parts < kMaxParts && groups * parts < 256 && chunks / (2 * parts) >= 32) parts *= 2;
+  o.chunks = ((chunks + parts - 1) / parts + 7) / 8 * 8;
+  o.splits = (chunks + o.chunks - 1) / o.chunks;
+  o.weight_groups = groups * o.splits;
+  o.a_groups = a_groups;
+  return o;
+}
+
 template <bool BF16, bool DOWN>
-void launch_rows(const AdapterArgs& p, hipStream_t st) {
-  const int weights = ((DOWN ? p.d : 2 * p.F) + 15) / 16;
-  const int a_groups = p.n ? ((DOWN ? p.r : 2 * p.r) + 15) / 16 : 0;
-  const dim3 grid((unsigned)(weights + p.T * a_groups));
-  const int tb = (p.T + 15) / 16;
-#define OMNIMOE_ROWS(TB_) \
-  hipLaunchKernelGGL((few_rows_kernel<BF16, TB_, DOWN>), grid, dim3(64 * PW), 0, st, p, weights, a_groups)
-  if (tb == 1) OMNIMOE_ROWS(1);
-  else if (tb == 2) OMNIMOE_ROWS(2);
-  else if (tb == 3) OMNIMOE_ROWS(3);
-  else OMNIMOE_ROWS(4);
+int launch_rows(const AdapterArgs& p, hipStream_t st) {
+  const int tb = (p.T + 15) / 16, rb = tb > 1 ? 2 : 1;
+  const RowSplit split = row_split(DOWN ? p.d : 2 * p.F, DOWN ? p.F : p.d, BF16 ? 2 : 4, rb,
+                                   p.n ? ((DOWN ? p.r : 2 * p.r) + 15) / 16 : 0);
+  const dim3 grid((unsigned)(split.weight_groups + p.T * split.a_groups));
+#define OMNIMOE_ROWS(RB_, TB_) \
+  hipLaunchKernelGGL((few_rows_kernel<BF16, RB_, TB_, DOWN>), grid, dim3(256), 0, st, p, split)
+  if (tb == 1) OMNIMOE_ROWS(1, 1);
+  else if (tb == 2) OMNIMOE_ROWS(2, 2);
+  else if (tb == 3) OMNIMOE_ROWS(2, 3);
+  else OMNIMOE_ROWS(2, 4);
 #undef OMNIMOE_ROWS
+  return split.splits;
 }
 
 // The largest tile that leaves few compute units without one: a 4096-token batch, d = d_ff = 2048, down projection (128
-// tiles of 256 x 256) 68 us on 64 x 128, 65 on 128 x 256; fp32, 333 tokens, 520 wide: 29 and 31 us on 64 x 128 (54 and 30
-// tiles), 15 and 20 on 32 x 128.
+// tiles of 256 x 256) 68 us on 64 x 128, 65 on 128 x 256; fp32, 333 tokens, 520 wide, down projection: 31 us on 64 x 128
+// (30 tiles), 20 on 32 x 128. (A wave of the first projection holds gate rows and their up rows, two blocks of them at
+// least: its 32 x 128 tile would have two waves and takes the 64 x 128 tile's 30 us.)
 template <class T, int TM, int TN, int WR, int WC, bool DOWN>
 bool try_tile(const AdapterArgs& p, int64_t least, hipStream_t st) {
   const int64_t width = DOWN ? p.d : p.F, step = DOWN ? TN : TN / 2;
@@ -418,8 +483,8 @@ void launch_tiles(const AdapterArgs& p, hipStream_t st) {
     if (try_tile<T, 256, 256, 2, 4, DOWN>(p, 192, st)) return;
     if (try_tile<T, 128, 256, 2, 4, DOWN>(p, 192, st)) return;
   }
-  if (try_tile<T, 64, 128, 2, 2, DOWN>(p, 192, st)) return;
-  try_tile<T, 32, 128, 1, 4, DOWN>(p, 0, st);
+  if (try_tile<T, 64, 128, 2, 2, DOWN>(p, DOWN ? 192 : 0, st)) return;
+  if constexpr (DOWN) try_tile<T, 32, 128, 1, 4, DOWN>(p, 0, st);
 }
 
 template <class T>
@@ -428,13 +493,13 @@ hipError_t run(const AdapterArgs& p, const Layout& o, bool few, hipStream_t st) 
   hipError_t e;
   if (few) {
     const unsigned T_ = (unsigned)p.T;
-    launch_rows<kBf16, false>(p, st);
+    const int parts = launch_rows<kBf16, false>(p, st);
     hipLaunchKernelGGL((few_expand_kernel<kBf16, false>), dim3((unsigned)((p.F + 255) / 256), T_), dim3(256),
-                       (size_t)2 * p.r * 4, st, p);
+                       (size_t)2 * p.r * 4, st, p, parts);
     if ((e = hipGetLastError())) return e;
-    launch_rows<kBf16, true>(p, st);
+    const int down_parts = launch_rows<kBf16, true>(p, st);
     hipLaunchKernelGGL((few_expand_kernel<kBf16, true>), dim3((unsigned)((p.d + 255) / 256), T_), dim3(256),
-                       (size_t)p.r * 4, st, p);
+                       (size_t)p.r * 4, st, p, down_parts);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), (size_t)(p.n + 1) * 4, st, p);

@@ -38,25 +38,23 @@ struct FewArgs {
   int down_groups;    // workgroups of sixteen output columns
 };
 
-#ifndef PW
-#define PW 4
-#endif
 template <bool BF16>
-__global__ __launch_bounds__(64 * PW) void few_products(FewArgs p) {
-  constexpr int W = PW, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
+__global__ __launch_bounds__(256) void few_products(FewArgs p) {
+  constexpr int W = 4, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
   __shared__ f32x4 tiles[W][1][64];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, t = l & 15;
   if (blockIdx.x == 0 && threadIdx.x < kTokens) p.count[threadIdx.x] = 0;
   const char* const x = (const char*)p.x + (int64_t)(t < p.T ? t : p.T - 1) * p.d * kSize;
+  f32x4 acc[1];
   int g = blockIdx.x;
   const int half = g < p.key_groups[0] ? 0 : 1;
   if (half) g -= p.key_groups[0];
   if (g < (half ? p.key_groups[1] : p.key_groups[0])) {
     const int n = half ? p.n[1] : p.n[0], rows = p.H * n, r0 = g * 16, r = r0 + t < rows ? r0 + t : rows - 1;
+    const uint4* const row[1] = {
+        (const uint4*)((const char*)(half ? p.keys[1] : p.keys[0]) + (int64_t)r * p.dk * kSize)};
     const uint4* const tok[1] = {(const uint4*)(x + (half ? p.col0 * kSize : 0))};
-    const uint4* const row = (const uint4*)((const char*)(half ? p.keys[1] : p.keys[0]) + (int64_t)r * p.dk * kSize);
-    f32x4 acc[1];
-    wave_tile<BF16, 1, 1, W>(row, tok, p.dk / E, w, acc);
+    wave_tile<BF16, 1, 1, 1, W>(row, tok, p.dk / E, w, acc);
     add_tiles(acc, tiles, w, l);
     if (w == 0 && t < p.T)
 #pragma unroll
@@ -68,16 +66,15 @@ __global__ __launch_bounds__(64 * PW) void few_products(FewArgs p) {
       }
     return;
   }
-  // eight features: a lane's four accumulators are the gate and up values of two of them
+  // eight features a workgroup: a lane's four accumulators are the gate and up values of two of them
   const int f0 = (g - p.key_groups[1]) * 8, f = f0 + 2 * (t >> 2) + (t & 1);
   const int r = (f < p.F ? f : p.F - 1) + (t & 2 ? p.F : 0);
+  const uint4* const row[1] = {(const uint4*)((const char*)p.w_gu + (int64_t)r * p.d * kSize)};
   const uint4* const tok[1] = {(const uint4*)x};
-  const uint4* const row = (const uint4*)((const char*)p.w_gu + (int64_t)r * p.d * kSize);
-  f32x4 acc[1];
-  wave_tile<BF16, 1, 1, W>(row, tok, p.d / E, w, acc);
+  wave_tile<BF16, 1, 1, 1, W>(row, tok, p.d / E, w, acc);
   add_tiles(acc, tiles, w, l);
-  if (w == 0) {
-    const int fo = f0 + 2 * (l >> 4);
+  const int fo = f0 + 2 * (l >> 4);
+  if (w == 0 && fo < p.F) {
     const float a0 = activation(1, acc[0][0]) * acc[0][2], a1 = activation(1, acc[0][1]) * acc[0][3];
     if constexpr (BF16) {
       // three bf16 values a feature, their sum a itself: the down projection keeps fp32's accuracy
@@ -231,16 +228,16 @@ __device__ __forceinline__ void down_group(const FewArgs& p, FinishShared& sh, i
   constexpr int E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4, NB = BF16 ? kSplit : 1;
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, t = l & 15;
   const int r = g * 16 + t < p.d ? g * 16 + t : p.d - 1;
-  const uint4* const row = (const uint4*)((const char*)p.w_down + (int64_t)r * p.F * kSize);
+  const uint4* const row[1] = {(const uint4*)((const char*)p.w_down + (int64_t)r * p.F * kSize)};
   // (the hidden values of lanes past the last token are that token's again)
   auto act = [&](int n) { return (const uint4*)((const char*)p.act + (int64_t)(n * kTokens + t) * p.F * kSize); };
   f32x4 acc[1];
   if constexpr (BF16) {
     const uint4* const tok[NB] = {act(0), act(1), act(2)};
-    wave_tile<BF16, NB, 1, kWaves>(row, tok, p.F / E, w, acc);
+    wave_tile<BF16, 1, NB, 1, kWaves>(row, tok, p.F / E, w, acc);
   } else {
     const uint4* const tok[NB] = {act(0)};
-    wave_tile<BF16, NB, 1, kWaves>(row, tok, p.F / E, w, acc);
+    wave_tile<BF16, 1, NB, 1, kWaves>(row, tok, p.F / E, w, acc);
   }
   add_tiles(acc, sh.tiles, w, l);
   int mine = 0;
@@ -464,9 +461,9 @@ hipError_t launch_few(const Shape& s, int F, const void* x, const void* keys_row
   p.part = (float*)w;
   w += up((size_t)s.rows * s.d * 4);
   p.shared = (float*)w;
-  const dim3 products((unsigned)(p.key_groups[0] + p.key_groups[1] + F / 8));
-  if (s.bf16) hipLaunchKernelGGL(few_products<true>, products, dim3(64 * PW), 0, st, p);
-  else hipLaunchKernelGGL(few_products<false>, products, dim3(64 * PW), 0, st, p);
+  const dim3 products((unsigned)(p.key_groups[0] + p.key_groups[1] + (F + 7) / 8));
+  if (s.bf16) hipLaunchKernelGGL(few_products<true>, products, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL(few_products<false>, products, dim3(256), 0, st, p);
   const dim3 finish((unsigned)(s.rows + p.down_groups));
   const int n = s.nr > s.nc ? s.nr : s.nc;
 #define OMNIMOE_FEW(R_)                                                                         \

@@ -37,16 +37,16 @@ struct Chunk<false> {
   }
 };
 
-// The weights' rows against NB token operands, summed over this wave's steps (w of W): a step is four lanes x 32 bytes
+// RB x 16 weight rows against NB token operands, summed over this wave's steps (w of W): a step is four lanes x 32 bytes
 // (128 bytes of every row), a wave takes U neighbouring ones at a time and has their weights in flight together, U as
 // large as leaves every wave some.
-// row: this lane's weight row, of `chunks` times 16 bytes; tok: this lane's token row in each of the operands (lanes past
-// the last token have that one's: their columns of the tile are not used), which have a tile each (NACC = NB) or are
-// summed (NACC = 1). The loads are unconditional; chunks past the row's end read its last one, and the weights' are then
-// zeros.
-template <bool BF16, int NB, int NACC, int W, int U>
-__device__ __forceinline__ void wave_steps(const uint4* row, const uint4* const (&tok)[NB], int chunks, int w,
-                                           f32x4 (&acc)[NACC]) {
+// row: this lane's weight row in each of the row blocks, of `chunks` times 16 bytes; tok: this lane's token row in each of
+// the operands (lanes past the last token have that one's: their columns of the tile are not used), which have tiles of
+// their own (NACC = NB: tile b NB + n) or are summed (NACC = 1). The loads are unconditional; chunks past the row's end
+// read its last one and become zeros, the token's too (its infinity times a weight's zero would not be one).
+template <bool BF16, int RB, int NB, int NACC, int W, int U>
+__device__ __forceinline__ void wave_steps(const uint4* const (&row)[RB], const uint4* const (&tok)[NB], int chunks, int w,
+                                           f32x4 (&acc)[RB * NACC]) {
   const int quad = (threadIdx.x & 63) >> 4;
   auto steps = [&](int s0, auto whole) {
     constexpr bool kWhole = decltype(whole)::value;
@@ -54,11 +54,13 @@ __device__ __forceinline__ void wave_steps(const uint4* row, const uint4* const 
       const int c = (s0 + i) * 8 + quad * 2 + e;
       return kWhole || c < chunks ? c : chunks - 1;
     };
-    uint4 a[U][2];
+    uint4 a[U][2][RB];
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) a[i][e] = row[chunk(i, e)];
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int r = 0; r < RB; ++r) a[i][e][r] = row[r][chunk(i, e)];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       uint4 b[2][NB];
@@ -68,9 +70,17 @@ __device__ __forceinline__ void wave_steps(const uint4* row, const uint4* const 
         for (int n = 0; n < NB; ++n) b[e][n] = tok[n][chunk(i, e)];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        if (!kWhole && (s0 + i) * 8 + quad * 2 + e >= chunks) a[i][e] = make_uint4(0, 0, 0, 0);
+        if (!kWhole && (s0 + i) * 8 + quad * 2 + e >= chunks) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n) Chunk<BF16>::mma(acc[NACC == NB ? n : 0], a[i][e], b[e][n]);
+          for (int r = 0; r < RB; ++r) a[i][e][r] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int n = 0; n < NB; ++n) b[e][n] = make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+#pragma unroll
+          for (int n = 0; n < NB; ++n) Chunk<BF16>::mma(acc[r * NACC + (NACC == NB ? n : 0)], a[i][e][r], b[e][n]);
+        }
       }
     }
   };
@@ -78,14 +88,14 @@ __device__ __forceinline__ void wave_steps(const uint4* row, const uint4* const 
   for (; (s0 + U) * 8 <= chunks; s0 += W * U) steps(s0, std::true_type{});
   if (s0 * 8 < chunks) steps(s0, std::false_type{});
 }
-template <bool BF16, int NB, int NACC, int W>
-__device__ __forceinline__ void wave_tile(const uint4* row, const uint4* const (&tok)[NB], int chunks, int w,
-                                          f32x4 (&acc)[NACC]) {
+template <bool BF16, int RB, int NB, int NACC, int W>
+__device__ __forceinline__ void wave_tile(const uint4* const (&row)[RB], const uint4* const (&tok)[NB], int chunks, int w,
+                                          f32x4 (&acc)[RB * NACC]) {
 #pragma unroll
-  for (int n = 0; n < NACC; ++n) acc[n] = {0.f, 0.f, 0.f, 0.f};
-  if (chunks >= 32 * W) wave_steps<BF16, NB, NACC, W, 4>(row, tok, chunks, w, acc);
-  else if (chunks >= 16 * W) wave_steps<BF16, NB, NACC, W, 2>(row, tok, chunks, w, acc);
-  else wave_steps<BF16, NB, NACC, W, 1>(row, tok, chunks, w, acc);
+  for (int n = 0; n < RB * NACC; ++n) acc[n] = {0.f, 0.f, 0.f, 0.f};
+  if (chunks >= 32 * W) wave_steps<BF16, RB, NB, NACC, W, 4>(row, tok, chunks, w, acc);
+  else if (chunks >= 16 * W) wave_steps<BF16, RB, NB, NACC, W, 2>(row, tok, chunks, w, acc);
+  else wave_steps<BF16, RB, NB, NACC, W, 1>(row, tok, chunks, w, acc);
 }
 
 // Sum of the W waves' tiles in wave order, on wave 0.
