@@ -303,11 +303,13 @@ __device__ __forceinline__ typename T::frag low_frag(const typename T::elem* row
 }
 
 // A tile of TM places x TN weight rows: of W_gu TN / 2 gate and TN / 2 up rows (DOWN: of W_down TN), then the low-rank
-// part, then a = silu(g) u by places (DOWN: y by tokens).
+// part, then a = silu(g) u by places (DOWN: y by tokens). A wave of W_gu's tile holds gate rows and the same features' up
+// rows; where it has one block only (kApart), the second half of the waves holds the up rows and hands them over in LDS.
 template <class T, int TM, int TN, int WR, int WC, bool DOWN>
 __global__ __launch_bounds__(64 * WR * WC) void adapter_tile_kernel(AdapterArgs p) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32, FN = TN / 2;
-  static_assert(DOWN || NI % 2 == 0, "a wave holds gate rows and their up rows");
+  constexpr bool kApart = !DOWN && NI == 1;
+  static_assert(DOWN || NI % 2 == 0 || (MJ == 1 && WR == 1 && WC % 2 == 0), "gate rows and their up rows");
   typedef typename T::elem elem;
   __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
@@ -318,9 +320,9 @@ __global__ __launch_bounds__(64 * WR * WC) void adapter_tile_kernel(AdapterArgs 
   for (int j = 0; j < MJ; ++j) b0[j] = (wr * MJ + j) * 32;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
-    if constexpr (DOWN) {
+    if constexpr (DOWN || kApart) {
       a0[i] = (wc * NI + i) * 32;
-      c0[i] = n0 + a0[i];
+      c0[i] = n0 + (kApart ? a0[i] % FN : a0[i]);
     } else {  // even blocks: gate rows, odd ones: the same features' up rows
       const int f = (wc * (NI / 2) + i / 2) * 32;
       a0[i] = f + (i & 1) * FN;
@@ -356,7 +358,7 @@ __global__ __launch_bounds__(64 * WR * WC) void adapter_tile_kernel(AdapterArgs 
       const elem* const b = (const elem*)(DOWN ? p.b_down : p.b_gu) + (int64_t)f * (DOWN ? p.d : 2 * p.F) * r;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int up = !DOWN && (i & 1), c = c0[i] + (lane & 31);
+        const int up = kApart ? wc >= WC / 2 : !DOWN && (i & 1), c = c0[i] + (lane & 31);
         const elem* const brow = b + (int64_t)((c < width ? c : width - 1) + (up ? p.F : 0)) * r;
         tg_f32x16 s;
 #pragma unroll
@@ -365,6 +367,26 @@ __global__ __launch_bounds__(64 * WR * WC) void adapter_tile_kernel(AdapterArgs 
           tile_mma(s, low_frag<T>(brow, r, ks, half), low_frag<T>(low + (up ? r : 0), r, ks, half));
 #pragma unroll
         for (int q = 0; q < 16; ++q) acc[i][j][q] += e == f ? s[q] : 0.0f;
+      }
+    }
+    tg_f32x16 ups;
+    if constexpr (kApart) {
+      float4(*const turned)[4][64] = (float4(*)[4][64])st0;
+      __syncthreads();
+      if (wc >= WC / 2)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          turned[wc - WC / 2][q][lane] =
+              make_float4(acc[0][j][4 * q], acc[0][j][4 * q + 1], acc[0][j][4 * q + 2], acc[0][j][4 * q + 3]);
+      __syncthreads();
+      if (wc >= WC / 2) return;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float4 v = turned[wc][q][lane];
+        ups[4 * q] = v.x;
+        ups[4 * q + 1] = v.y;
+        ups[4 * q + 2] = v.z;
+        ups[4 * q + 3] = v.w;
       }
     }
     if (place >= p.T) continue;
@@ -395,7 +417,8 @@ __global__ __launch_bounds__(64 * WR * WC) void adapter_tile_kernel(AdapterArgs 
           if (c >= width) continue;
           float v[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = activation(1, acc[i][j][4 * q + k]) * acc[i + 1][j][4 * q + k];
+          for (int k = 0; k < 4; ++k)
+            v[k] = activation(1, acc[i][j][4 * q + k]) * (kApart ? ups[4 * q + k] : acc[kApart ? 0 : i + 1][j][4 * q + k]);
           store4((elem*)p.act + (int64_t)place * p.F + c, v[0], v[1], v[2], v[3]);
         }
     }
@@ -466,9 +489,8 @@ int launch_rows(const AdapterArgs& p, hipStream_t st) {
 }
 
 // The largest tile that leaves few compute units without one: a 4096-token batch, d = d_ff = 2048, down projection (128
-// tiles of 256 x 256) 68 us on 64 x 128, 65 on 128 x 256; fp32, 333 tokens, 520 wide, down projection: 31 us on 64 x 128
-// (30 tiles), 20 on 32 x 128. (A wave of the first projection holds gate rows and their up rows, two blocks of them at
-// least: its 32 x 128 tile would have two waves and takes the 64 x 128 tile's 30 us.)
+// tiles of 256 x 256) 68 us on 64 x 128, 65 on 128 x 256; fp32, 333 tokens, 520 wide: 30 and 31 us on 64 x 128 (54 and 30
+// tiles), 20 and 20 on 32 x 128.
 template <class T, int TM, int TN, int WR, int WC, bool DOWN>
 bool try_tile(const AdapterArgs& p, int64_t least, hipStream_t st) {
   const int64_t width = DOWN ? p.d : p.F, step = DOWN ? TN : TN / 2;
@@ -483,8 +505,8 @@ void launch_tiles(const AdapterArgs& p, hipStream_t st) {
     if (try_tile<T, 256, 256, 2, 4, DOWN>(p, 192, st)) return;
     if (try_tile<T, 128, 256, 2, 4, DOWN>(p, 192, st)) return;
   }
-  if (try_tile<T, 64, 128, 2, 2, DOWN>(p, DOWN ? 192 : 0, st)) return;
-  if constexpr (DOWN) try_tile<T, 32, 128, 1, 4, DOWN>(p, 0, st);
+  if (try_tile<T, 64, 128, 2, 2, DOWN>(p, 192, st)) return;
+  try_tile<T, 32, 128, 1, 4, DOWN>(p, 0, st);
 }
 
 template <class T>
