@@ -37,7 +37,7 @@ def kernel_sources_hash(files):
 # Source files each kernel group is built from (a counter file stays valid while they match).
 KERNEL_FILES = {
     "score": ["score_gemm.hip", "device_common.hpp"],
-    "select": ["select.hip", "device_common.hpp"],
+    "select": ["select.hip", "cand_table.hpp", "device_common.hpp"],
     "schedule": ["schedule.hip", "device_common.hpp"],
     "expert_dot": ["expert.hip", "device_common.hpp"],
     "accumulate": ["expert.hip", "device_common.hpp"],
