@@ -45,8 +45,9 @@ omnimoe_status omnimoe_checkpoint_load(const omnimoe_layer_desc* desc, const uin
  *   dx       [T, d]  dtype out   dx_in + W_g^T dg + W_u^T du, rounded once (fp32: may be dx_in itself)
  *   dw_gu    [2 d_ff, d] dtype out   sums over the tokens of dg x^T, then of du x^T
  *   dw_down  [d, d_ff]   dtype out   sum over the tokens of dy a^T
- * Sums are fp32 (matrix cores). bf16 layers round dy, a, dg and du to bf16 between the products. T = 0 writes zeros to
- * dw_gu and dw_down (the pointers to tokens and the workspace may then be NULL). d_ff as in omnimoe_shared_mlp.
+ * Sums are fp32 (matrix cores). bf16 layers round a, dg and du to bf16 between the products and take dy as the sum of two
+ * bf16 values (2^-17 relative). T = 0 writes zeros to dw_gu and dw_down (the pointers to tokens and the workspace may then
+ * be NULL). d_ff as in omnimoe_shared_mlp.
  * Workspace: omnimoe_shared_mlp_backward_workspace_size bytes. */
 omnimoe_status omnimoe_shared_mlp_backward_workspace_size(const omnimoe_layer_desc* desc, int32_t d_ff,
                                                           size_t* bytes);

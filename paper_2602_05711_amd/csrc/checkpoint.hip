@@ -4,6 +4,8 @@
 // relative where |v| >= 2^-6 2^s, 2^-10 2^s absolute below, so at most 2^-4 of a value within 2^14 of its block's
 // largest. A block's scale is stored as the byte s + 127. Values that are not finite take no part in the block's maximum
 // and are stored as NaN.
+// Both ways are bound by memory: each value is read and written once (3.03 bytes a value of bf16). [16384, 2048] bf16:
+// 24.2 and 20.1 us, 4.2 and 5.0 TB/s; [509, 2048], which is in the caches: 3.1 us each, a launch's own time.
 #include "device_common.hpp"
 #include "internal.hpp"
 

@@ -12,8 +12,13 @@
 //     lanes of a 16-lane group one column each of a 4 (k) x 16 (r) block; the 64-byte chunks of row k are permuted by
 //     its low bits, so that a block's four rows fall in distinct banks.
 //   MNC fp32: rows k of 4 R bytes, read value by value; the 128-byte chunks alternate with bit 2 of k.
-// The sum's last stage may be partial: chunks past K are copied from a chunk of zeros. Rows past the operand's last one read that
-// row again (their results are not stored).
+// The sum's last stage may be partial: chunks past K are copied from a chunk of zeros. Rows past the operand's last one
+// read that row again (their results are not stored).
+//
+// A 256 x 256 tile of eight waves moves 256 KiB through the LDS port in a stage (64 in, 192 out), 2048 cycles, as long as
+// its products take on the matrix cores: 1.05 to 1.2 PFLOP/s, where the library's product of the same sizes reaches 1.2 to
+// 1.4. Four waves of 128 x 128, four stages of half the depth, copies spread over the stage and an epilogue through LDS
+// were no faster. Small tiles run at the rate at which L2 fills LDS (9.5 to 11.6 TB/s).
 #pragma once
 
 #include "device_common.hpp"
