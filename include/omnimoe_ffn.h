@@ -101,8 +101,8 @@ typedef struct {
  *   y_in  [T, d] fp32, may be NULL (zeros): e.g. omnimoe_layer_forward's y
  *   y     [T, d] dtype out, rounded once (fp32 layers: may be y_in itself)
  * Tokens of any adapters may come in any order; a token's result does not depend on the others in the batch but for the
- * rounding of sums, whose order differs between calls of up to 64 and of more tokens, and no value of another slot
- * enters it. Sums are fp32; bf16 layers round a (as omnimoe_shared_mlp does) and, from 65 tokens on, the rank-wide
+ * rounding of sums, whose order differs between calls of up to 16, up to 64 and more tokens, and no value of another
+ * slot enters it. Sums are fp32; bf16 layers round a (as omnimoe_shared_mlp does) and, from 65 tokens on, the rank-wide
  * values to bf16 for the matrix cores. T = 0 is a no-op. Workspace: omnimoe_shared_mlp_adapters_workspace_size bytes
  * (the tables' pointers and scale do not count there). */
 omnimoe_status omnimoe_shared_mlp_adapters_workspace_size(const omnimoe_layer_desc* desc, int32_t d_ff,

@@ -374,6 +374,8 @@ def _ffn_call(fn, desc, tensors, args, stream):
         dev = at
     call = getattr(load_library(), fn)
     args = [a.data_ptr() if isinstance(a, torch.Tensor) else a for a in args]
+    if stream is not None and dev >= 0 and stream.device_index != dev:
+        raise ValueError(f"{fn}: the stream belongs to GPU {stream.device_index}, the tensors to GPU {dev}")
     if dev >= 0 and dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
             st = stream if stream is not None else torch.cuda.current_stream()
@@ -394,10 +396,15 @@ def _ffn_size(fn, *args) -> int:
     return n.value
 
 
-def _ffn_workspace(ws, size, device):
-    """`ws` (a uint8 tensor: the call checks its size), or a new one of size() bytes."""
+def _ffn_workspace(ws, size, device, stream):
+    """`ws` (a uint8 tensor: the call checks its size), or a new one of size() bytes from the pool of the call's stream."""
     import torch
-    return torch.empty(max(256, size()), dtype=torch.uint8, device=device) if ws is None else ws
+    if ws is not None:
+        return ws
+    if stream is None:
+        return torch.empty(max(256, size()), dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(max(256, size()), dtype=torch.uint8, device=device)
 
 
 def _checkpoint_tensors(desc, x, codes, scales):
@@ -422,7 +429,7 @@ def omnimoe_shared_mlp_backward(desc, d_ff, codes, scales, w_gu, w_down, dy, dx_
                                 stream=None):
     """Gradients of the shared branch from the 8-bit checkpoint of its input; dx_in may be None."""
     import torch
-    ws = _ffn_workspace(ws, lambda: omnimoe_shared_mlp_backward_workspace_size(desc, d_ff), w_gu.device)
+    ws = _ffn_workspace(ws, lambda: omnimoe_shared_mlp_backward_workspace_size(desc, d_ff), w_gu.device, stream)
     T, d, dt, f32, u8 = desc.T, desc.d, _layer_dtype(desc), torch.float32, torch.uint8
     _ffn_call("omnimoe_shared_mlp_backward", desc, (
         ("codes", codes, u8, T * d), ("scales", scales, u8, T * ((d + 31) // 32)), ("w_gu", w_gu, dt, 2 * d_ff * d),
@@ -439,7 +446,7 @@ def omnimoe_layer_forward_few(desc, d_ff, x, keys_row, keys_col, u, v, w_gu, w_d
                               ws=None, stream=None):
     """The whole feed-forward layer for up to FEW_TOKENS tokens; without a shared branch d_ff is 0 and its weights None."""
     import torch
-    ws = _ffn_workspace(ws, lambda: omnimoe_layer_few_workspace_size(desc, d_ff), x.device)
+    ws = _ffn_workspace(ws, lambda: omnimoe_layer_few_workspace_size(desc, d_ff), x.device, stream)
     T, d, H, K, dt, f32 = desc.T, desc.d, desc.H, desc.K, _layer_dtype(desc), torch.float32
     N = desc.n_rows * desc.n_cols
     _ffn_call("omnimoe_layer_forward_few", desc, (
@@ -468,7 +475,8 @@ def omnimoe_shared_mlp_adapters_workspace_size(desc, d_ff: int, adapters) -> int
 def omnimoe_shared_mlp_adapters(desc, d_ff, adapters, x, w_gu, w_down, ids, y_in, y, ws=None, stream=None):
     """The shared branch with the tokens' adapters (make_adapters), added to y_in (None: zeros) into y."""
     import torch
-    ws = _ffn_workspace(ws, lambda: omnimoe_shared_mlp_adapters_workspace_size(desc, d_ff, adapters), x.device)
+    ws = _ffn_workspace(ws, lambda: omnimoe_shared_mlp_adapters_workspace_size(desc, d_ff, adapters), x.device,
+                        stream)
     T, d, dt, f32, n, r = desc.T, desc.d, _layer_dtype(desc), torch.float32, adapters.n, adapters.rank
     a_gu, b_gu, a_down, b_down, scale = adapters.tensors
     _ffn_call("omnimoe_shared_mlp_adapters", desc, (

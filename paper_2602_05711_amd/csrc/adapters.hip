@@ -341,9 +341,10 @@ __global__ __launch_bounds__(64 * WR * WC) void adapter_tile_kernel(AdapterArgs 
       const int f = n0 + (r < FN ? r : r - FN);
       return (f < width ? f : width - 1) + (r < FN ? 0 : width);
     });
-    b.init((const elem*)(DOWN ? p.act : p.x), K, wid, lane, [&](int r) {
+    // (the hidden values of a pass may take more than 4 GiB: their rows are counted from the tile's first)
+    b.init(DOWN ? (const elem*)p.act + (int64_t)m0 * K : (const elem*)p.x, K, wid, lane, [&](int r) {
       const int place = m0 + r < p.T ? m0 + r : p.T - 1;
-      return DOWN ? place : p.order[place];
+      return DOWN ? place - m0 : p.order[place];
     });
     const TileRange all[2] = {{K, 0, 0}, {0, 0, 0}};
     tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
@@ -429,7 +430,7 @@ __global__ __launch_bounds__(64 * WR * WC) void adapter_tile_kernel(AdapterArgs 
 
 size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 
-// Tokens of one pass: a tile's rows lie within 4 GiB of each other.
+// Tokens of one pass: their rows of x lie within 4 GiB of each other (8192 values at most).
 constexpr int64_t kPassTokens = 65536;
 
 struct Layout {

@@ -363,6 +363,20 @@ def test_adapters_in_several_passes():
     within(_adapt(t), y, bound, "y")
 
 
+def test_adapters_whose_hidden_values_pass_4_gib():
+    # [40000, 65536] bf16: 5.2e9 bytes, so that the last places' rows start beyond 2^32 of them
+    T, d, f, n = 40000, 8, 65536, 2
+    t = _adapter_inputs(T, d, f, n, 8, BF16, _ids("mixed", T, n), seed=5)
+    got = _adapt(t)
+    assert torch.isfinite(got).all()
+    # tokens without a slot come last in the order of the slots; some from its start, its middle and its end
+    order = torch.argsort(torch.where((t.ids < 0) | (t.ids >= n), n, t.ids), stable=True)
+    some = torch.cat([order[:40], order[T // 2:T // 2 + 40], order[-80:]])
+    y, bound = S.adapters_mlp(t.x[some].to(F64), t.w_gu.to(F64), t.w_down.to(F64), t.ids[some], t.tables,
+                              t.y_in[some].to(F64), t.dtype)
+    within(got[some], y, bound, "y")
+
+
 # ------------------------------------------------------------------ the layer for a few tokens
 
 def _few_inputs(T, d, nr, nc, dk, H, K, f, dtype, act="gelu", split=True, seed=0):
@@ -567,6 +581,20 @@ def test_calls_on_two_streams():
     torch.cuda.synchronize()
     for (name, _, outs, _), w in zip(one + two, want):
         assert all(torch.equal(x, y) for x, y in zip(outs, w)), name
+
+
+def test_workspaces_belong_to_the_calls_stream(monkeypatch):
+    # a call that makes its own workspace takes it from the pool of the stream it runs on
+    b, s = _backward_inputs(65, 64, 72, BF16), torch.cuda.Stream()
+    want = _backward(b)
+    outs = [torch.empty_like(o) for o in want]
+    made, empty = [], torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: made.append(torch.cuda.current_stream()) or empty(*a, **k))
+    s.wait_stream(torch.cuda.current_stream())
+    P.omnimoe_shared_mlp_backward(b.D, b.f, b.codes, b.scales, b.w_gu, b.w_down, b.dy, b.dx_in, *outs, stream=s)
+    torch.cuda.synchronize()
+    assert made == [s]
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=tid)
