@@ -376,13 +376,18 @@ def _ffn_call(fn, desc, tensors, args, stream):
     args = [a.data_ptr() if isinstance(a, torch.Tensor) else a for a in args]
     if stream is not None and dev >= 0 and stream.device_index != dev:
         raise ValueError(f"{fn}: the stream belongs to GPU {stream.device_index}, the tensors to GPU {dev}")
-    if dev >= 0 and dev != torch.cuda.current_device():
-        with torch.cuda.device(dev):
-            st = stream if stream is not None else torch.cuda.current_stream()
-            _check(fn, call(ctypes.byref(desc), *args, st.cuda_stream))
-    else:
-        st = stream if stream is not None else torch.cuda.current_stream()
-        _check(fn, call(ctypes.byref(desc), *args, st.cuda_stream))
+    at = torch.cuda.current_device()
+    if dev < 0 or dev == at:
+        # (the stream's address alone: torch.cuda.current_stream() takes 2.9 us)
+        _check(fn, call(ctypes.byref(desc), *args, _raw_stream(at) if stream is None else stream.cuda_stream))
+        return
+    with torch.cuda.device(dev):
+        _check(fn, call(ctypes.byref(desc), *args, _raw_stream(dev) if stream is None else stream.cuda_stream))
+
+
+def _raw_stream(device):
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _layer_dtype(desc):
@@ -458,13 +463,26 @@ def omnimoe_layer_forward_few(desc, d_ff, x, keys_row, keys_col, u, v, w_gu, w_d
         (d_ff, x, keys_row, keys_col, u, v, w_gu, w_down, y, idx_out, gates_out, ws, ws.numel()), stream)
 
 
+def _adapter_tensors(n, r, d, d_ff, dt, tensors):
+    import torch
+    a_gu, b_gu, a_down, b_down, scale = tensors
+    return (("a_gu", a_gu, dt, n * 2 * r * d), ("b_gu", b_gu, dt, n * 2 * d_ff * r), ("a_down", a_down, dt, n * r * d_ff),
+            ("b_down", b_down, dt, n * d * r), ("scale", scale, torch.float32, n))
+
+
 def make_adapters(a_gu, b_gu, a_down, b_down, scale=None) -> OmnimoeAdapters:
     """The adapter tables' descriptor, which keeps the tensors: a_gu [n, 2 rank, d], b_gu [n, 2 d_ff, rank],
     a_down [n, rank, d_ff], b_down [n, d, rank], scale [n] fp32 or None."""
-    n, rank, _ = a_down.shape
+    n, rank, d_ff = a_down.shape
     a = OmnimoeAdapters(n=n, rank=rank, a_gu=a_gu.data_ptr(), b_gu=b_gu.data_ptr(), a_down=a_down.data_ptr(),
                         b_down=b_down.data_ptr(), scale=None if scale is None else scale.data_ptr())
     a.tensors = (a_gu, b_gu, a_down, b_down, scale)
+    # what a call's tables must be, where they are: checked here once, since the tables outlive many calls
+    at, d = a_gu.get_device(), b_down.shape[1]
+    a.fits = (at, d, d_ff, a_gu.dtype)
+    for _, t, dtype, size in _adapter_tensors(n, rank, d, d_ff, a_gu.dtype, a.tensors):
+        if t is not None and (t.dtype is not dtype or t.numel() != size or not t.is_contiguous() or t.get_device() != at):
+            a.fits = None
     return a
 
 
@@ -477,11 +495,12 @@ def omnimoe_shared_mlp_adapters(desc, d_ff, adapters, x, w_gu, w_down, ids, y_in
     import torch
     ws = _ffn_workspace(ws, lambda: omnimoe_shared_mlp_adapters_workspace_size(desc, d_ff, adapters), x.device,
                         stream)
-    T, d, dt, f32, n, r = desc.T, desc.d, _layer_dtype(desc), torch.float32, adapters.n, adapters.rank
-    a_gu, b_gu, a_down, b_down, scale = adapters.tensors
+    T, d, dt, f32 = desc.T, desc.d, _layer_dtype(desc), torch.float32
+    tables = ()
+    if adapters.fits != (x.get_device(), d, d_ff, dt):
+        tables = _adapter_tensors(adapters.n, adapters.rank, d, d_ff, dt, adapters.tensors)
     _ffn_call("omnimoe_shared_mlp_adapters", desc, (
         ("x", x, dt, T * d), ("w_gu", w_gu, dt, 2 * d_ff * d), ("w_down", w_down, dt, d * d_ff),
-        ("ids", ids, torch.int32, T), ("y_in", y_in, f32, T * d), ("y", y, dt, T * d),
-        ("a_gu", a_gu, dt, n * 2 * r * d), ("b_gu", b_gu, dt, n * 2 * d_ff * r), ("a_down", a_down, dt, n * r * d_ff),
-        ("b_down", b_down, dt, n * d * r), ("scale", scale, f32, n), ("ws", ws, torch.uint8, ws.numel())),
+        ("ids", ids, torch.int32, T), ("y_in", y_in, f32, T * d), ("y", y, dt, T * d), *tables,
+        ("ws", ws, torch.uint8, ws.numel())),
         (d_ff, ctypes.byref(adapters), x, w_gu, w_down, ids, y_in, y, ws, ws.numel()), stream)
