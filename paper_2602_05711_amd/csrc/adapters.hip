@@ -7,8 +7,8 @@
 // Up to 64 tokens (kFewTokens) every weight is read once and that bounds the call: four launches, a weight row's tile of
 // all tokens beside the A rows of every adapter's tokens (sixteen tokens of one adapter to a tile), then B's rows, then
 // the same for the other projection.
-// More tokens are put in the order of their adapters (one workgroup counts, places and lists runs of up to sixteen tokens
-// of one adapter), and the projections run as tile products whose rows follow that order. The low-rank part of a tile is
+// More tokens are put in the order of their adapters (one workgroup counts, places and lists runs of up to sixteen
+// tokens of one adapter), and the projections run as tile products whose rows follow that order. The low-rank part of a tile is
 // r more values of its summed index: for every adapter among a 32-token block's rows (few, in that order) the block's low
 // values meet that adapter's B rows on the matrix cores, and a token keeps the sum of its own adapter only, so that no
 // value of one request reaches another's. The order of the tokens of one adapter is left to LDS atomics: no token's
@@ -216,8 +216,8 @@ __device__ __forceinline__ int place_in(int* bins, int bin) {  // bin < 0: no to
   return at;
 }
 
-// Tokens by adapter (bin n: none), and the runs of up to sixteen places of one adapter. One workgroup.
-constexpr int kPlanThreads = 1024;
+// Tokens by adapter (bin n: none), and the runs of up to kRun places of one adapter. One workgroup.
+constexpr int kPlanThreads = 1024, kRun = 16;
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AdapterArgs p) {
   extern __shared__ int bins[];  // [n + 1] counts, then the next free place
   __shared__ int sums[2][kPlanThreads / 64];
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AdapterArgs p) {
   int tokens = 0, runs = 0;
   for (int i = b0; i < b1; ++i) {
     tokens += bins[i];
-    if (i < p.n) runs += (bins[i] + 15) / 16;
+    if (i < p.n) runs += (bins[i] + kRun - 1) / kRun;
   }
   int at = wave_excl_scan_i32(tokens), run = wave_excl_scan_i32(runs);
   if (l == 63) {
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AdapterArgs p) {
     const int count = bins[i];
     bins[i] = at;
     if (i < p.n)
-      for (int k = 0; k < count; k += 16) p.runs[run++] = make_int4(at + k, count - k < 16 ? count - k : 16, i, 0);
+      for (int k = 0; k < count; k += kRun) p.runs[run++] = make_int4(at + k, min(count - k, kRun), i, 0);
     at += count;
   }
   __syncthreads();
@@ -265,31 +265,37 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AdapterArgs p) {
   }
 }
 
-// low values of a run's tokens: sixteen A rows a workgroup (32: 17.0 us instead of 19.6 for 4096 tokens of 16 adapters,
-// rank 32, but 7.8 instead of 6.9 for a few hundred).
-template <bool BF16, bool DOWN>
+// low values of a run's tokens: 16 RB rows of A a workgroup, two blocks where there are more than sixteen (4096 tokens of
+// 16 adapters, d = d_ff = 2048, rank 32: 16.4 and 11.7 us instead of 19.4 and 12.4). Bound by the loads of rows from L2;
+// runs of 32 and 64 tokens read less but are fewer: 20.1 and 18.0, 12.6 and 16.8 us.
+template <bool BF16, int RB, bool DOWN>
 __global__ __launch_bounds__(256) void run_low_kernel(AdapterArgs p) {
   constexpr int W = 4, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4;
-  __shared__ f32x4 tiles[W][1][64];
+  __shared__ f32x4 tiles[W][RB][64];
   if ((int)blockIdx.x >= *p.nruns) return;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int4 run = p.runs[blockIdx.x];
-  const int rows = DOWN ? p.r : 2 * p.r, K = DOWN ? p.F : p.d, r0 = blockIdx.y * 16;
-  const int r = r0 + (l & 15) < rows ? r0 + (l & 15) : rows - 1;
+  const int rows = DOWN ? p.r : 2 * p.r, K = DOWN ? p.F : p.d, r0 = blockIdx.y * 16 * RB;
   const int place = run.x + ((l & 15) < run.y ? (l & 15) : run.y - 1);
-  const char* const in = DOWN ? (const char*)p.act + (int64_t)place * K * kSize
-                              : (const char*)p.x + (int64_t)p.order[place] * K * kSize;
-  const uint4* const tok[1] = {(const uint4*)in};
-  const uint4* const row[1] = {
-      (const uint4*)((const char*)(DOWN ? p.a_down : p.a_gu) + ((int64_t)run.z * rows + r) * K * kSize)};
-  f32x4 acc[1];
-  wave_tile<BF16, 1, 1, 1, W>(row, tok, K / E, w, acc);
+  const uint4* const tok[1] = {(const uint4*)(DOWN ? (const char*)p.act + (int64_t)place * K * kSize
+                                                   : (const char*)p.x + (int64_t)p.order[place] * K * kSize)};
+  const uint4* row[RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const int r = r0 + 16 * b + (l & 15) < rows ? r0 + 16 * b + (l & 15) : rows - 1;
+    row[b] = (const uint4*)((const char*)(DOWN ? p.a_down : p.a_gu) + ((int64_t)run.z * rows + r) * K * kSize);
+  }
+  f32x4 acc[RB];
+  wave_tile<BF16, RB, 1, 1, W>(row, tok, K / E, w, acc);
   add_tiles(acc, tiles, w, l);
-  const int o = r0 + 4 * (l >> 4);
-  if (w == 0 && (l & 15) < run.y && o < rows) {
-    const float s = p.scale ? p.scale[run.z] : 1.0f;
+  if (w || (l & 15) >= run.y) return;
+  const float s = p.scale ? p.scale[run.z] : 1.0f;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const int o = r0 + 16 * b + 4 * (l >> 4);
+    if (o >= rows) break;
     typedef typename std::conditional<BF16, uint16_t, float>::type elem;
-    store4((elem*)p.lowt + (int64_t)place * rows + o, acc[0][0] * s, acc[0][1] * s, acc[0][2] * s, acc[0][3] * s);
+    store4((elem*)p.lowt + (int64_t)place * rows + o, acc[b][0] * s, acc[b][1] * s, acc[b][2] * s, acc[b][3] * s);
   }
 }
 
@@ -451,7 +457,7 @@ Layout layout(const Shape& s, int F, int n, int r) {
     o.raw = take(kMaxParts * T * (2 * (size_t)F > (size_t)s.d ? 2 * (size_t)F : (size_t)s.d) * 4);
     o.low = take(T * 2 * r * 4);
   } else {
-    o.max_runs = (int64_t)(T / 16 + (T < (size_t)n ? T : (size_t)n));
+    o.max_runs = (int64_t)(T / kRun + (T < (size_t)n ? T : (size_t)n));
     o.lowt = take(T * 2 * r * size);
     o.order = take(T * 4);
     o.ident = take(T * 4);
@@ -491,6 +497,16 @@ int launch_rows(const AdapterArgs& p, hipStream_t st) {
   return split.splits;
 }
 
+template <bool BF16, bool DOWN>
+void launch_low(const AdapterArgs& p, int64_t max_runs, hipStream_t st) {
+  const int rows = DOWN ? p.r : 2 * p.r;
+  if (rows > 16)
+    hipLaunchKernelGGL((run_low_kernel<BF16, 2, DOWN>), dim3((unsigned)max_runs, (unsigned)((rows + 31) / 32)), dim3(256),
+                       0, st, p);
+  else
+    hipLaunchKernelGGL((run_low_kernel<BF16, 1, DOWN>), dim3((unsigned)max_runs), dim3(256), 0, st, p);
+}
+
 // The largest tile that leaves few compute units without one: a 4096-token batch, d = d_ff = 2048, down projection (128
 // tiles of 256 x 256) 68 us on 64 x 128, 65 on 128 x 256; fp32, 333 tokens, 520 wide: 30 and 31 us on 64 x 128 (54 and 30
 // tiles), 20 and 20 on 32 x 128.
@@ -528,14 +544,10 @@ hipError_t run(const AdapterArgs& p, const Layout& o, bool few, hipStream_t st) 
     return hipGetLastError();
   }
   hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), (size_t)(p.n + 1) * 4, st, p);
-  if (p.n)
-    hipLaunchKernelGGL((run_low_kernel<kBf16, false>), dim3((unsigned)o.max_runs, (unsigned)((2 * p.r + 15) / 16)),
-                       dim3(256), 0, st, p);
+  if (p.n) launch_low<kBf16, false>(p, o.max_runs, st);
   if ((e = hipGetLastError())) return e;
   launch_tiles<T, false>(p, st);
-  if (p.n)
-    hipLaunchKernelGGL((run_low_kernel<kBf16, true>), dim3((unsigned)o.max_runs, (unsigned)((p.r + 15) / 16)),
-                       dim3(256), 0, st, p);
+  if (p.n) launch_low<kBf16, true>(p, o.max_runs, st);
   if ((e = hipGetLastError())) return e;
   launch_tiles<T, true>(p, st);
   return hipGetLastError();
