@@ -6,7 +6,7 @@
 // and are stored as NaN.
 // Both ways are bound by memory: each value is read and written once (3.03 bytes a value of bf16). [16384, 2048] bf16:
 // 24.2 and 20.1 us, 4.2 and 5.0 TB/s; [509, 2048], which is in the caches: 3.1 us each, a launch's own time.
-#include "device_common.hpp"
+#include "checkpoint.hpp"
 #include "internal.hpp"
 
 namespace omnimoe {
@@ -81,37 +81,12 @@ template <bool BF16>
 __global__ __launch_bounds__(256) void load_kernel(const uint8_t* __restrict__ codes,
                                                    const uint8_t* __restrict__ scales, void* __restrict__ x,
                                                    int64_t T, int d, int nblk) {
-  const float kLargest = __uint_as_float(BF16 ? 0x7F7F0000u : 0x7F7FFFFFu);
   const int q8 = d / 8;
   const int64_t n = T * q8;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int64_t t = i / q8;
     const int c = (int)(i - t * q8);
-    const uint2 w = *(const uint2*)(codes + i * 8);
-    const int s = (int)scales[t * nblk + (c >> 2)] - 127;
-    float v[8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int p = (int)(h ? w.y : w.x);
-      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(p, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(p, true);
-      const float q[4] = {lo[0], lo[1], hi[0], hi[1]};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float y = ldexpf(q[e], s);
-        // a value next to the type's largest may have been rounded up past it
-        v[4 * h + e] = fabsf(y) > kLargest ? copysignf(kLargest, y) : y;
-      }
-    }
-    if constexpr (BF16) {
-      uint32_t o[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        o[e] = (uint32_t)bf16_rne(v[2 * e]) | ((uint32_t)bf16_rne(v[2 * e + 1]) << 16);
-      *(uint4*)((uint16_t*)x + i * 8) = make_uint4(o[0], o[1], o[2], o[3]);
-    } else {
-      *(float4*)((float*)x + i * 8) = make_float4(v[0], v[1], v[2], v[3]);
-      *(float4*)((float*)x + i * 8 + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    }
+    checkpoint_load8<BF16>(codes + i * 8, scales[t * nblk + (c >> 2)], x, i * 8);
   }
 }
 

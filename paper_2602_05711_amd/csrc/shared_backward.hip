@@ -10,19 +10,27 @@
 // bf16 values, its rounding and what that leaves (2^-17 relative), for two products more: with dy rounded as well, three
 // roundings (dy, a or dg, the result) put the weight gradients 0.0029 of their norm from the exact ones instead of
 // 0.0024, the rounding of the result alone being 0.0017.
+#include "checkpoint.hpp"
 #include "internal.hpp"
 #include "tile_gemm.hpp"
 
 namespace omnimoe {
 namespace {
 
-// hi = bf16(in), lo = bf16(in - hi), eight values a thread. Where hi is not finite, lo is zero. Bound by memory: [16384,
-// 2048] 42 us, 6.4 TB/s (of which the last-level cache serves a part). A pass of its own, because the tiles' operands are
-// copied to LDS without passing registers.
-__global__ __launch_bounds__(256) void split_kernel(const float* __restrict__ in, uint16_t* __restrict__ hi,
-                                                    uint16_t* __restrict__ lo, int64_t n8) {
+// The bf16 operands: the checkpoint's values to x, and dy to hi = bf16(dy) and lo = bf16(dy - hi), eight of each a thread.
+// Where hi is not finite, lo is zero. Bound by memory: [16384, 2048] 59 us, 6.3 TB/s. A pass of its own, because the tiles' operands
+// are copied to LDS without passing registers.
+__global__ __launch_bounds__(256) void operands_kernel(const uint8_t* __restrict__ codes,
+                                                       const uint8_t* __restrict__ scales, const float* __restrict__ dy,
+                                                       uint16_t* __restrict__ x, uint16_t* __restrict__ hi,
+                                                       uint16_t* __restrict__ lo, int64_t T, int d) {
+  const int q8 = d / 8, nblk = (d + 31) / 32;
+  const int64_t n8 = T * q8;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n8; i += (int64_t)gridDim.x * 256) {
-    const float4 a = *(const float4*)(in + i * 8), b = *(const float4*)(in + i * 8 + 4);
+    const float4 a = *(const float4*)(dy + i * 8), b = *(const float4*)(dy + i * 8 + 4);
+    const int64_t t = i / q8;
+    const int c = (int)(i - t * q8);
+    checkpoint_load8<true>(codes + i * 8, scales[t * nblk + (c >> 2)], x, i * 8);
     const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     uint32_t h[4], l[4];
 #pragma unroll
@@ -283,12 +291,12 @@ hipError_t run(const Shape& s, int F, const uint8_t* codes, const uint8_t* scale
   char* part = act + up((size_t)s.T * F * T::kSize);
   hipError_t e;
   if (s.T > 0) {
-    if ((e = launch_checkpoint_load(s.T, d, kBf16, codes, scales, xb, st))) return e;
     if (kBf16) {
-      const int64_t n8 = s.T * d / 8;
-      const int64_t blocks = (n8 + 255) / 256;
-      hipLaunchKernelGGL(split_kernel, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), 0, st, dy,
-                         (uint16_t*)dyb, (uint16_t*)dyl, n8);
+      const int64_t blocks = (s.T * d / 8 + 255) / 256;
+      hipLaunchKernelGGL(operands_kernel, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), 0, st, codes,
+                         scales, dy, (uint16_t*)xb, (uint16_t*)dyb, (uint16_t*)dyl, s.T, d);
+    } else if ((e = launch_checkpoint_load(s.T, d, false, codes, scales, xb, st))) {
+      return e;
     }
     HiddenArgs h{xb, kBf16 ? (const void*)dyb : dy, dyl, w_gu, w_down, dh, act, s.T, d, F};
     bool done = false;
