@@ -4,8 +4,8 @@
 //   dg = da u p (1 + g (1 - p)), du = da g p
 //   dx = dx_in + W_g^T dg + W_u^T du,  dW_g = dg x~^T, dW_u = du x~^T, dW_down = dy a^T (sums over the tokens)
 // Four launches: the checkpoint's and dy's values in the layer's type; the three products that a tile of dg, du and a
-// needs, whose sums meet in registers; dx; the weight gradients, split over the tokens into fp32 partial sums that are
-// added in order. No atomics: the result is the same on every run. Sums are fp32. bf16 layers round a, dg and du to bf16
+// needs, whose sums meet in registers; dx and the weight gradients (large tiles: a launch each), the latter split over the
+// tokens into fp32 partial sums that a last launch adds in order. No atomics: the result is the same on every run. Sums are fp32. bf16 layers round a, dg and du to bf16
 // (once each, to nearest) for the matrix cores, as the forward pass rounds a; dy, fp32 from the caller, enters as two
 // bf16 values, its rounding and what that leaves (2^-17 relative), for two products more: with dy rounded as well, three
 // roundings (dy, a or dg, the result) put the weight gradients 0.0029 of their norm from the exact ones instead of
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(64 * WR * WC) void hidden_kernel(HiddenArgs p) {
 // summed range. Parts (parts > 1) go to part[z][m, n] in fp32, whole sums to out in the layer's type, with add[m, n].
 // With b_lo, B is b + b_lo: the range is run through twice, k in [K, 2 K) being b_lo's.
 // Bound as hidden_kernel: 16384 tokens, d = d_ff = 2048, dx 321 us and the weight gradients 483 us, 0.86 and 1.14
-// PFLOP/s; 4093 tokens, d = d_ff = 512, on 64 x 64 tiles 15.4 and 21.7 us; fp32, 1000 tokens, 520: 27.8 and 24.9 us.
+// PFLOP/s.
 struct Product {
   const void *a, *b, *b_lo;
   int64_t lda, ldb, M;
@@ -141,18 +141,16 @@ struct Product {
   float* part;
 };
 struct ProductArgs {
-  Product p[2];
+  Product p[3];  // dx, dW_gu, dW_down
   int kpart;
 };
+enum { kDx = 1, kWeights = 2 };  // the products of a launch
 
 template <class T, int TM, int TN, int WR, int WC, bool B_MNC>
-__global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args) {
+__device__ __forceinline__ void product_tile(const Product& p, int wg, int kpart, unsigned char* st0, unsigned char* st1) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
   typedef typename T::elem elem;
-  __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
-  const int wg = (int)xcd_contiguous(blockIdx.x, gridDim.x);
-  const Product& p = args.p[wg >= args.p[1].first];
   const int part = (wg - p.first) % p.parts, tile = (wg - p.first) / p.parts;
   const int n0 = tile % p.tiles_n * TN;
   const int64_t m0 = (int64_t)(tile / p.tiles_n) * TM;
@@ -161,7 +159,7 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args)
   {
     const int64_t ka = p.lda * T::kSize, kb = (B_MNC ? p.ldb : 1) * T::kSize;
     const int64_t lo = (const char*)p.b_lo - (const char*)p.b;
-    const int64_t k0 = (int64_t)part * args.kpart, k1 = p.parts == 1 ? 2 * (int64_t)p.K : k0 + args.kpart;
+    const int64_t k0 = (int64_t)part * kpart, k1 = p.parts == 1 ? 2 * (int64_t)p.K : k0 + kpart;
     auto cut = [&](int64_t v) { return (int)(v < 0 ? 0 : v > p.K ? p.K : v); };
     const int h0 = cut(k0), h1 = cut(k1), l0 = cut(k0 - p.K), l1 = p.b_lo ? cut(k1 - p.K) : l0;
     range[0] = {h1 - h0, h0 * ka, h0 * kb};
@@ -211,12 +209,30 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args)
   }
 }
 
-// out = the parts' sum, in order, of one or both products (n4 quads of p[0], then those of p[1]): 4 to 9 us.
+// The workgroups of dx come before the weight gradients', each XCD having neighbouring tiles of both. Small tiles take
+// them in one launch, since neither fills the compute units alone: 4093 tokens, d = d_ff = 512,
+// 32.8 us instead of 15.3 and 21.8; fp32, 1000 tokens, 520, 44.5 instead of 27.8 and 24.8.
+template <class T, int TM, int TN, int WR, int WC, int WHICH>
+__global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args) {
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
+  const unsigned first = WHICH == kWeights ? 0 : WHICH == kDx ? gridDim.x : (unsigned)args.p[1].first;
+  if (blockIdx.x < first) {
+    if constexpr (WHICH & kDx)
+      product_tile<T, TM, TN, WR, WC, false>(args.p[0], (int)xcd_contiguous(blockIdx.x, first), args.kpart, st0, st1);
+  } else {
+    if constexpr (WHICH & kWeights) {
+      const int wg = (int)(first + xcd_contiguous(blockIdx.x - first, gridDim.x - first));
+      product_tile<T, TM, TN, WR, WC, true>(args.p[wg >= args.p[2].first ? 2 : 1], wg, args.kpart, st0, st1);
+    }
+  }
+}
+
+// out = the parts' sum, in order, of one or both weight gradients (n4 quads of dW_gu, then those of dW_down): 4 to 9 us.
 template <class T>
 __global__ __launch_bounds__(256) void add_parts_kernel(ProductArgs args, int64_t n4_first, int64_t n4) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
     const bool second = i >= n4_first;
-    const Product& p = args.p[second];
+    const Product& p = args.p[1 + second];
     const int64_t at = (i - (second ? n4_first : 0)) * 4, size = p.M * p.N;
     float4 v = *(const float4*)(p.part + at);
     for (int z = 1; z < p.parts; ++z) {
@@ -266,15 +282,14 @@ Parts weight_parts(const Shape& s, int F, int tile) {
 
 bool large_tiles(int64_t T, int d, int F, bool bf16) { return bf16 && tiles(T, F, 256, 128) >= 192; }
 
-template <class T, bool B_MNC>
+template <class T, int WHICH>
 void launch_product(bool big, const ProductArgs& g, int workgroups, hipStream_t st) {
-  if constexpr (T::kSize == 2)
+  if constexpr (T::kSize == 2 && WHICH != (kDx | kWeights))
     if (big) {
-      hipLaunchKernelGGL((product_kernel<T, 256, 256, 2, 4, B_MNC>), dim3((unsigned)workgroups), dim3(512), 0, st,
-                         g);
+      hipLaunchKernelGGL((product_kernel<T, 256, 256, 2, 4, WHICH>), dim3((unsigned)workgroups), dim3(512), 0, st, g);
       return;
     }
-  hipLaunchKernelGGL((product_kernel<T, 64, 64, 2, 2, B_MNC>), dim3((unsigned)workgroups), dim3(256), 0, st, g);
+  hipLaunchKernelGGL((product_kernel<T, 64, 64, 2, 2, WHICH>), dim3((unsigned)workgroups), dim3(256), 0, st, g);
 }
 
 template <class T>
@@ -313,25 +328,29 @@ hipError_t run(const Shape& s, int F, const uint8_t* codes, const uint8_t* scale
   }
   const void* dyk = kBf16 ? (const void*)dyb : dy;
   ProductArgs g{};
+  const bool big_dx = kBf16 && tiles(s.T, d, 256, 256) >= 192, big = large_tiles(s.T, d, F, kBf16);
+  int n = 0;
   if (s.T > 0) {
-    const bool big = kBf16 && tiles(s.T, d, 256, 256) >= 192;
-    const int tile = big ? 256 : 64;
-    const int n = (int)tiles(s.T, d, tile, tile);
+    const int tile = big_dx ? 256 : 64;
+    n = (int)tiles(s.T, d, tile, tile);
     g.p[0] = {w_gu, dh, nullptr, d, 2 * (int64_t)F, s.T, d, 2 * F, (d + tile - 1) / tile, 1, 0, dx, dx_in, nullptr};
-    g.p[1].first = n;
-    launch_product<T, false>(big, g, n, st);
-    if ((e = hipGetLastError())) return e;
+    if constexpr (kBf16)
+      if (big_dx || big) {
+        launch_product<T, kDx>(big_dx, g, n, st);
+        if ((e = hipGetLastError())) return e;
+        n = 0;
+      }
   }
-  const bool big = large_tiles(s.T, d, F, kBf16);
   const int tile = big ? 256 : 64;
   const Parts z = weight_parts(s, F, tile);
   const int n0 = (int)tiles(2 * (int64_t)F, d, tile, tile) * z.gu, n1 = (int)tiles(d, F, tile, tile) * z.down;
   g.kpart = z.kpart;
-  g.p[0] = {xb, dh, nullptr, d, 2 * (int64_t)F, 2 * (int64_t)F, d, (int)s.T, (d + tile - 1) / tile, z.gu, 0, dw_gu,
+  g.p[1] = {xb, dh, nullptr, d, 2 * (int64_t)F, 2 * (int64_t)F, d, (int)s.T, (d + tile - 1) / tile, z.gu, n, dw_gu,
             nullptr, (float*)part};
-  g.p[1] = {act, dyk, kBf16 ? dyl : nullptr, F, d, d, F, (int)s.T, (F + tile - 1) / tile, z.down, n0, dw_down, nullptr,
+  g.p[2] = {act, dyk, kBf16 ? dyl : nullptr, F, d, d, F, (int)s.T, (F + tile - 1) / tile, z.down, n + n0, dw_down, nullptr,
             (float*)part + (z.gu > 1 ? (size_t)z.gu * 2 * F * d : 0)};
-  launch_product<T, true>(big, g, n0 + n1, st);
+  if (n > 0) launch_product<T, kDx | kWeights>(false, g, n + n0 + n1, st);
+  else launch_product<T, kWeights>(big, g, n0 + n1, st);
   if ((e = hipGetLastError())) return e;
   if (z.down > 1) {  // (and with it perhaps z.gu: dW_down has as many parts as dW_gu or more)
     const int64_t first = z.gu > 1 ? (int64_t)F * d / 2 : 0, all = first + (int64_t)F * d / 4;
