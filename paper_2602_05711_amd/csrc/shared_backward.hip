@@ -5,11 +5,11 @@
 //   dx = dx_in + W_g^T dg + W_u^T du,  dW_g = dg x~^T, dW_u = du x~^T, dW_down = dy a^T (sums over the tokens)
 // Four launches: the checkpoint's and dy's values in the layer's type; the three products that a tile of dg, du and a
 // needs, whose sums meet in registers; dx and the weight gradients (large tiles: a launch each), the latter split over the
-// tokens into fp32 partial sums that a last launch adds in order. No atomics: the result is the same on every run. Sums are fp32. bf16 layers round a, dg and du to bf16
-// (once each, to nearest) for the matrix cores, as the forward pass rounds a; dy, fp32 from the caller, enters as two
-// bf16 values, its rounding and what that leaves (2^-17 relative), for two products more: with dy rounded as well, three
-// roundings (dy, a or dg, the result) put the weight gradients 0.0029 of their norm from the exact ones instead of
-// 0.0024, the rounding of the result alone being 0.0017.
+// tokens into fp32 partial sums that a last launch adds in order. No atomics: the result is the same on every run. Sums
+// are fp32. bf16 layers round a, dg and du to bf16 (once each, to nearest) for the matrix cores, as the forward pass rounds
+// a; dy, fp32 from the caller, enters as two bf16 values, its rounding and what that leaves (2^-17 relative), for two
+// products more: with dy rounded as well, three roundings (dy, a or dg, the result) put the weight gradients 0.0029 of
+// their norm from the exact ones instead of 0.0023, the rounding of the result alone being 0.0017.
 #include "checkpoint.hpp"
 #include "internal.hpp"
 #include "tile_gemm.hpp"
