@@ -53,10 +53,9 @@ struct HiddenArgs {
 };
 
 // TM tokens x FN features a workgroup; a wave holds 32 MJ tokens x 32 FI features of each of g, u and da (bf16: da in two
-// passes, dy's two halves). Bound by the LDS port: a stage's copies and reads take as long as its products. 16384 tokens,
-// d = d_ff = 2048: 697 us, 0.79 PFLOP/s of the 4 x 137 GFLOP. 64 x 64 tiles are for fewer than 192 of the large ones
-// (4093 tokens, d = d_ff = 512, 24.9 us) and run at L2's rate, 9.4 TB/s; 128 x 64 and 64 x 128 took 24.3 and 23.9 there
-// but fp32's 1000 tokens of d = d_ff = 520 64 us instead of 40.
+// passes, dy's two halves). Large tiles are bound by the LDS port (a stage's copies and reads take as long as its
+// products): 16384 tokens, d = d_ff = 2048, 697 us, 0.79 PFLOP/s of the 4 x 137 GFLOP. Small ones run at L2's rate: 4093
+// tokens, d = d_ff = 512, 24.9 us, 9.4 TB/s; fp32, 1000 tokens, 520, 40 us (64 us on 128 x 64).
 template <class T, int TM, int FN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC) void hidden_kernel(HiddenArgs p) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, FI = FN / WC / 32;
@@ -209,9 +208,9 @@ __device__ __forceinline__ void product_tile(const Product& p, int wg, int kpart
   }
 }
 
-// The workgroups of dx come before the weight gradients', each XCD having neighbouring tiles of both. Small tiles take
-// them in one launch, since neither fills the compute units alone: 4093 tokens, d = d_ff = 512,
-// 32.8 us instead of 15.3 and 21.8; fp32, 1000 tokens, 520, 44.5 instead of 27.8 and 24.8.
+// The workgroups of dx come before the weight gradients', each XCD having neighbouring tiles of both. Tiles below 256 x 256
+// take them in one launch, since neither fills the compute units alone: 64 x 64 tiles, 4093 tokens, d = d_ff = 512, 32.8 us
+// instead of 15.3 and 21.8; fp32, 1000 tokens, 520, 44.5 instead of 27.8 and 24.8.
 template <class T, int TM, int TN, int WR, int WC, int WHICH>
 __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args) {
   __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
@@ -260,10 +259,10 @@ Parts weight_parts(const Shape& s, int F, int tile) {
   if (s.T == 0) return {1, 1, 64};
   const int64_t tg = tiles(2 * (int64_t)F, s.d, tile, tile), td = tiles(s.d, F, tile, tile);
   const int64_t range = (s.bf16 ? 2 : 1) * s.T;
-  // 256 compute units; the small tiles' workgroups share one, four at a time
-  const int64_t slots = tile == 256 ? 256 : 1024;
+  // 256 compute units; smaller tiles' workgroups share one, two or four at a time
+  const int64_t slots = tile == 256 ? 256 : tile == 128 ? 512 : 1024;
   // ns of a value of k in a tile, of a tile's start and end, of a KiB of a part written and read
-  const double per_k = tile == 256 ? 55.0 : 12.0, fixed = 4000.0, per_kib = 0.5;
+  const double per_k = tile == 256 ? 55.0 : tile == 128 ? 16.0 : 12.0, fixed = 4000.0, per_kib = 0.5;
   Parts best{1, 1, 64};
   double least = 0;
   for (int n = 1; n <= 64; ++n) {
@@ -280,15 +279,33 @@ Parts weight_parts(const Shape& s, int F, int tile) {
   return best;
 }
 
+// Tiles. Hidden values: 256 x 128, or 128 x 64 where there are 512 of them (4096 tokens, d = d_ff = 1024: the call takes 175
+// us instead of 192; with 256 of them no difference), or 64 x 64. dx and weight gradients: 256 x 256, or 128 x 128 where dx
+// has 128 of them (2048 tokens, d = d_ff = 2048: 295 us instead of 362; 1000 tokens of 520, 40 tiles: 53 instead of 49.5),
+// or 64 x 64.
 bool large_tiles(int64_t T, int d, int F, bool bf16) { return bf16 && tiles(T, F, 256, 128) >= 192; }
+int small_tile(const Shape& s) { return s.bf16 && tiles(s.T, s.d, 128, 128) >= 128 ? 128 : 64; }
+int weight_tile(const Shape& s, int F) { return large_tiles(s.T, s.d, F, s.bf16) ? 256 : small_tile(s); }
+
+template <class T, int TM, int FN, int WR, int WC>
+void launch_hidden(const HiddenArgs& h, hipStream_t st) {
+  hipLaunchKernelGGL((hidden_kernel<T, TM, FN, WR, WC>), dim3((unsigned)tiles(h.T, h.F, TM, FN)), dim3(64 * WR * WC), 0, st,
+                     h);
+}
 
 template <class T, int WHICH>
-void launch_product(bool big, const ProductArgs& g, int workgroups, hipStream_t st) {
-  if constexpr (T::kSize == 2 && WHICH != (kDx | kWeights))
-    if (big) {
-      hipLaunchKernelGGL((product_kernel<T, 256, 256, 2, 4, WHICH>), dim3((unsigned)workgroups), dim3(512), 0, st, g);
+void launch_product(int tile, const ProductArgs& g, int workgroups, hipStream_t st) {
+  if constexpr (T::kSize == 2) {
+    if constexpr (WHICH != (kDx | kWeights))
+      if (tile == 256) {
+        hipLaunchKernelGGL((product_kernel<T, 256, 256, 2, 4, WHICH>), dim3((unsigned)workgroups), dim3(512), 0, st, g);
+        return;
+      }
+    if (tile == 128) {
+      hipLaunchKernelGGL((product_kernel<T, 128, 128, 2, 4, WHICH>), dim3((unsigned)workgroups), dim3(512), 0, st, g);
       return;
     }
+  }
   hipLaunchKernelGGL((product_kernel<T, 64, 64, 2, 2, WHICH>), dim3((unsigned)workgroups), dim3(256), 0, st, g);
 }
 
@@ -314,34 +331,30 @@ hipError_t run(const Shape& s, int F, const uint8_t* codes, const uint8_t* scale
       return e;
     }
     HiddenArgs h{xb, kBf16 ? (const void*)dyb : dy, dyl, w_gu, w_down, dh, act, s.T, d, F};
-    bool done = false;
-    if constexpr (kBf16)
-      if (large_tiles(s.T, d, F, true)) {
-        done = true;
-        hipLaunchKernelGGL((hidden_kernel<T, 256, 128, 4, 2>),
-                           dim3((unsigned)tiles(s.T, F, 256, 128)), dim3(512), 0, st, h);
-      }
-    if (!done)
-      hipLaunchKernelGGL((hidden_kernel<T, 64, 64, 2, 2>),
-                         dim3((unsigned)tiles(s.T, F, 64, 64)), dim3(256), 0, st, h);
+    if (kBf16 && large_tiles(s.T, d, F, true)) {
+      if constexpr (kBf16) launch_hidden<T, 256, 128, 4, 2>(h, st);
+    } else if (kBf16 && tiles(s.T, F, 128, 64) >= 512) {
+      if constexpr (kBf16) launch_hidden<T, 128, 64, 4, 2>(h, st);
+    } else {
+      launch_hidden<T, 64, 64, 2, 2>(h, st);
+    }
     if ((e = hipGetLastError())) return e;
   }
   const void* dyk = kBf16 ? (const void*)dyb : dy;
   ProductArgs g{};
-  const bool big_dx = kBf16 && tiles(s.T, d, 256, 256) >= 192, big = large_tiles(s.T, d, F, kBf16);
+  const int tile = weight_tile(s, F);
   int n = 0;
   if (s.T > 0) {
-    const int tile = big_dx ? 256 : 64;
-    n = (int)tiles(s.T, d, tile, tile);
-    g.p[0] = {w_gu, dh, nullptr, d, 2 * (int64_t)F, s.T, d, 2 * F, (d + tile - 1) / tile, 1, 0, dx, dx_in, nullptr};
+    const int dx_tile = kBf16 && tiles(s.T, d, 256, 256) >= 192 ? 256 : small_tile(s);
+    n = (int)tiles(s.T, d, dx_tile, dx_tile);
+    g.p[0] = {w_gu, dh, nullptr, d, 2 * (int64_t)F, s.T, d, 2 * F, (d + dx_tile - 1) / dx_tile, 1, 0, dx, dx_in, nullptr};
     if constexpr (kBf16)
-      if (big_dx || big) {
-        launch_product<T, kDx>(big_dx, g, n, st);
+      if (dx_tile == 256 || tile == 256) {
+        launch_product<T, kDx>(dx_tile, g, n, st);
         if ((e = hipGetLastError())) return e;
         n = 0;
       }
   }
-  const int tile = big ? 256 : 64;
   const Parts z = weight_parts(s, F, tile);
   const int n0 = (int)tiles(2 * (int64_t)F, d, tile, tile) * z.gu, n1 = (int)tiles(d, F, tile, tile) * z.down;
   g.kpart = z.kpart;
@@ -349,8 +362,8 @@ hipError_t run(const Shape& s, int F, const uint8_t* codes, const uint8_t* scale
             nullptr, (float*)part};
   g.p[2] = {act, dyk, kBf16 ? dyl : nullptr, F, d, d, F, (int)s.T, (F + tile - 1) / tile, z.down, n + n0, dw_down, nullptr,
             (float*)part + (z.gu > 1 ? (size_t)z.gu * 2 * F * d : 0)};
-  if (n > 0) launch_product<T, kDx | kWeights>(false, g, n + n0 + n1, st);
-  else launch_product<T, kWeights>(big, g, n0 + n1, st);
+  if (n > 0) launch_product<T, kDx | kWeights>(tile, g, n + n0 + n1, st);
+  else launch_product<T, kWeights>(tile, g, n0 + n1, st);
   if ((e = hipGetLastError())) return e;
   if (z.down > 1) {  // (and with it perhaps z.gu: dW_down has as many parts as dW_gu or more)
     const int64_t first = z.gu > 1 ? (int64_t)F * d / 2 : 0, all = first + (int64_t)F * d / 4;
@@ -365,8 +378,7 @@ hipError_t run(const Shape& s, int F, const uint8_t* codes, const uint8_t* scale
 
 size_t shared_backward_ws_bytes(const Shape& s, int F) {
   const size_t size = s.bf16 ? 2 : 4, T = (size_t)s.T;
-  const int tile = large_tiles(s.T, s.d, F, s.bf16) ? 256 : 64;
-  const Parts z = weight_parts(s, F, tile);
+  const Parts z = weight_parts(s, F, weight_tile(s, F));
   return up(T * s.d * size) + (s.bf16 ? 2 * up(T * s.d * 2) : 0) + up(T * 2 * F * size) + up(T * F * size) +
          up(((z.gu > 1 ? 2 * (size_t)z.gu : 0) + (z.down > 1 ? (size_t)z.down : 0)) * F * s.d * 4);
 }

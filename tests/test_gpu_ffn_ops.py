@@ -149,9 +149,11 @@ SHAPES = [(1, 8, 8), (1, 64, 64), (2, 72, 40), (63, 64, 128), (64, 128, 64), (65
           (257, 256, 264), (1000, 520, 520), (4093, 136, 72)]
 # bf16 only: tiles of 256 (hidden values, dx and weight gradients), whole and ragged, their rows and columns past the end
 LARGE = [(6144, 64, 1024), (6100, 72, 1032), (12288, 1024, 1024), (12200, 1000, 1032)]
+# and tiles of 128: of dx and the weight gradients, of the hidden values, of both; dx's of 256 beside the others
+MIDDLE = [(2048, 1024, 128), (2000, 1032, 264), (4093, 72, 1000), (4096, 1024, 1024), (4090, 1000, 1016), (6100, 2040, 264)]
 
 
-@pytest.mark.parametrize("T,d,f,dtype", [s + (t,) for s in SHAPES for t in TYPES] + [s + (BF16,) for s in LARGE],
+@pytest.mark.parametrize("T,d,f,dtype", [s + (t,) for s in SHAPES for t in TYPES] + [s + (BF16,) for s in LARGE + MIDDLE],
                          ids=lambda v: tid(v) if v in TYPES else str(v))
 def test_backward(T, d, f, dtype):
     print(f"[backward] T={T} d={d} d_ff={f} {dtype}", file=sys.stderr, flush=True)
