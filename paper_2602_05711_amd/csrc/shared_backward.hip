@@ -4,8 +4,8 @@
 //   dg = da u p (1 + g (1 - p)), du = da g p
 //   dx = dx_in + W_g^T dg + W_u^T du,  dW_g = dg x~^T, dW_u = du x~^T, dW_down = dy a^T (sums over the tokens)
 // Four launches: the checkpoint's and dy's values in the layer's type; the three products that a tile of dg, du and a
-// needs, whose sums meet in registers; dx and the weight gradients (large tiles: a launch each), the latter split over the
-// tokens into fp32 partial sums that a last launch adds in order. No atomics: the result is the same on every run. Sums
+// needs, whose sums meet in registers; dx and the weight gradients (large tiles: a launch each), split over the summed
+// index (the tokens; for dx of few tokens the features) into fp32 partial sums that a last launch adds in order. No atomics: the result is the same on every run. Sums
 // are fp32. bf16 layers round a, dg and du to bf16 (once each, to nearest) for the matrix cores, as the forward pass rounds
 // a; dy, fp32 from the caller, enters as two bf16 values, its rounding and what that leaves (2^-17 relative), for two
 // products more: with dy rounded as well, three roundings (dy, a or dg, the result) put the weight gradients 0.0029 of
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(64 * WR * WC) void hidden_kernel(HiddenArgs p) {
 struct Product {
   const void *a, *b, *b_lo;
   int64_t lda, ldb, M;
-  int N, K, tiles_n, parts;
+  int N, K, tiles_n, parts, kpart;
   int first;  // workgroup of the product's first tile
   void* out;
   const float* add;  // or NULL
@@ -141,12 +141,11 @@ struct Product {
 };
 struct ProductArgs {
   Product p[3];  // dx, dW_gu, dW_down
-  int kpart;
 };
 enum { kDx = 1, kWeights = 2 };  // the products of a launch
 
 template <class T, int TM, int TN, int WR, int WC, bool B_MNC>
-__device__ __forceinline__ void product_tile(const Product& p, int wg, int kpart, unsigned char* st0, unsigned char* st1) {
+__device__ __forceinline__ void product_tile(const Product& p, int wg, unsigned char* st0, unsigned char* st1) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
   typedef typename T::elem elem;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
@@ -158,7 +157,7 @@ __device__ __forceinline__ void product_tile(const Product& p, int wg, int kpart
   {
     const int64_t ka = p.lda * T::kSize, kb = (B_MNC ? p.ldb : 1) * T::kSize;
     const int64_t lo = (const char*)p.b_lo - (const char*)p.b;
-    const int64_t k0 = (int64_t)part * kpart, k1 = p.parts == 1 ? 2 * (int64_t)p.K : k0 + kpart;
+    const int64_t k0 = (int64_t)part * p.kpart, k1 = p.parts == 1 ? 2 * (int64_t)p.K : k0 + p.kpart;
     auto cut = [&](int64_t v) { return (int)(v < 0 ? 0 : v > p.K ? p.K : v); };
     const int h0 = cut(k0), h1 = cut(k1), l0 = cut(k0 - p.K), l1 = p.b_lo ? cut(k1 - p.K) : l0;
     range[0] = {h1 - h0, h0 * ka, h0 * kb};
@@ -217,30 +216,36 @@ __global__ __launch_bounds__(64 * WR * WC) void product_kernel(ProductArgs args)
   const unsigned first = WHICH == kWeights ? 0 : WHICH == kDx ? gridDim.x : (unsigned)args.p[1].first;
   if (blockIdx.x < first) {
     if constexpr (WHICH & kDx)
-      product_tile<T, TM, TN, WR, WC, false>(args.p[0], (int)xcd_contiguous(blockIdx.x, first), args.kpart, st0, st1);
+      product_tile<T, TM, TN, WR, WC, false>(args.p[0], (int)xcd_contiguous(blockIdx.x, first), st0, st1);
   } else {
     if constexpr (WHICH & kWeights) {
       const int wg = (int)(first + xcd_contiguous(blockIdx.x - first, gridDim.x - first));
-      product_tile<T, TM, TN, WR, WC, true>(args.p[wg >= args.p[2].first ? 2 : 1], wg, args.kpart, st0, st1);
+      product_tile<T, TM, TN, WR, WC, true>(args.p[wg >= args.p[2].first ? 2 : 1], wg, st0, st1);
     }
   }
 }
 
-// out = the parts' sum, in order, of one or both weight gradients (n4 quads of dW_gu, then those of dW_down): 4 to 9 us.
+// out = the parts' sum, in order (and add), of the products that have parts: n4[i] quads of p[i]. 4 to 9 us.
+struct Quads {
+  int64_t n4[3];
+};
 template <class T>
-__global__ __launch_bounds__(256) void add_parts_kernel(ProductArgs args, int64_t n4_first, int64_t n4) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (int64_t)gridDim.x * 256) {
-    const bool second = i >= n4_first;
-    const Product& p = args.p[1 + second];
-    const int64_t at = (i - (second ? n4_first : 0)) * 4, size = p.M * p.N;
+__global__ __launch_bounds__(256) void add_parts_kernel(ProductArgs args, Quads quads) {
+  const int64_t all = quads.n4[0] + quads.n4[1] + quads.n4[2];
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int64_t first = quads.n4[0], second = first + quads.n4[1];
+    const Product& p = args.p[i < first ? 0 : i < second ? 1 : 2];
+    const int64_t at = (i - (i < first ? 0 : i < second ? first : second)) * 4, size = p.M * p.N;
     float4 v = *(const float4*)(p.part + at);
-    for (int z = 1; z < p.parts; ++z) {
-      const float4 s = *(const float4*)(p.part + z * size + at);
+    auto sum = [&](const float* from) {
+      const float4 s = *(const float4*)from;
       v.x += s.x;
       v.y += s.y;
       v.z += s.z;
       v.w += s.w;
-    }
+    };
+    for (int z = 1; z < p.parts; ++z) sum(p.part + z * size + at);
+    if (p.add) sum(p.add + at);
     store4((typename T::elem*)p.out + at, v.x, v.y, v.z, v.w);
   }
 }
@@ -285,7 +290,18 @@ Parts weight_parts(const Shape& s, int F, int tile) {
 // or 64 x 64.
 bool large_tiles(int64_t T, int d, int F, bool bf16) { return bf16 && tiles(T, F, 256, 128) >= 192; }
 int small_tile(const Shape& s) { return s.bf16 && tiles(s.T, s.d, 128, 128) >= 128 ? 128 : 64; }
+int dx_tile(const Shape& s) { return s.bf16 && tiles(s.T, s.d, 256, 256) >= 192 ? 256 : small_tile(s); }
 int weight_tile(const Shape& s, int F) { return large_tiles(s.T, s.d, F, s.bf16) ? 256 : small_tile(s); }
+
+// Parts of dx's sum over the 2 F columns: few tokens have few tiles, each a long chain. As many as bring the workgroups to
+// 320, of 512 values at least. 32 tokens, d = 2048, d_ff = 4096: the call takes 100 us instead of 128, fp32 194 instead of
+// 302; with 256 tiles, 500 tokens of d = d_ff = 2048, two parts take 134 us and one 126.
+int dx_parts(const Shape& s, int F) {
+  if (s.T == 0 || dx_tile(s) != 64 || weight_tile(s, F) == 256) return 1;
+  const int64_t wanted = 320 / tiles(s.T, s.d, 64, 64), most = 2 * F / 512;
+  const int64_t parts = wanted < most ? wanted : most;
+  return parts < 1 ? 1 : parts > 16 ? 16 : (int)parts;
+}
 
 template <class T, int TM, int FN, int WR, int WC>
 void launch_hidden(const HiddenArgs& h, hipStream_t st) {
@@ -343,33 +359,37 @@ hipError_t run(const Shape& s, int F, const uint8_t* codes, const uint8_t* scale
   const void* dyk = kBf16 ? (const void*)dyb : dy;
   ProductArgs g{};
   const int tile = weight_tile(s, F);
+  const Parts z = weight_parts(s, F, tile);
+  const int zx = dx_parts(s, F);
+  float* const gu_part = (float*)part;
+  float* const down_part = gu_part + (z.gu > 1 ? (size_t)z.gu * 2 * F * d : 0);
+  float* const dx_part = down_part + (z.down > 1 ? (size_t)z.down * F * d : 0);
   int n = 0;
   if (s.T > 0) {
-    const int dx_tile = kBf16 && tiles(s.T, d, 256, 256) >= 192 ? 256 : small_tile(s);
-    n = (int)tiles(s.T, d, dx_tile, dx_tile);
-    g.p[0] = {w_gu, dh, nullptr, d, 2 * (int64_t)F, s.T, d, 2 * F, (d + dx_tile - 1) / dx_tile, 1, 0, dx, dx_in, nullptr};
+    const int dxt = dx_tile(s);
+    n = (int)tiles(s.T, d, dxt, dxt) * zx;
+    g.p[0] = {w_gu, dh, nullptr, d, 2 * (int64_t)F, s.T, d, 2 * F, (d + dxt - 1) / dxt, zx,
+              (2 * F / zx + 63) / 64 * 64, 0, dx, dx_in, dx_part};
     if constexpr (kBf16)
-      if (dx_tile == 256 || tile == 256) {
-        launch_product<T, kDx>(dx_tile, g, n, st);
+      if (dxt == 256 || tile == 256) {
+        launch_product<T, kDx>(dxt, g, n, st);
         if ((e = hipGetLastError())) return e;
         n = 0;
       }
   }
-  const Parts z = weight_parts(s, F, tile);
   const int n0 = (int)tiles(2 * (int64_t)F, d, tile, tile) * z.gu, n1 = (int)tiles(d, F, tile, tile) * z.down;
-  g.kpart = z.kpart;
-  g.p[1] = {xb, dh, nullptr, d, 2 * (int64_t)F, 2 * (int64_t)F, d, (int)s.T, (d + tile - 1) / tile, z.gu, n, dw_gu,
-            nullptr, (float*)part};
-  g.p[2] = {act, dyk, kBf16 ? dyl : nullptr, F, d, d, F, (int)s.T, (F + tile - 1) / tile, z.down, n + n0, dw_down, nullptr,
-            (float*)part + (z.gu > 1 ? (size_t)z.gu * 2 * F * d : 0)};
+  g.p[1] = {xb, dh, nullptr, d, 2 * (int64_t)F, 2 * (int64_t)F, d, (int)s.T, (d + tile - 1) / tile, z.gu, z.kpart, n,
+            dw_gu, nullptr, gu_part};
+  g.p[2] = {act, dyk, kBf16 ? dyl : nullptr, F, d, d, F, (int)s.T, (F + tile - 1) / tile, z.down, z.kpart, n + n0,
+            dw_down, nullptr, down_part};
   if (n > 0) launch_product<T, kDx | kWeights>(tile, g, n + n0 + n1, st);
   else launch_product<T, kWeights>(tile, g, n0 + n1, st);
   if ((e = hipGetLastError())) return e;
-  if (z.down > 1) {  // (and with it perhaps z.gu: dW_down has as many parts as dW_gu or more)
-    const int64_t first = z.gu > 1 ? (int64_t)F * d / 2 : 0, all = first + (int64_t)F * d / 4;
+  const int64_t quads = (int64_t)F * d / 4;
+  const Quads q{{zx > 1 ? s.T * d / 4 : 0, z.gu > 1 ? 2 * quads : 0, z.down > 1 ? quads : 0}};
+  if (const int64_t all = q.n4[0] + q.n4[1] + q.n4[2]) {
     const int64_t blocks = (all + 255) / 256;
-    hipLaunchKernelGGL(add_parts_kernel<T>, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), 0, st, g,
-                       first, all);
+    hipLaunchKernelGGL(add_parts_kernel<T>, dim3((unsigned)(blocks > 65536 ? 65536 : blocks)), dim3(256), 0, st, g, q);
   }
   return hipGetLastError();
 }
@@ -380,7 +400,8 @@ size_t shared_backward_ws_bytes(const Shape& s, int F) {
   const size_t size = s.bf16 ? 2 : 4, T = (size_t)s.T;
   const Parts z = weight_parts(s, F, weight_tile(s, F));
   return up(T * s.d * size) + (s.bf16 ? 2 * up(T * s.d * 2) : 0) + up(T * 2 * F * size) + up(T * F * size) +
-         up(((z.gu > 1 ? 2 * (size_t)z.gu : 0) + (z.down > 1 ? (size_t)z.down : 0)) * F * s.d * 4);
+         up(((z.gu > 1 ? 2 * (size_t)z.gu : 0) + (z.down > 1 ? (size_t)z.down : 0)) * F * s.d * 4 +
+            (dx_parts(s, F) > 1 ? dx_parts(s, F) * T * s.d * 4 : 0));
 }
 
 hipError_t launch_shared_backward(const Shape& s, int F, const uint8_t* codes, const uint8_t* scales,

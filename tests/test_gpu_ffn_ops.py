@@ -146,7 +146,8 @@ def _backward(i, dx_in=True, stream=None, guarded=False):
 
 
 SHAPES = [(1, 8, 8), (1, 64, 64), (2, 72, 40), (63, 64, 128), (64, 128, 64), (65, 520, 24), (100, 40, 520), (129, 2048, 8),
-          (257, 256, 264), (1000, 520, 520), (4093, 136, 72)]
+          (257, 256, 264), (1000, 520, 520), (4093, 136, 72),
+          (1, 40, 2056), (33, 72, 4104), (140, 520, 1400)]  # dx in parts
 # bf16 only: tiles of 256 (hidden values, dx and weight gradients), whole and ragged, their rows and columns past the end
 LARGE = [(6144, 64, 1024), (6100, 72, 1032), (12288, 1024, 1024), (12200, 1000, 1032)]
 # and tiles of 128: of dx and the weight gradients, of the hidden values, of both; dx's of 256 beside the others
