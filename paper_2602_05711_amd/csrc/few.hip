@@ -406,9 +406,14 @@ __global__ __launch_bounds__(kThreads) void few_finish(FewArgs p) {
         if (k != w || q) load_u(k, q + l);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (q + l + 64 * i >= chunks) xr[i] = make_uint4(0, 0, 0, 0);
+          // (both zeros: an infinity of u times a zero would not be one)
+          const bool past = q + l + 64 * i >= chunks;
+          if (past) xr[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-          for (int n = 0; n < 2; ++n) acc[n] = chunk_dot<BF16>(ur[n][i], xr[i], acc[n]);
+          for (int n = 0; n < 2; ++n) {
+            if (past) ur[n][i] = make_uint4(0, 0, 0, 0);
+            acc[n] = chunk_dot<BF16>(ur[n][i], xr[i], acc[n]);
+          }
         }
       }
 #pragma unroll

@@ -489,6 +489,30 @@ def test_few_agrees_with_the_layer():
     within(_few(t)[0], routed.to(F64), 2 * bound, "routed")
 
 
+def _same_or_within(got, want, bound, what):
+    """Infinities and NaN where the 64-bit form has them, the other values within their bound."""
+    fine = torch.isfinite(want)
+    assert _same(torch.where(fine, 0.0, got.to(F64)), torch.where(fine, 0.0, want)), what
+    within(torch.where(fine, got.to(F64), 0.0), torch.where(fine, want, 0.0), torch.where(fine, bound, 0.0), what)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=tid)
+@pytest.mark.parametrize("d", [8, 520, 1544, 2056])
+def test_few_infinity_at_the_end_of_a_u_row(d, dtype):
+    # one expert of a token's picks has an infinite last value in its u row, whose x there is 1: its h is an infinity, and
+    # so is y (GELU of it, times nonzero gates and v values of either sign). No row of a wave's loads ends with the row.
+    t = _few_inputs(2, d, 16, 16, 8, 2, 5, 0, dtype, split=False, seed=d)
+    t.x[:, -1] = 1.0
+    t.v.copy_(torch.where(t.v == 0, 1.0, t.v))
+    y, idx, _ = _few(t)
+    t.u[idx[0, 1, 3].long(), -1] = float("inf")
+    want = S.few_layer(t.x, t.kr, t.kc, t.u, t.v, None, None, t.K, "gelu", False)
+    assert torch.isinf(want[2][0]).all()
+    y, idx, _ = _few(t)
+    assert torch.equal(idx.long(), want[0])
+    _same_or_within(y, want[2], want[3], "y")
+
+
 # ------------------------------------------------------------------ graphs, streams, together
 
 def _calls(seed=0, T=40):
