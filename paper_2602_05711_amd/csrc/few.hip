@@ -12,6 +12,7 @@
 // behind which one wave counts the workgroup in, and nothing waits for another workgroup.
 #include <type_traits>
 
+#include "bf16_parts.hpp"
 #include "cand_table.hpp"
 #include "few_tile.hpp"
 #include "internal.hpp"
@@ -95,10 +96,8 @@ __global__ __launch_bounds__(256) void few_products(FewArgs p) {
       float r0 = a0, r1 = a1;
 #pragma unroll
       for (int n = 0; n < kSplit; ++n) {
-        const uint32_t h0 = bf16_rne(r0), h1 = bf16_rne(r1);
+        const uint32_t h0 = bf16_part(r0), h1 = bf16_part(r1);
         *(uint32_t*)((uint16_t*)p.act + (n * kTokens + t) * p.F + fo) = h0 | (h1 << 16);
-        r0 -= __uint_as_float(h0 << 16);
-        r1 -= __uint_as_float(h1 << 16);
       }
     } else {
       *(float2*)((float*)p.act + t * p.F + fo) = make_float2(a0, a1);

@@ -513,6 +513,27 @@ def test_few_infinity_at_the_end_of_a_u_row(d, dtype):
     _same_or_within(y, want[2], want[3], "y")
 
 
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("dtype", TYPES, ids=tid)
+def test_few_hidden_values_at_the_end_of_the_range(dtype, sign):
+    # token 0: a = 2^140, an infinity in fp32, as y is then; token 1: a = 2^128 - 2^116, which fp32 holds and which lies past
+    # bf16's largest value; token 2: neither
+    t = _few_inputs(3, 64, 16, 16, 32, 2, 4, 40, dtype, seed=11)
+    t.x[:, 60:] = 0
+    t.x[0, 60] = t.x[1, 61] = t.x[1, 62] = 1.0
+    t.w_gu[:, 60:] = 0
+    t.w_gu[0, 60], t.w_gu[40, 60] = 2.0 ** 70, sign * 2.0 ** 70
+    t.w_gu[1, 61], t.w_gu[41, 61], t.w_gu[41, 62] = 2.0 ** 64, sign * 2.0 ** 64, sign * -(2.0 ** 52)
+    t.w_down[:, 0] = torch.where(t.w_down[:, 0] == 0, 1.0, t.w_down[:, 0])
+    t.w_down[:, 1] *= 2.0 ** -10
+    want = S.few_layer(t.x, t.kr, t.kc, t.u, t.v, t.w_gu, t.w_down, t.K, "gelu", True)
+    y, idx, _ = _few(t)
+    assert torch.equal(idx.long(), want[0])
+    most = want[2].to(F32).to(F64)  # 2^140 w: an infinity
+    assert torch.isinf(most[0]).all() and torch.isfinite(most[1:]).all()
+    _same_or_within(y, most, want[3] + 2 * S.U32 * want[2].abs(), "y")
+
+
 # ------------------------------------------------------------------ graphs, streams, together
 
 def _calls(seed=0, T=40):
