@@ -190,10 +190,14 @@ __device__ __forceinline__ void half_best(const float* __restrict__ logits, int 
   }
 }
 
+// Tiles of a down projection: the hidden values' leading parts, and (bf16) their other parts.
+template <bool BF16>
+constexpr int kDownTiles = BF16 ? 2 : 1;
+
 constexpr int kCells = 288;  // at least the 280 cells of K = 64, and what the last wave's share runs past them
 struct FinishShared {
   union {
-    f32x4 tiles[kWaves][1][64];
+    f32x4 tiles[kWaves * kDownTiles<true>][64];
     struct {
       uint64_t cand[2][64], best[2][64];
       uint4 cell[kCells];  // score (order map of the double), id
@@ -256,25 +260,31 @@ __device__ __forceinline__ void add_finished(const FewArgs& p, const FinishShare
 
 template <bool BF16>
 __device__ __forceinline__ void down_group(const FewArgs& p, FinishShared& sh, int g) {
-  constexpr int E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4, NB = BF16 ? kSplit : 1;
+  constexpr int E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4, NB = BF16 ? kSplit : 1, NACC = kDownTiles<BF16>;
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, t = l & 15;
   const int col = g * 16 + t < p.d ? g * 16 + t : p.d - 1;
   const uint4* const row[1] = {(const uint4*)((const char*)p.w_down + (int64_t)col * p.F * kSize)};
   // (the hidden values of lanes past the last token are that token's again)
   auto act = [&](int n) { return (const uint4*)((const char*)p.act + (int64_t)(n * kTokens + t) * p.F * kSize); };
-  f32x4 acc[1];
+  f32x4 acc[NACC];
   if constexpr (BF16) {
     const uint4* const tok[NB] = {act(0), act(1), act(2)};
-    wave_tile<BF16, 1, NB, 1, kWaves>(row, tok, p.F / E, w, acc);
+    wave_tile<BF16, 1, NB, NACC, kWaves>(row, tok, p.F / E, w, acc);
   } else {
     const uint4* const tok[NB] = {act(0)};
-    wave_tile<BF16, 1, NB, 1, kWaves>(row, tok, p.F / E, w, acc);
+    wave_tile<BF16, 1, NB, NACC, kWaves>(row, tok, p.F / E, w, acc);
   }
-  add_tiles(acc, sh.tiles, w, l);
+  add_tiles(acc, *(f32x4(*)[kWaves][NACC][64])sh.tiles, w, l);
+  // An infinite weight: the leading parts' sum is the infinity, or NaN where a is zero; of the others' products one may be
+  // an infinity of the other sign, or zero times it.
+  if constexpr (BF16)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if ((__float_as_uint(acc[0][q]) & 0x7F800000u) != 0x7F800000u) acc[0][q] += acc[1][q];
   const int r = g / p.range_groups;
   if (w == 0) {
     // through LDS, so that a store covers whole lines: token by token, sixteen columns each
-    float2* const turned = (float2*)sh.tiles[0][0];
+    float2* const turned = (float2*)sh.tiles;
     turned[t * 8 + 2 * (l >> 4)] = make_float2(acc[0][0], acc[0][1]);
     turned[t * 8 + 2 * (l >> 4) + 1] = make_float2(acc[0][2], acc[0][3]);
     wave_lds_sync();

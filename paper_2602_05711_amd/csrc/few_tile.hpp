@@ -41,9 +41,10 @@ struct Chunk<false> {
 // (128 bytes of every row), a wave takes U neighbouring ones at a time and has their weights in flight together, U as
 // large as leaves every wave some.
 // row: this lane's weight row in each of the row blocks, of `chunks` times 16 bytes; tok: this lane's token row in each of
-// the operands (lanes past the last token have that one's: their columns of the tile are not used), which have tiles of
-// their own (NACC = NB: tile b NB + n) or are summed (NACC = 1). The loads are unconditional; chunks past the row's end
-// read its last one and become zeros, the token's too (its infinity times a weight's zero would not be one).
+// the operands (lanes past the last token have that one's: their columns of the tile are not used). Operand n has tile
+// b NACC + n of row block b; those past the last of the NACC tiles are summed in that one. The loads are unconditional;
+// chunks past the row's end read its last one and become zeros, the token's too (its infinity times a weight's zero would
+// not be one).
 template <bool BF16, int RB, int NB, int NACC, int W, int U>
 __device__ __forceinline__ void wave_steps(const uint4* const (&row)[RB], const uint4* const (&tok)[NB], int chunks, int w,
                                            f32x4 (&acc)[RB * NACC]) {
@@ -79,7 +80,7 @@ __device__ __forceinline__ void wave_steps(const uint4* const (&row)[RB], const 
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
 #pragma unroll
-          for (int n = 0; n < NB; ++n) Chunk<BF16>::mma(acc[r * NACC + (NACC == NB ? n : 0)], a[i][e][r], b[e][n]);
+          for (int n = 0; n < NB; ++n) Chunk<BF16>::mma(acc[r * NACC + (n < NACC ? n : NACC - 1)], a[i][e][r], b[e][n]);
         }
       }
     }

@@ -534,6 +534,22 @@ def test_few_hidden_values_at_the_end_of_the_range(dtype, sign):
     _same_or_within(y, most, want[3] + 2 * S.U32 * want[2].abs(), "y")
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=tid)
+@pytest.mark.parametrize("T,d,f", [(1, 64, 8), (5, 136, 136), (16, 64, 1032)])
+def test_few_infinite_weights_of_the_down_projection(T, d, f, dtype):
+    # columns 3 and 20 of the output have one infinite weight each, column 33 two of either sign: infinities of the hidden
+    # values' signs, and NaN where the two meet; a hidden value of zero gives NaN too
+    t = _few_inputs(T, d, 16, 16, 32, 2, 4, f, dtype, seed=f)
+    t.w_down[3, f - 1], t.w_down[20, 0] = float("inf"), -float("inf")
+    t.w_down[33, 1], t.w_down[33, f - 2] = float("inf"), -float("inf")
+    t.w_gu[f] = 0  # feature 0's hidden value
+    want = S.few_layer(t.x, t.kr, t.kc, t.u, t.v, t.w_gu, t.w_down, t.K, "gelu", True)
+    assert torch.isinf(want[2][:, 3]).all() and torch.isnan(want[2][:, 20]).all() and not torch.isfinite(want[2][:, 33]).any()
+    y, idx, _ = _few(t)
+    assert torch.equal(idx.long(), want[0])
+    _same_or_within(y, want[2], want[3], "y")
+
+
 # ------------------------------------------------------------------ graphs, streams, together
 
 def _calls(seed=0, T=40):
