@@ -10,6 +10,7 @@
 // a; dy, fp32 from the caller, enters as two bf16 values, its rounding and what that leaves (2^-17 relative), for two
 // products more: with dy rounded as well, three roundings (dy, a or dg, the result) put the weight gradients 0.0029 of
 // their norm from the exact ones instead of 0.0023, the rounding of the result alone being 0.0017.
+#include "bf16_parts.hpp"
 #include "checkpoint.hpp"
 #include "internal.hpp"
 #include "tile_gemm.hpp"
@@ -17,9 +18,9 @@
 namespace omnimoe {
 namespace {
 
-// The bf16 operands: the checkpoint's values to x, and dy to hi = bf16(dy) and lo = bf16(dy - hi), eight of each a thread.
-// Where hi is not finite, lo is zero. Bound by memory: [16384, 2048] 59 us, 6.3 TB/s. A pass of its own, because the tiles' operands
-// are copied to LDS without passing registers.
+// The bf16 operands: the checkpoint's values to x, and dy to hi = bf16(dy) and lo = bf16(dy - hi), eight of each a thread
+// (bf16_part: hi is finite where dy is, lo zero where it is not). Bound by memory: [16384, 2048] 59 us, 6.3 TB/s. A pass
+// of its own, because the tiles' operands are copied to LDS without passing registers.
 __global__ __launch_bounds__(256) void operands_kernel(const uint8_t* __restrict__ codes,
                                                        const uint8_t* __restrict__ scales, const float* __restrict__ dy,
                                                        uint16_t* __restrict__ x, uint16_t* __restrict__ hi,
@@ -31,14 +32,13 @@ __global__ __launch_bounds__(256) void operands_kernel(const uint8_t* __restrict
     const int64_t t = i / q8;
     const int c = (int)(i - t * q8);
     checkpoint_load8<true>(codes + i * 8, scales[t * nblk + (c >> 2)], x, i * 8);
-    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     uint32_t h[4], l[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      h[e] = (uint32_t)bf16_rne(v[2 * e]) | ((uint32_t)bf16_rne(v[2 * e + 1]) << 16);
-      const float r0 = v[2 * e] - bf16_lo(h[e]), r1 = v[2 * e + 1] - bf16_hi(h[e]);
-      l[e] = ((h[e] & 0x7F80u) == 0x7F80u ? 0u : (uint32_t)bf16_rne(r0)) |
-             ((h[e] & 0x7F800000u) == 0x7F800000u ? 0u : (uint32_t)bf16_rne(r1) << 16);
+      h[e] = bf16_part(v[2 * e]);
+      h[e] |= bf16_part(v[2 * e + 1]) << 16;
+      l[e] = (uint32_t)bf16_rne(v[2 * e]) | ((uint32_t)bf16_rne(v[2 * e + 1]) << 16);
     }
     *(uint4*)(hi + i * 8) = make_uint4(h[0], h[1], h[2], h[3]);
     *(uint4*)(lo + i * 8) = make_uint4(l[0], l[1], l[2], l[3]);

@@ -197,6 +197,20 @@ def test_backward_matches_differences():
         assert abs(slope - mine) <= float((bound[k] * to.abs()).sum()) + 1e-6 * (1 + abs(slope) + abs(up))
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=tid)
+def test_backward_of_dy_past_the_largest_bf16(dtype):
+    # fp32's largest value and one a little below it round to infinity in bf16; as two bf16 values they are kept to 2^-17
+    i = _backward_inputs(3, 64, 72, dtype, seed=17)
+    i.w_gu *= 2.0 ** -5
+    i.w_down[5] *= 2.0 ** -20
+    i.w_down[7] *= 2.0 ** -20
+    i.dy[0, 5], i.dy[1, 7] = torch.finfo(F32).max, -(2.0 ** 128 - 2.0 ** 118)
+    want, bound = S.mlp_backward_bounds(S.dequantise(i.codes, i.scales), i.w_gu.to(F64), i.w_down.to(F64), i.dy.to(F64),
+                                        i.dx_in.to(F64), dtype)
+    for g, w, b, name in zip(_backward(i), want, bound, ("dx", "dw_gu", "dw_down")):
+        within(g, w, b, name)
+
+
 def test_backward_of_no_tokens():
     for dtype in TYPES:
         i = _backward_inputs(0, 64, 40, dtype)
