@@ -48,6 +48,7 @@ class OmnimoeLayerDesc(ctypes.Structure):
 class OmnimoeAdapters(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int32), ("rank", ctypes.c_int32), ("a_gu", ctypes.c_void_p), ("b_gu", ctypes.c_void_p),
                 ("a_down", ctypes.c_void_p), ("b_down", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+    tensors = fits = None  # make_adapters' tables and what they fit
 
 
 class OmnimoeError(RuntimeError):
@@ -497,7 +498,10 @@ def omnimoe_shared_mlp_adapters(desc, d_ff, adapters, x, w_gu, w_down, ids, y_in
                         stream)
     T, d, dt, f32 = desc.T, desc.d, _layer_dtype(desc), torch.float32
     tables = ()
-    if adapters.fits != (x.get_device(), d, d_ff, dt):
+    if adapters.tensors is None:
+        if adapters.n > 0:
+            raise ValueError("omnimoe_shared_mlp_adapters: a descriptor of slots comes from make_adapters, which keeps its tables")
+    elif adapters.fits != (x.get_device(), d, d_ff, dt):
         tables = _adapter_tensors(adapters.n, adapters.rank, d, d_ff, dt, adapters.tensors)
     _ffn_call("omnimoe_shared_mlp_adapters", desc, (
         ("x", x, dt, T * d), ("w_gu", w_gu, dt, 2 * d_ff * d), ("w_down", w_down, dt, d * d_ff),

@@ -167,6 +167,21 @@ def test_binding_refuses_before_the_call():
         P.omnimoe_layer_few_workspace_size(_desc(T=17), 64)
 
 
+def _bound_adapters_call(ad, T=4, d=64, f=72):
+    x, w_gu, w_down = torch.zeros(T, d), torch.zeros(2 * f, d), torch.zeros(d, f)
+    P.omnimoe_shared_mlp_adapters(_desc(T=T, d=d, dtype=torch.float32), f, ad, x, w_gu, w_down,
+                                  torch.zeros(T, dtype=torch.int32), None, torch.zeros(T, d),
+                                  ws=torch.zeros(256, dtype=torch.uint8))
+
+
+def test_binding_of_a_descriptor_made_directly():
+    # its tables are not known to the binding, so that it takes one without slots only
+    with pytest.raises(ValueError, match="make_adapters"):
+        _bound_adapters_call(_adapters())
+    with pytest.raises(ValueError, match="not on a GPU"):  # the next refusal: these tensors are not
+        _bound_adapters_call(B.OmnimoeAdapters(n=0, rank=8))
+
+
 def test_every_e4m3_value_is_its_own_checkpoint():
     # all finite codes, times powers of two from the least to the largest scale
     byte = torch.tensor([b for b in range(256) if b & 127 != 127], dtype=torch.uint8)

@@ -330,6 +330,16 @@ def test_adapters_of_no_slots_and_without_y_in(T, dtype):
     assert torch.equal(out, _adapt(t))
 
 
+@pytest.mark.parametrize("T", [20, 200])
+def test_adapters_of_a_descriptor_without_slots(T):
+    # made directly, as a program without adapters has it
+    t = _adapter_inputs(T, 72, 104, 4, 8, BF16, _ids("none", T, 4), seed=T)
+    y = torch.empty((T, 72), dtype=BF16, device="cuda")
+    P.omnimoe_shared_mlp_adapters(t.D, t.f, P.OmnimoeAdapters(n=0, rank=8), t.x, t.w_gu, t.w_down, t.ids, t.y_in, y)
+    torch.cuda.synchronize()
+    assert torch.equal(y, _adapt(t))
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=tid)
 @pytest.mark.parametrize("T", [20, 64, 65, 200, 700])
 def test_a_slots_values_stay_with_its_tokens(T, dtype):
