@@ -48,7 +48,7 @@ class OmnimoeLayerDesc(ctypes.Structure):
 class OmnimoeAdapters(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int32), ("rank", ctypes.c_int32), ("a_gu", ctypes.c_void_p), ("b_gu", ctypes.c_void_p),
                 ("a_down", ctypes.c_void_p), ("b_down", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
-    tensors = fits = None  # make_adapters' tables and what they fit
+    tensors = fits = made = None  # make_adapters' tables, what they fit, their (n, rank)
 
 
 class OmnimoeError(RuntimeError):
@@ -478,6 +478,7 @@ def make_adapters(a_gu, b_gu, a_down, b_down, scale=None) -> OmnimoeAdapters:
     a = OmnimoeAdapters(n=n, rank=rank, a_gu=a_gu.data_ptr(), b_gu=b_gu.data_ptr(), a_down=a_down.data_ptr(),
                         b_down=b_down.data_ptr(), scale=None if scale is None else scale.data_ptr())
     a.tensors = (a_gu, b_gu, a_down, b_down, scale)
+    a.made = (n, rank)
     # what a call's tables must be, where they are: checked here once, since the tables outlive many calls
     at, d = a_gu.get_device(), b_down.shape[1]
     a.fits = (at, d, d_ff, a_gu.dtype)
@@ -501,6 +502,9 @@ def omnimoe_shared_mlp_adapters(desc, d_ff, adapters, x, w_gu, w_down, ids, y_in
     if adapters.tensors is None:
         if adapters.n > 0:
             raise ValueError("omnimoe_shared_mlp_adapters: a descriptor of slots comes from make_adapters, which keeps its tables")
+    elif adapters.n > adapters.made[0] or adapters.rank != adapters.made[1]:
+        raise ValueError(f"omnimoe_shared_mlp_adapters: {adapters.n} slots of rank {adapters.rank} in tables made for "
+                         "{} of rank {}".format(*adapters.made))
     elif adapters.fits != (x.get_device(), d, d_ff, dt):
         tables = _adapter_tensors(adapters.n, adapters.rank, d, d_ff, dt, adapters.tensors)
     _ffn_call("omnimoe_shared_mlp_adapters", desc, (

@@ -182,6 +182,20 @@ def test_binding_of_a_descriptor_made_directly():
         _bound_adapters_call(B.OmnimoeAdapters(n=0, rank=8))
 
 
+def test_binding_of_a_descriptor_changed_after_its_tables_were_checked():
+    f, n, r, d = 72, 4, 8, 64
+    tables = [torch.zeros(n, 2 * r, d), torch.zeros(n, 2 * f, r), torch.zeros(n, r, f), torch.zeros(n, d, r)]
+    for name, value in (("n", n + 1), ("rank", 2 * r), ("rank", r // 2)):
+        ad = P.make_adapters(*tables)
+        setattr(ad, name, value)
+        with pytest.raises(ValueError, match="tables made for 4 of rank 8"):
+            _bound_adapters_call(ad)
+    ad = P.make_adapters(*tables)
+    ad.n = n - 1  # fewer slots: the first ones
+    with pytest.raises(ValueError, match="not on a GPU"):
+        _bound_adapters_call(ad)
+
+
 def test_every_e4m3_value_is_its_own_checkpoint():
     # all finite codes, times powers of two from the least to the largest scale
     byte = torch.tensor([b for b in range(256) if b & 127 != 127], dtype=torch.uint8)
