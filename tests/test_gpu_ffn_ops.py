@@ -361,6 +361,27 @@ def test_a_slots_values_stay_with_its_tokens(T, dtype):
     assert torch.equal(got[1:], clean[1:]) and torch.isnan(got[0].float()).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=tid)
+@pytest.mark.parametrize("T", [20, 64, 65, 200, 700])
+@pytest.mark.parametrize("table", range(4))
+def test_a_slots_bad_values_reach_its_tokens(T, dtype, table):
+    # an infinity in one row of one of slot 3's tables: every value that it enters is not finite. (The row of A: a rank-wide
+    # value, and with it a column of B, all of the token's outputs. The row of B: a gate value, which silu and the down
+    # projection spread, or one output.)
+    t = _adapter_inputs(T, 96, 72, 6, 16, dtype, _ids("own", T, 5), seed=T)
+    clean = _adapt(t)
+    bad = [v.clone() for v in t.tables]
+    bad[table][3, 7] = float("inf")
+    got, mine = _adapt(t, bad), t.ids == 3
+    assert mine.any() and torch.equal(got[~mine], clean[~mine])
+    if table == 3:
+        assert not torch.isfinite(got[mine][:, 7]).any()
+        got[mine, 7] = clean[mine, 7]
+        assert torch.equal(got, clean)
+    else:
+        assert not torch.isfinite(got[mine]).any()
+
+
 def test_adapters_in_place_fp32_and_far_slots():
     t = _adapter_inputs(90, 64, 72, 5, 8, F32, _ids("mixed", 90, 5))
     want = _adapt(t)
