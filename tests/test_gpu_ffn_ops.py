@@ -672,6 +672,47 @@ def test_two_graphs_share_a_workspace():
             assert all(torch.equal(x, y) for x, y in zip(ao, want)), name
 
 
+def test_graphs_of_different_calls_share_a_workspace():
+    # one workspace under the graphs of all operators, each of two sets of inputs, replayed in turn and in the other order
+    ws = torch.zeros(1 << 22, dtype=torch.uint8, device="cuda")
+    calls = []
+    for T, seed in ((40, 0), (97, 7)):
+        b = _backward_inputs(T, 128, 72, BF16, seed)
+        assert P.omnimoe_shared_mlp_backward_workspace_size(b.D, b.f) <= ws.numel()
+        outs = [torch.zeros((T, 128), dtype=BF16, device="cuda"), torch.zeros_like(b.w_gu), torch.zeros_like(b.w_down)]
+        calls.append((f"backward {T}", outs, lambda b=b, o=outs: P.omnimoe_shared_mlp_backward(
+            b.D, b.f, b.codes, b.scales, b.w_gu, b.w_down, b.dy, b.dx_in, *o, ws=ws)))
+        a = _adapter_inputs(T, 64, 72, 5, 16, BF16, _ids("mixed", T, 5), seed + 1)
+        ad = P.make_adapters(*a.tables)
+        assert P.omnimoe_shared_mlp_adapters_workspace_size(a.D, a.f, ad) <= ws.numel()
+        outs = [torch.zeros((T, 64), dtype=BF16, device="cuda")]
+        calls.append((f"adapters {T}", outs, lambda a=a, ad=ad, o=outs: P.omnimoe_shared_mlp_adapters(
+            a.D, a.f, ad, a.x, a.w_gu, a.w_down, a.ids, a.y_in, *o, ws=ws)))
+        f = _few_inputs(3 + seed, 256, 64, 64, 128, 4, 16, 136, BF16, seed=seed + 2)
+        assert P.omnimoe_layer_few_workspace_size(f.D, f.f) <= ws.numel()
+        outs = [torch.zeros((f.T, 256), dtype=F32, device="cuda"), torch.zeros((f.T, 4, 16), dtype=torch.int32, device="cuda")]
+        calls.append((f"few {f.T}", outs, lambda f=f, o=outs: P.omnimoe_layer_forward_few(
+            f.D, f.f, f.x, f.kr, f.kc, f.u, f.v, f.w_gu, f.w_down, *o, None, ws=ws)))
+    want, graphs, s = [], [], torch.cuda.Stream()
+    for _, outs, call in calls:
+        call()
+        torch.cuda.synchronize()
+        want.append([o.clone() for o in outs])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            call()
+        graphs.append(graph)
+    for order in (graphs, graphs[::-1], graphs[::2] + graphs[1::2]):
+        for _, outs, _ in calls:
+            for o in outs:
+                o.zero_()
+        for graph in order:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (name, outs, _), w in zip(calls, want):
+            assert all(torch.equal(x, y) for x, y in zip(outs, w)), name
+
+
 def test_calls_on_two_streams():
     one, two = _calls(0), _calls(7)
     for _, call, _, _ in one + two:
