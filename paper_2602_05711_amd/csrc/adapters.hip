@@ -436,8 +436,9 @@ __global__ __launch_bounds__(64 * WR * WC) void adapter_tile_kernel(AdapterArgs 
 
 size_t up(size_t v) { return (v + 255) & ~(size_t)255; }
 
-// Tokens of one pass: their rows of x lie within 4 GiB of each other (8192 values at most).
+// Tokens of one pass: its tiles' offsets count over all their rows of x.
 constexpr int64_t kPassTokens = 65536;
+static_assert(kPassTokens * kMaxWidth * 2 < kTileReach && kPassTokens * kMaxWidthF32 * 4 < kTileReach, "rows of x");
 
 struct Layout {
   size_t raw, low, lowt, act, order, ident, runs, bytes;

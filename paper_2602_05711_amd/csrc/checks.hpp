@@ -17,7 +17,7 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline omnimoe_status check_desc(const omnimoe_layer_desc* d, Shape* s) {
   if (!d) return OMNIMOE_ERR_INVALID_ARG;
   if (d->T < 0 || d->T > (1LL << 23)) return OMNIMOE_ERR_INVALID_ARG;
-  if (d->d < 8 || d->d > 8192 || d->d % 8) return OMNIMOE_ERR_INVALID_ARG;
+  if (d->d < 8 || d->d > kMaxWidth || d->d % 8) return OMNIMOE_ERR_INVALID_ARG;
   if (d->n_rows < 1 || d->n_rows > 4096 || d->n_cols < 1 || d->n_cols > 4096)
     return OMNIMOE_ERR_INVALID_ARG;
   if (d->d_key < 8 || d->d_key % 8) return OMNIMOE_ERR_INVALID_ARG;
@@ -33,7 +33,7 @@ inline omnimoe_status check_desc(const omnimoe_layer_desc* d, Shape* s) {
   if (d->K > N) return OMNIMOE_ERR_INVALID_ARG;
   if (d->K > 4096) return OMNIMOE_ERR_UNSUPPORTED;
   if (d->dtype != OMNIMOE_F32 && d->dtype != OMNIMOE_BF16) return OMNIMOE_ERR_INVALID_ARG;
-  if (d->dtype == OMNIMOE_F32 && d->d > 4096) return OMNIMOE_ERR_UNSUPPORTED;
+  if (d->dtype == OMNIMOE_F32 && d->d > kMaxWidthF32) return OMNIMOE_ERR_UNSUPPORTED;
   if (d->act != OMNIMOE_ACT_GELU && d->act != OMNIMOE_ACT_SILU) return OMNIMOE_ERR_INVALID_ARG;
   if (d->group_size < 1) return OMNIMOE_ERR_INVALID_ARG;
   const int64_t rows = d->T * d->H;
@@ -72,6 +72,6 @@ inline omnimoe_status check_opt(const void* p) {
 inline omnimoe_status hip_status(hipError_t e) { return e == hipSuccess ? OMNIMOE_OK : OMNIMOE_ERR_HIP; }
 
 // Widths of the shared branch: rows of whole 16-byte chunks.
-inline bool valid_d_ff(int32_t d_ff) { return d_ff >= 8 && d_ff <= 65536 && d_ff % 8 == 0; }
+inline bool valid_d_ff(int32_t d_ff) { return d_ff >= 8 && d_ff <= kMaxFeatures && d_ff % 8 == 0; }
 
 }  // namespace omnimoe

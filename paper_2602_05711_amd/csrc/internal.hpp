@@ -6,6 +6,9 @@
 
 namespace omnimoe {
 
+// Largest sizes that the host API lets through: d of bf16 and of fp32 layers, and the shared branch's d_ff.
+constexpr int kMaxWidth = 8192, kMaxWidthF32 = 4096, kMaxFeatures = 65536;
+
 // Derived sizes of one layer call (validated by the host API before any launch).
 struct Shape {
   int64_t T;

@@ -22,6 +22,7 @@
 #pragma once
 
 #include "device_common.hpp"
+#include "internal.hpp"
 
 namespace omnimoe {
 
@@ -55,6 +56,10 @@ __device__ __forceinline__ void tile_mma(tg_f32x16& acc, tg_f32x4 a, tg_f32x4 b)
   for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], acc, 0, 0, 0);
 }
 
+constexpr int64_t kTileReach = int64_t(1) << 32;  // bytes that a tile's 32-bit offsets count
+static_assert(256LL * 2 * kMaxFeatures * 4 < kTileReach, "256 rows");
+static_assert(2LL * kMaxFeatures * kMaxWidth * 2 < kTileReach && 2LL * kMaxFeatures * kMaxWidthF32 * 4 < kTileReach, "w_gu");
+
 // One operand's R rows of a stage, copied by NW waves.
 template <class T, int R, bool MNC, int NW>
 struct TileOperand {
@@ -66,8 +71,9 @@ struct TileOperand {
   static constexpr int kRowChunks = MNC ? R / kPer : 8;      // 16-byte chunks per LDS row
   typedef typename T::elem elem;
 
-  // Copy i of stage kt reads from base + kt step + off[i] (bytes; base and step are the same on every lane, and a tile's
-  // rows lie within 4 GiB of its first: 256 rows, or 64 of the summed index, of at most 2^17 values).
+  // Copy i of stage kt reads from base + kt step + off[i] (bytes; base and step are the same on every lane). off is less
+  // than 4 GiB: it reaches over 256 rows, or 64 of the summed index, of at most 2 kMaxFeatures values, over all of w_gu (up
+  // rows beside gate rows) or w_down, or over the rows of x of an adapters' pass (a static_assert each).
   const char* base;
   int64_t step;
   uint32_t off[kCopies];
