@@ -22,11 +22,14 @@ namespace {
 
 constexpr int kTokens = 16;
 constexpr int kSplit = 3;  // bf16 values of a hidden value
-// The columns are divided into at most 64 ranges. The workgroups of the down projection count themselves into their range,
-// whose last one counts it in for every token; a head's counts in for each range of its token. With a single range a
-// workgroup of the down projection that came last would have all the tokens to add: 16 tokens, d = d_ff = 2048, back to
-// back, 52.5 us a call instead of 27.7 (ranges of 256 columns 29.4, of 64 27.4).
-constexpr int kRanges = 64, kRangeLine = 16;                         // (counters of different ranges lie 64 bytes apart)
+// The columns are divided into at most 64 ranges of 128. The workgroups of the down projection (eight to a range, sixteen
+// columns each) count themselves into their range, whose last one counts it in for every token; a head's counts in for
+// each range of its token. With a single range a workgroup of the down projection that came last would have all the tokens
+// to add: 16 tokens, d = d_ff = 2048, back to back, 52.5 us a call instead of 27.7 (ranges of 256 columns 29.4, of 64 27.4).
+// Without a shared branch there is one range, all the columns.
+constexpr int kRanges = 64, kRangeGroups = 8;
+static_assert(kRanges * kRangeGroups * 16 >= kMaxWidth, "a range for every column");
+constexpr int kRangeLine = 16;                                       // (counters of different ranges lie 64 bytes apart)
 constexpr int kCounts = kTokens * kRanges + kRanges * kRangeLine;    // the tokens' by ranges, then the ranges'
 
 struct FewArgs {
@@ -39,13 +42,11 @@ struct FewArgs {
   float* part;    // [T H, d] the heads' sums
   float* shared;  // [down_groups, T, 16] the down projection
   int* count;     // [kCounts]
-  int64_t N;
   int T, d, F, H, K, act_kind, dk, col0;
   int n[2], npad[2];
   int key_groups[2];  // workgroups of sixteen sub-keys per half
   int down_groups;    // workgroups of sixteen output columns
   int ranges, span;   // of the columns, and the columns of one
-  int range_groups;   // workgroups of one
 };
 
 // Sixteen sub-keys or eight features (their gate and up rows) a workgroup, its four waves each a quarter of k. Bound by
@@ -281,7 +282,7 @@ __device__ __forceinline__ void down_group(const FewArgs& p, FinishShared& sh, i
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if ((__float_as_uint(acc[0][q]) & 0x7F800000u) != 0x7F800000u) acc[0][q] += acc[1][q];
-  const int r = g / p.range_groups;
+  const int r = g / kRangeGroups;
   if (w == 0) {
     // through LDS, so that a store covers whole lines: token by token, sixteen columns each
     float2* const turned = (float2*)sh.tiles;
@@ -295,9 +296,9 @@ __device__ __forceinline__ void down_group(const FewArgs& p, FinishShared& sh, i
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the wave's stores are past L2
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup");
-    const int rest = p.down_groups - r * p.range_groups;
+    const int rest = p.down_groups - r * kRangeGroups;
     int last = 0;
-    if (l == 0) last = count_in(p.count + kTokens * kRanges + r * kRangeLine) == min(rest, p.range_groups) - 1;
+    if (l == 0) last = count_in(p.count + kTokens * kRanges + r * kRangeLine) == min(rest, kRangeGroups) - 1;
     last = readlane_i32(last, 0);
     list_finished(p, sh, last && l < p.T, l, r);
   }
@@ -487,7 +488,6 @@ hipError_t launch_few(const Shape& s, int F, const void* x, const void* keys_row
   p.y = y;
   p.idx = idx;
   p.gates = gates;
-  p.N = s.N;
   p.T = (int)s.T;
   p.d = s.d;
   p.F = F;
@@ -503,10 +503,8 @@ hipError_t launch_few(const Shape& s, int F, const void* x, const void* keys_row
     p.key_groups[i] = (int)(((int64_t)s.H * p.n[i] + 15) / 16);
   }
   p.down_groups = F ? (s.d + 15) / 16 : 0;
-  p.range_groups = (p.down_groups + kRanges - 1) / kRanges;
-  if (p.range_groups < 8) p.range_groups = 8;
-  p.ranges = F ? (p.down_groups + p.range_groups - 1) / p.range_groups : 1;
-  p.span = F ? 16 * p.range_groups : s.d;
+  p.ranges = F ? (p.down_groups + kRangeGroups - 1) / kRangeGroups : 1;
+  p.span = F ? 16 * kRangeGroups : s.d;
   char* w = (char*)ws;
   p.count = (int*)w;
   w += kCounts * 4;
