@@ -595,7 +595,44 @@ def test_few_infinite_weights_of_the_down_projection(T, d, f, dtype):
     _same_or_within(y, want[2], want[3], "y")
 
 
+@pytest.mark.parametrize("K", [4, 16, 64])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), float("nan")], ids=["inf", "-inf", "nan"])
+@pytest.mark.parametrize("dtype", TYPES, ids=tid)
+def test_few_selects_as_the_layer_where_keys_are_not_finite(dtype, value, K):
+    t = _few_inputs(4, 256, 64, 64, 128, 2, K, 0, dtype, seed=6)
+    t.x[:, 0] = t.x[:, 128] = 1.0
+    t.kr[:, 3::7, 0] = value
+    t.kc[:, 5::9, 0] = value
+    y, idx, g = _few(t)
+    ly, li, lg = torch.empty_like(y), torch.empty_like(idx), torch.empty_like(g)
+    P.omnimoe_layer_forward(t.D, t.x, t.kr, t.kc, t.u, t.v, ly, li, lg)
+    torch.cuda.synchronize()
+    assert torch.equal(idx, li)
+    # both within K + 16 units of the exact gates; NaN in the same places
+    assert torch.equal(torch.isnan(g), torch.isnan(lg)) and torch.equal(torch.isnan(y), torch.isnan(ly))
+    assert (torch.nan_to_num(g - lg).abs() <= 2 * (K + 16) * S.U32 * torch.nan_to_num(lg)).all()
+
+
 # ------------------------------------------------------------------ graphs, streams, together
+
+
+@pytest.mark.parametrize("dtype,d,f", [(BF16, 8, 65536), (BF16, 8192, 72), (F32, 8, 65536), (F32, 4096, 72)],
+                         ids=lambda v: tid(v) if v in TYPES else str(v))
+def test_largest_widths(dtype, d, f):
+    i = _backward_inputs(3, d, f, dtype, seed=3)
+    want, bound = S.mlp_backward_bounds(S.dequantise(i.codes, i.scales), i.w_gu.to(F64), i.w_down.to(F64), i.dy.to(F64),
+                                        i.dx_in.to(F64), dtype)
+    for g, w, b, name in zip(_backward(i), want, bound, ("dx", "dw_gu", "dw_down")):
+        within(g, w, b, name)
+    for T in (3, 40, 70):
+        t = _adapter_inputs(T, d, f, 3, 16, dtype, _ids("mixed", T, 3), seed=4)
+        y, bound = _adapt_reference(t)
+        within(_adapt(t), y, bound, f"adapters, {T} tokens")
+    t = _few_inputs(3, d, 16, 16, 8, 2, 5, f, dtype, split=False, seed=5)
+    want = S.few_layer(t.x, t.kr, t.kc, t.u, t.v, t.w_gu, t.w_down, t.K, "gelu", False)
+    y, idx, _ = _few(t)
+    assert torch.equal(idx.long(), want[0])
+    within(y, want[2], want[3], "few")
 
 def _calls(seed=0, T=40):
     """One call of each operator on buffers of its own: (name, call, outputs, workspace)."""
