@@ -13,7 +13,9 @@
 // values meet that adapter's B rows on the matrix cores, and a token keeps the sum of its own adapter only, so that no
 // value of one request reaches another's. The order of the tokens of one adapter is left to LDS atomics: no token's
 // result depends on its place.
-// bf16 layers round low, a and low' to bf16 for the matrix cores (a as omnimoe_shared_mlp does); sums are fp32.
+// bf16 layers round a to bf16 for the matrix cores, as omnimoe_shared_mlp does, and with more than 64 tokens low and low'
+// (their expansion to few tokens is on the vector units, in fp32); sums are fp32. y, itself rounded to bf16, is 0.0019 to
+// 0.0022 of its norm from the exact one; rounded once from fp32 values it is 0.0017.
 #include "few_tile.hpp"
 #include "internal.hpp"
 #include "tile_gemm.hpp"

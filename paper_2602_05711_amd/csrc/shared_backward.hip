@@ -9,7 +9,9 @@
 // are fp32. bf16 layers round a, dg and du to bf16 (once each, to nearest) for the matrix cores, as the forward pass rounds
 // a; dy, fp32 from the caller, enters as two bf16 values, its rounding and what that leaves (2^-17 relative), for two
 // products more: with dy rounded as well, three roundings (dy, a or dg, the result) put the weight gradients 0.0029 of
-// their norm from the exact ones instead of 0.0023, the rounding of the result alone being 0.0017.
+// their norm from the exact ones instead of 0.0023, the rounding of the result alone being 0.0017. Where a weight of W_down
+// or a value of a is infinite, the two values' products can meet as infinities of either sign or as zero times it: NaN
+// instead of an infinity (keeping them apart would take da's accumulators twice).
 #include "bf16_parts.hpp"
 #include "checkpoint.hpp"
 #include "internal.hpp"
