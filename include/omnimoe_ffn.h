@@ -67,9 +67,9 @@ omnimoe_status omnimoe_shared_mlp_backward(const omnimoe_layer_desc* desc, int32
  * rounding of their sums (and, for bf16 layers, of the hidden values there); logits summed in another order can put
  * near-ties the other way. T <= OMNIMOE_FEW_TOKENS and K <= 64, else OMNIMOE_ERR_UNSUPPORTED. T = 0 is a no-op.
  * When to take it: up to K = 32 it takes less time than those two calls (than the first alone with d_ff = 0). For K > 40, and
- * where a half has more than 64 but fewer than 4 K sub-keys, its selection goes one pick at a time; then the two calls take
- * less time for one token, and the first alone does with d_ff = 0 on grids below 1024 x 1024 (320 x 320, K = 64, one head:
- * 39 instead of 53 us, without a shared branch 31; sixteen tokens 52 instead of 55).
+ * where a half has more than 64 but fewer than 4 K sub-keys, its selection goes one pick at a time; then, on grids below
+ * 1024 x 1024, the two calls take less time for one token, and the first alone does with d_ff = 0 (320 x 320, K = 64, one
+ * head: 39 instead of 53 us, without a shared branch 31).
  * Workspace: omnimoe_layer_few_workspace_size bytes. */
 #define OMNIMOE_FEW_TOKENS 16
 omnimoe_status omnimoe_layer_few_workspace_size(const omnimoe_layer_desc* desc, int32_t d_ff, size_t* bytes);

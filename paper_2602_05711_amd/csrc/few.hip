@@ -126,9 +126,9 @@ constexpr int kThreads = 512, kWaves = 8;
 // largest of the lanes' maxima, its low bits cleared) are ranked by counting; more than 64 of them are taken one after the
 // other instead. That is so with ties, and with most rows for kh near 64, where the threshold is near the least of the 64
 // maxima: of Gaussian logits (n = 320 to 4096) in no row for kh = 32, in 15 to 36% of them for 40, in 71 to 86% for 44, in
-// nearly all from 48 on; with fewer than 4 kh logits, where fewer than kh lanes hold any, always if n > 64. One at a time costs
-// most of the kernel's time: one token, 8 heads of 1024 + 1024 logits, K = 64, 61 us (K = 16: 12), one head of 320 + 320
-// 49 us.
+// nearly all from 48 on; with fewer than 4 kh logits, where fewer than kh lanes hold any, always if n > 64. One at a time
+// costs most of the kernel's time: one token, 8 heads of 1024 + 1024 logits, K = 64, 61 us (K = 16: 12), one head of
+// 320 + 320 49 us.
 template <int R>
 __device__ __forceinline__ void half_best(const float* __restrict__ logits, int n, int kh, uint64_t* __restrict__ cand,
                                           uint64_t* __restrict__ out) {
