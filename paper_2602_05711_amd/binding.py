@@ -1,4 +1,4 @@
-"""Python binding of libomnimoe.so (declared in include/omnimoe.h and include/omnimoe_ffn.h): argument marshalling only.
+"""Python binding of libomnimoe.so (include/omnimoe.h, omnimoe_ffn.h and omnimoe_block.h): argument marshalling only.
 
 Every function has the name of the C entry point it calls and takes torch tensors on the GPU.
 torch provides device memory and the stream (the current stream unless one is given); all of
@@ -51,6 +51,11 @@ class OmnimoeAdapters(ctypes.Structure):
     tensors = fits = made = None  # make_adapters' tables, what they fit, their (n, rank)
 
 
+class OmnimoeProduct(ctypes.Structure):
+    _fields_ = [("n_in", ctypes.c_int32), ("n_out", ctypes.c_int32), ("swiglu", ctypes.c_int32),
+                ("x_order", ctypes.c_int32), ("y_order", ctypes.c_int32)]
+
+
 class OmnimoeError(RuntimeError):
     def __init__(self, fn: str, status: int, text: str):
         super().__init__(f"{fn} failed: {text} (status {status})")
@@ -69,7 +74,7 @@ def load_library():
         raise RuntimeError(f"{LIB_PATH} is missing: build it with __graft_entry__.build()")
     lib = ctypes.CDLL(LIB_PATH)
     P, I32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
-    D = ctypes.POINTER(OmnimoeLayerDesc)
+    D, Q, F = ctypes.POINTER(OmnimoeLayerDesc), ctypes.POINTER(OmnimoeProduct), ctypes.c_float
     sig = {
         "omnimoe_workspace_size": [D, I32, ctypes.POINTER(SZ)],
         "omnimoe_route": [D, P, P, P, P, P, P, P, SZ, P],
@@ -99,6 +104,16 @@ def load_library():
         "omnimoe_layer_forward_few": [D, I32, P, P, P, P, P, P, P, P, P, P, P, SZ, P],
         "omnimoe_shared_mlp_adapters_workspace_size": [D, I32, ctypes.POINTER(OmnimoeAdapters), ctypes.POINTER(SZ)],
         "omnimoe_shared_mlp_adapters": [D, I32, ctypes.POINTER(OmnimoeAdapters), P, P, P, P, P, P, P, SZ, P],
+        "omnimoe_block_join": [D, F, I32, P, P, P, P, P, P, P, P, P],
+        "omnimoe_block_join_backward_workspace_size": [D, ctypes.POINTER(SZ)],
+        "omnimoe_block_join_backward": [D, F, I32, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, SZ, P],
+        "omnimoe_grouped_product": [D, Q, P, P, P, P, P, P],
+        "omnimoe_grouped_product_dx": [D, Q, P, P, P, P, P, P],
+        "omnimoe_grouped_product_dw_workspace_size": [D, Q, ctypes.POINTER(SZ)],
+        "omnimoe_grouped_product_dw": [D, Q, P, P, P, P, P, P, SZ, P],
+        "omnimoe_weights4_store": [D, Q, P, P, P, P],
+        "omnimoe_weights4_load": [D, Q, P, P, P, P],
+        "omnimoe_grouped_product4": [D, Q, P, P, P, P, P, P, P],
         "omnimoe_timer_create": [I32, ctypes.POINTER(P)],
         "omnimoe_timer_destroy": [P],
         "omnimoe_timer_read": [P, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(I32)],
@@ -512,3 +527,124 @@ def omnimoe_shared_mlp_adapters(desc, d_ff, adapters, x, w_gu, w_down, ids, y_in
         ("ids", ids, torch.int32, T), ("y_in", y_in, f32, T * d), ("y", y, dt, T * d), *tables,
         ("ws", ws, torch.uint8, ws.numel())),
         (d_ff, ctypes.byref(adapters), x, w_gu, w_down, ids, y_in, y, ws, ws.numel()), stream)
+
+
+# ------------------------------------------------------------------ include/omnimoe_block.h
+
+EXPORTED_BLOCK = (
+    "omnimoe_block_join", "omnimoe_block_join_backward_workspace_size", "omnimoe_block_join_backward",
+    "omnimoe_grouped_product", "omnimoe_grouped_product_dx", "omnimoe_grouped_product_dw_workspace_size",
+    "omnimoe_grouped_product_dw", "omnimoe_weights4_store", "omnimoe_weights4_load", "omnimoe_grouped_product4",
+)
+ORDERS = {"position": 0, "task": 1, "token": 2}  # OMNIMOE_ORDER_*
+
+
+def _gate_width(gate):
+    return 0 if gate is None else 1 if gate.dim() == 1 else gate.shape[1]
+
+
+def omnimoe_block_join(desc, eps, x, y, gate, w_out, scale, w_in, x_out, n, stream=None):
+    """x_out = x + scale sigmoid(gate) w_out norm(y), n = w_in norm(x_out); gate [T], [T, 1], [T, d] or None; y None: n of x
+    alone; w_out, scale, w_in may be None."""
+    import torch
+    T, d, dt, f32 = desc.T, desc.d, _layer_dtype(desc), torch.float32
+    width = _gate_width(gate)
+    _ffn_call("omnimoe_block_join", desc, (
+        ("x", x, dt, T * d), ("y", y, f32, T * d), ("gate", gate, dt, T * width), ("w_out", w_out, f32, d),
+        ("scale", scale, f32, d), ("w_in", w_in, f32, d), ("x_out", x_out, dt, T * d), ("n", n, dt, T * d)),
+        (eps, width, x, y, gate, w_out, scale, w_in, x_out, n), stream)
+
+
+def omnimoe_block_join_backward_workspace_size(desc) -> int:
+    return _ffn_size("omnimoe_block_join_backward_workspace_size", ctypes.byref(desc))
+
+
+def omnimoe_block_join_backward(desc, eps, x_out, y, gate, w_out, scale, w_in, dx_out, dn, dx, dy, dgate, dw_out, dscale,
+                                dw_in, ws=None, stream=None):
+    """Gradients of omnimoe_block_join; outputs of inputs that are None may be None."""
+    import torch
+    device = (dx if dx is not None else dw_in).device
+    ws = _ffn_workspace(ws, lambda: omnimoe_block_join_backward_workspace_size(desc), device, stream)
+    T, d, dt, f32 = desc.T, desc.d, _layer_dtype(desc), torch.float32
+    width = _gate_width(gate)
+    _ffn_call("omnimoe_block_join_backward", desc, (
+        ("x_out", x_out, dt, T * d), ("y", y, f32, T * d), ("gate", gate, dt, T * width), ("w_out", w_out, f32, d),
+        ("scale", scale, f32, d), ("w_in", w_in, f32, d), ("dx_out", dx_out, dt, T * d), ("dn", dn, dt, T * d),
+        ("dx", dx, dt, T * d), ("dy", dy, f32, T * d), ("dgate", dgate, dt, T * width), ("dw_out", dw_out, f32, d),
+        ("dscale", dscale, f32, d), ("dw_in", dw_in, f32, d), ("ws", ws, torch.uint8, ws.numel())),
+        (eps, width, x_out, y, gate, w_out, scale, w_in, dx_out, dn, dx, dy, dgate, dw_out, dscale, dw_in, ws, ws.numel()),
+        stream)
+
+
+def make_product(n_in, n_out, swiglu=False, x_order="position", y_order="position") -> OmnimoeProduct:
+    """Widths of a product grouped by expert and the orders of its rows: "position", "task" or "token" (x only)."""
+    return OmnimoeProduct(n_in=n_in, n_out=n_out, swiglu=int(swiglu), x_order=ORDERS[x_order], y_order=ORDERS[y_order])
+
+
+def _product_sizes(desc, product):
+    """(dtype, experts, tasks, elements of x, of y, of the weights)"""
+    N, M = desc.n_rows * desc.n_cols, desc.T * desc.H * desc.K
+    w = N * product.n_out * product.n_in * (2 if product.swiglu else 1)
+    return _layer_dtype(desc), N, M, (desc.T if product.x_order == 2 else M) * product.n_in, M * product.n_out, w
+
+
+def _schedule_tensors(N, M, offsets, perm):
+    import torch
+    return ("offsets", offsets, torch.int32, N + 1), ("perm", perm, torch.int32, M)
+
+
+def omnimoe_grouped_product(desc, product, x, w, offsets, perm, y, stream=None):
+    """y = W_e x (or the SwiGLU of gate and up rows) for every position of every expert e; offsets, perm: omnimoe_schedule's."""
+    dt, N, M, nx, ny, nw = _product_sizes(desc, product)
+    _ffn_call("omnimoe_grouped_product", desc, (
+        ("x", x, dt, nx), ("w", w, dt, nw), *_schedule_tensors(N, M, offsets, perm), ("y", y, dt, ny)),
+        (ctypes.byref(product), x, w, offsets, perm, y), stream)
+
+
+def omnimoe_grouped_product_dx(desc, product, dy, w, offsets, perm, dx, stream=None):
+    """dx = W_e^T dy for every position of every expert e."""
+    dt, N, M, nx, ny, nw = _product_sizes(desc, product)
+    _ffn_call("omnimoe_grouped_product_dx", desc, (
+        ("dy", dy, dt, ny), ("w", w, dt, nw), *_schedule_tensors(N, M, offsets, perm), ("dx", dx, dt, nx)),
+        (ctypes.byref(product), dy, w, offsets, perm, dx), stream)
+
+
+def omnimoe_grouped_product_dw_workspace_size(desc, product) -> int:
+    return _ffn_size("omnimoe_grouped_product_dw_workspace_size", ctypes.byref(desc), ctypes.byref(product))
+
+
+def omnimoe_grouped_product_dw(desc, product, x, dy, offsets, perm, dw, ws=None, stream=None):
+    """dw_e = sum over expert e's positions of dy x^T."""
+    import torch
+    ws = _ffn_workspace(ws, lambda: omnimoe_grouped_product_dw_workspace_size(desc, product), dw.device, stream)
+    dt, N, M, nx, ny, nw = _product_sizes(desc, product)
+    _ffn_call("omnimoe_grouped_product_dw", desc, (
+        ("x", x, dt, nx), ("dy", dy, dt, ny), *_schedule_tensors(N, M, offsets, perm), ("dw", dw, dt, nw),
+        ("ws", ws, torch.uint8, ws.numel())),
+        (ctypes.byref(product), x, dy, offsets, perm, dw, ws, ws.numel()), stream)
+
+
+def omnimoe_weights4_store(desc, product, w, codes, scales, stream=None):
+    import torch
+    dt, _, _, _, _, nw = _product_sizes(desc, product)
+    _ffn_call("omnimoe_weights4_store", desc, (
+        ("w", w, dt, nw), ("codes", codes, torch.uint8, nw // 2), ("scales", scales, torch.uint8, nw // 32)),
+        (ctypes.byref(product), w, codes, scales), stream)
+
+
+def omnimoe_weights4_load(desc, product, codes, scales, w, stream=None):
+    import torch
+    dt, _, _, _, _, nw = _product_sizes(desc, product)
+    _ffn_call("omnimoe_weights4_load", desc, (
+        ("codes", codes, torch.uint8, nw // 2), ("scales", scales, torch.uint8, nw // 32), ("w", w, dt, nw)),
+        (ctypes.byref(product), codes, scales, w), stream)
+
+
+def omnimoe_grouped_product4(desc, product, x, codes, scales, offsets, perm, y, stream=None):
+    """omnimoe_grouped_product with weights held in 4 bits (omnimoe_weights4_store)."""
+    import torch
+    dt, N, M, nx, ny, nw = _product_sizes(desc, product)
+    _ffn_call("omnimoe_grouped_product4", desc, (
+        ("x", x, dt, nx), ("codes", codes, torch.uint8, nw // 2), ("scales", scales, torch.uint8, nw // 32),
+        *_schedule_tensors(N, M, offsets, perm), ("y", y, dt, ny)),
+        (ctypes.byref(product), x, codes, scales, offsets, perm, y), stream)

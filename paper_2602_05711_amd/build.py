@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libomnimoe.so")
 SOURCES = ["api.hip", "score_gemm.hip", "select.hip", "schedule.hip", "expert.hip", "grouped.hip",
            "mlp.hip", "backward.hip", "dense.hip", "sweep.hip", "ffn_api.hip", "checkpoint.hip",
-           "shared_backward.hip", "few.hip", "adapters.hip"]
+           "shared_backward.hip", "few.hip", "adapters.hip", "block_api.hip", "block_join.hip",
+           "grouped_product.hip", "weights4.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -8,6 +8,7 @@
 // 24.2 and 20.1 us, 4.2 and 5.0 TB/s; [509, 2048], which is in the caches: 3.1 us each, a launch's own time.
 #include "checkpoint.hpp"
 #include "internal.hpp"
+#include "vec8.hpp"
 
 namespace omnimoe {
 namespace {
@@ -19,19 +20,6 @@ __device__ __forceinline__ int block_exponent(uint32_t amax_bits) {
   const int k = (int)(amax_bits >> 23) - 127;
   const int s = k - 8 + ((amax_bits & 0x007FFFFFu) > 0x00600000u ? 1 : 0);
   return s < -127 ? -127 : s;
-}
-
-template <bool BF16>
-__device__ __forceinline__ void load8(const void* x, int64_t i, float (&v)[8]) {
-  if constexpr (BF16) {
-    const uint4 q = *(const uint4*)((const uint16_t*)x + i);
-    v[0] = bf16_lo(q.x); v[1] = bf16_hi(q.x); v[2] = bf16_lo(q.y); v[3] = bf16_hi(q.y);
-    v[4] = bf16_lo(q.z); v[5] = bf16_hi(q.z); v[6] = bf16_lo(q.w); v[7] = bf16_hi(q.w);
-  } else {
-    const float4 a = *(const float4*)((const float*)x + i), b = *(const float4*)((const float*)x + i + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  }
 }
 
 // Eight values a thread, four threads a block (the last block of a row may be shorter).

@@ -1,0 +1,393 @@
+// Products of rows grouped by expert: position p of expert e has y_p = W_e x_p (or silu(G_e x_p) (U_e x_p), W_e being G_e's
+// rows and then U_e's), dx_p = W_e^T dy_p and dW_e = sum over e's positions of dy_p x_p^T.
+//
+// Many rows an expert: tile products (tile_gemm.hpp) whose rows are gathered by position, task or token while they are
+// copied to LDS. The experts' positions are cut into units of a tile's rows; a workgroup finds its unit from the offsets
+// itself, so that the grid depends on the sizes alone: units past the last leave at once.
+// Few rows an expert: the time is that of reading the weights of the experts that have rows, and of little beside it
+// (few_tile.hpp): a unit is up to sixteen rows, a workgroup takes 32 weight rows and splits the summed index over its waves.
+// Sums are fp32, rounded once; every result has one order of summation, so that it is the same on every run.
+#include "few_tile.hpp"
+#include "grouped_rows.hpp"
+#include "internal.hpp"
+#include "tile_gemm.hpp"
+
+namespace omnimoe {
+namespace {
+
+// Rows gathered over a whole tensor, the summed index contiguous: an address a copy, since the tensor may be larger than
+// 32-bit offsets reach.
+template <class T, int R, int NW>
+struct RowOperand : TileOperand<T, R, false, NW> {
+  typedef TileOperand<T, R, false, NW> Tile;
+  const char* ptr[Tile::kCopies];
+
+  template <class Row>
+  __device__ __forceinline__ void init(const void* p, int64_t ld, int wid, int lane, Row row) {
+    this->lds = wid * Tile::kCopies * 1024;
+#pragma unroll
+    for (int i = 0; i < Tile::kCopies; ++i) {
+      const int at = (wid * Tile::kCopies + i) * 64 + lane, lrow = at / 8;
+      ptr[i] = (const char*)p + ((int64_t)row(lrow) * ld + Tile::place(lrow, at % 8) * Tile::kPer) * T::kSize;
+    }
+  }
+  __device__ __forceinline__ void copy(unsigned char* st, int at, int64_t, int kt, int K, int wid, int lane) const {
+    const int to = at + this->lds;
+    const int64_t skip = (int64_t)kt * T::kStep * T::kSize;
+    if ((kt + 1) * T::kStep <= K) {
+#pragma unroll
+      for (int i = 0; i < Tile::kCopies; ++i)
+        __builtin_amdgcn_global_load_lds((const void*)(ptr[i] + skip), (tg_lds_ptr)(st + (to + i * 1024)), 16, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < Tile::kCopies; ++i) {
+        const char* const p = kt * T::kStep + Tile::chunk_k(i, lane, wid) < K ? ptr[i] + skip : (const char*)&tile_zeros;
+        __builtin_amdgcn_global_load_lds((const void*)p, (tg_lds_ptr)(st + (to + i * 1024)), 16, 0, 0);
+      }
+    }
+  }
+};
+
+// Rows as the summed index: stage kt holds positions first + kt kStep .. of `count`, R of their columns. Which row a copy
+// reads is looked up a stage ahead, so that the copies do not wait for it.
+template <class T, int R, int NW>
+struct SumOperand : TileOperand<T, R, true, NW> {
+  typedef TileOperand<T, R, true, NW> Tile;
+  const char* from;
+  int64_t ld;
+  uint32_t col[Tile::kCopies];
+  const int32_t* perm;
+  int order, hk, M, first, count;
+  mutable int row[Tile::kCopies];  // of the next stage; -1: zeros
+
+  __device__ __forceinline__ void init(const void* p, int width, int c0, const int32_t* perm_, int order_, int hk_, int M_,
+                                       int first_, int count_, int wid, int lane) {
+    from = (const char*)p, ld = (int64_t)width * T::kSize, perm = perm_, order = order_, hk = hk_, M = M_;
+    first = first_, count = count_;
+    this->lds = wid * Tile::kCopies * 1024;
+#pragma unroll
+    for (int i = 0; i < Tile::kCopies; ++i) {
+      const int at = (wid * Tile::kCopies + i) * 64 + lane, lrow = at / Tile::kRowChunks;
+      const int c = c0 + Tile::place(lrow, at % Tile::kRowChunks) * Tile::kPer;
+      col[i] = (uint32_t)((c < width ? c : width - Tile::kPer) * T::kSize);
+    }
+    look(0, wid, lane);
+  }
+  __device__ __forceinline__ void look(int kt, int wid, int lane) const {
+#pragma unroll
+    for (int i = 0; i < Tile::kCopies; ++i) {
+      const int k = kt * T::kStep + ((wid * Tile::kCopies + i) * 64 + lane) / Tile::kRowChunks;
+      row[i] = k < count ? row_of(perm, order, hk, M, first + k) : -1;
+    }
+  }
+  __device__ __forceinline__ void copy(unsigned char* st, int at, int64_t, int kt, int K, int wid, int lane) const {
+    const int to = at + this->lds;
+#pragma unroll
+    for (int i = 0; i < Tile::kCopies; ++i) {
+      const char* const p = K > 0 && row[i] >= 0 ? from + row[i] * ld + col[i] : (const char*)&tile_zeros;
+      __builtin_amdgcn_global_load_lds((const void*)p, (tg_lds_ptr)(st + (to + i * 1024)), 16, 0, 0);
+    }
+    if (K > 0) look(kt + 1, wid, lane);
+  }
+};
+
+struct GroupedArgs {
+  const void *in, *w;
+  void* out;
+  const int32_t *offsets, *perm;
+  int N, M, k, n;  // k: the summed width, n: the result's
+  int hk, in_order, out_order;
+};
+
+// TM positions x TN weight rows a workgroup (SWIGLU: TN / 2 gate rows and the same features' up rows, in blocks of 32 in
+// turn, so that a wave holds both). TRANSPOSED: the summed index is the weights' row (dx).
+template <class T, int TM, int TN, int WR, int WC, bool TRANSPOSED, bool SWIGLU>
+__global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs p) {
+  constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32, FN = SWIGLU ? TN / 2 : TN;
+  static_assert(!SWIGLU || (NI % 2 == 0 && !TRANSPOSED), "a wave's gate and up rows");
+  typedef typename T::elem elem;
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
+  const int tiles_n = (p.n + FN - 1) / FN;
+  // neighbouring tiles, which share rows or weights, go to one XCD
+  RowUnit u;
+  int tile = -1;
+  find_unit<64 * NW>(p.offsets, p.N, p.M, TM, (int*)st0, [&](int total) {
+    const int64_t all = (int64_t)total * tiles_n;
+    if (blockIdx.x >= all) return -1;
+    const unsigned item = (unsigned)xcd_contiguous(blockIdx.x, all), unit = item / (unsigned)tiles_n;
+    tile = __builtin_amdgcn_readfirstlane((int)(item - unit * tiles_n));
+    return (int)unit;
+  }, u);
+  if (tile < 0) return;
+  __syncthreads();
+  const int n0 = tile * FN;
+  int a0[NI], b0[MJ];
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) b0[j] = (wr * MJ + j) * 32;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) a0[i] = (wc * NI + i) * 32;
+  tg_f32x16 acc[NI][MJ];
+  tile_zero(acc);
+  RowOperand<T, TM, NW> b;
+  b.init(p.in, p.k, wid, lane, [&](int r) {
+    const int row = row_of(p.perm, p.in_order, p.hk, p.M, u.first + (r < u.count ? r : u.count - 1));
+    return row < 0 ? 0 : row;
+  });
+  TileOperand<T, TN, TRANSPOSED, NW> a;
+  const elem* const w = (const elem*)p.w + (int64_t)u.expert * (SWIGLU ? 2 : 1) * p.n * p.k;
+  if constexpr (TRANSPOSED)
+    a.init(w, p.n, wid, lane, [&](int r) { return n0 + r < p.n ? n0 + r : p.n - a.kPer; });
+  else
+    a.init(w, p.k, wid, lane, [&](int r) {
+      const int f = n0 + (SWIGLU ? (r >> 6) * 32 + (r & 31) : r), c = f < p.n ? f : p.n - 1;
+      return SWIGLU && (r & 32) ? p.n + c : c;
+    });
+  const TileRange all[2] = {{p.k, 0, 0}, {0, 0, 0}};
+  tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) {
+    const int r = b0[j] + (lane & 31);
+    if (r >= u.count) continue;
+    const int row = row_of(p.perm, p.out_order, p.hk, p.M, u.first + r);
+    if (row < 0) continue;
+    elem* const out = (elem*)p.out + (int64_t)row * p.n;
+#pragma unroll
+    for (int i = 0; i < NI; i += SWIGLU ? 2 : 1)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int f = n0 + (SWIGLU ? a0[i] / 2 : a0[i]) + 8 * q + 4 * (lane >> 5);
+        if (f >= p.n) continue;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = acc[i][j][4 * q + e];
+          if constexpr (SWIGLU) v[e] = activation(1, v[e]) * acc[i + 1][j][4 * q + e];
+        }
+        store4(out + f, v[0], v[1], v[2], v[3]);
+      }
+  }
+}
+
+// 16 RB weight rows (SWIGLU: half of them gate rows, in turn) for a unit of up to sixteen positions.
+template <bool BF16, int RB, bool SWIGLU>
+__global__ __launch_bounds__(256) void grouped_few_kernel(GroupedArgs p, int groups) {
+  constexpr int W = 4, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4, FB = SWIGLU ? RB / 2 : RB;
+  typedef typename std::conditional<BF16, uint16_t, float>::type elem;
+  __shared__ f32x4 tiles[W][RB][64];
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int want = blockIdx.x / (unsigned)groups, f0 = (int)(blockIdx.x % (unsigned)groups) * 16 * FB;
+  RowUnit u;
+  if (find_unit<256>(p.offsets, p.N, p.M, 16, (int*)tiles, [&](int) { return want; }, u) <= want) return;
+  __syncthreads();
+  const int at = row_of(p.perm, p.in_order, p.hk, p.M, u.first + ((l & 15) < u.count ? (l & 15) : u.count - 1));
+  const uint4* const tok[1] = {(const uint4*)((const char*)p.in + (int64_t)(at < 0 ? 0 : at) * p.k * kSize)};
+  const uint4* row[RB];
+  const char* const weights = (const char*)p.w + (int64_t)u.expert * (SWIGLU ? 2 : 1) * p.n * p.k * kSize;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const int f = f0 + 16 * (SWIGLU ? b / 2 : b) + (l & 15), c = f < p.n ? f : p.n - 1;
+    row[b] = (const uint4*)(weights + (int64_t)(SWIGLU && (b & 1) ? p.n + c : c) * p.k * kSize);
+  }
+  f32x4 acc[RB];
+  wave_tile<BF16, RB, 1, 1, W>(row, tok, p.k / E, w, acc);
+  add_tiles(acc, tiles, w, l);
+  if (w || (l & 15) >= u.count) return;
+  const int to = row_of(p.perm, p.out_order, p.hk, p.M, u.first + (l & 15));
+  if (to < 0) return;
+  elem* const out = (elem*)p.out + (int64_t)to * p.n;
+#pragma unroll
+  for (int b = 0; b < RB; b += SWIGLU ? 2 : 1) {
+    const int f = f0 + 16 * (SWIGLU ? b / 2 : b) + 4 * (l >> 4);
+    if (f >= p.n) break;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = acc[b][e];
+      if constexpr (SWIGLU) v[e] = activation(1, v[e]) * acc[b + 1][e];
+    }
+    store4(out + f, v[0], v[1], v[2], v[3]);
+  }
+}
+
+struct GroupedSumArgs {
+  const void *x, *dy;
+  void* dw;
+  float* part;  // [parts][N][n][k]
+  const int32_t *offsets, *perm;
+  int N, M, n, k, hk, x_order, y_order, parts;
+};
+
+// A tile of dW_e: TM of y's columns x TN of x's, one part of e's positions.
+template <class T, int TM, int TN, int WR, int WC>
+__global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArgs p) {
+  constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
+  typedef typename T::elem elem;
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
+  const int tiles_k = (p.k + TN - 1) / TN, tiles_n = (p.n + TM - 1) / TM;
+  const int64_t item = xcd_contiguous(blockIdx.x, gridDim.x);
+  const int tk = (int)(item % tiles_k), tn = (int)(item / tiles_k % tiles_n);
+  const int64_t rest = item / ((int64_t)tiles_k * tiles_n);
+  const int part = (int)(rest % p.parts), e = (int)(rest / p.parts);
+  const int lo = expert_start(p.offsets, e, p.N, p.M), hi = expert_start(p.offsets, e + 1, p.N, p.M);
+  const int rows = hi > lo ? hi - lo : 0, per = ((rows + p.parts - 1) / p.parts + 63) / 64 * 64;
+  const int64_t skip = (int64_t)part * per;
+  const int first = (int)(lo + skip), count = skip >= rows ? 0 : rows - skip < per ? (int)(rows - skip) : per;
+  int a0[NI], b0[MJ];
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) b0[j] = (wr * MJ + j) * 32;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) a0[i] = (wc * NI + i) * 32;
+  tg_f32x16 acc[NI][MJ];
+  tile_zero(acc);
+  SumOperand<T, TN, NW> a;
+  SumOperand<T, TM, NW> b;
+  a.init(p.x, p.k, tk * TN, p.perm, p.x_order, p.hk, p.M, first, count, wid, lane);
+  b.init(p.dy, p.n, tn * TM, p.perm, p.y_order, p.hk, p.M, first, count, wid, lane);
+  const TileRange all[2] = {{count, 0, 0}, {0, 0, 0}};
+  tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) {
+    const int n = tn * TM + b0[j] + (lane & 31);
+    if (n >= p.n) continue;
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int k = tk * TN + a0[i] + 8 * q + 4 * (lane >> 5);
+        if (k >= p.k) continue;
+        const int64_t at = ((int64_t)e * p.n + n) * p.k + k;
+        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        if (p.parts > 1) *(float4*)(p.part + (int64_t)part * p.N * p.n * p.k + at) = make_float4(v[0], v[1], v[2], v[3]);
+        else store4((elem*)p.dw + at, v[0], v[1], v[2], v[3]);
+      }
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void grouped_add_kernel(const float* __restrict__ part, void* __restrict__ dw, int64_t size,
+                                                          int parts) {
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)gridDim.x * 1024) {
+    float4 v = *(const float4*)(part + i);
+    for (int z = 1; z < parts; ++z) {
+      const float4 s = *(const float4*)(part + z * size + i);
+      v.x += s.x;
+      v.y += s.y;
+      v.z += s.z;
+      v.w += s.w;
+    }
+    store4((typename T::elem*)dw + i, v.x, v.y, v.z, v.w);
+  }
+}
+
+// Units of R rows that M positions of N experts can have at most.
+int64_t most_units(int64_t M, int N, int R) {
+  const int64_t n = M / R + N;
+  return n < M ? n : M;
+}
+int64_t cut(int64_t v, int64_t by) { return (v + by - 1) / by; }
+
+// The tile's side by how many tiles of 256 or 128 the sizes make.
+int tile_side(bool bf16, int64_t M, int N, int n) {
+  if (!bf16) return 64;
+  const int64_t rows = M / N;  // of an expert
+  if (rows >= 128 && cut(M, 256) * cut(n, 256) >= 192) return 256;
+  if (rows >= 64 && cut(M, 128) * cut(n, 128) >= 128) return 128;
+  return 64;
+}
+
+template <class T, bool TRANSPOSED, bool SWIGLU>
+hipError_t tiles(const GroupedArgs& p, hipStream_t st) {
+  const int width = SWIGLU ? 2 * p.n : p.n;
+  auto go = [&](auto kernel, int tm, int tn, int threads) -> hipError_t {
+    const int64_t grid = most_units(p.M, p.N, tm) * cut(p.n, SWIGLU ? tn / 2 : tn);
+    if (grid > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, st, p);
+    return hipGetLastError();
+  };
+  const int side = tile_side(T::kSize == 2, p.M, p.N, width);
+  if constexpr (T::kSize == 2) {
+    if (side == 256) return go(grouped_tile_kernel<T, 256, 256, 2, 4, TRANSPOSED, SWIGLU>, 256, 256, 512);
+    if (side == 128) return go(grouped_tile_kernel<T, 128, 128, 4, 2, TRANSPOSED, SWIGLU>, 128, 128, 512);
+  }
+  return go(grouped_tile_kernel<T, 64, 128, 2, 2, TRANSPOSED, SWIGLU>, 64, 128, 256);
+}
+
+template <bool BF16, bool SWIGLU>
+hipError_t few(const GroupedArgs& p, hipStream_t st) {
+  constexpr int RB = 2;
+  const int64_t groups = cut(p.n, SWIGLU ? 8 * RB : 16 * RB), grid = most_units(p.M, p.N, 16) * groups;
+  hipLaunchKernelGGL((grouped_few_kernel<BF16, RB, SWIGLU>), dim3((unsigned)grid), dim3(256), 0, st, p, (int)groups);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t forward(const GroupedArgs& p, bool swiglu, hipStream_t st) {
+  if (p.M <= 16 * (int64_t)p.N) return swiglu ? few<T::kSize == 2, true>(p, st) : few<T::kSize == 2, false>(p, st);
+  return swiglu ? tiles<T, false, true>(p, st) : tiles<T, false, false>(p, st);
+}
+
+int sum_side(const Shape& s, int k, int n) {
+  if (!s.bf16) return 64;
+  if (s.N * cut(k, 256) * cut(n, 256) >= 192) return 256;
+  return s.N * cut(k, 128) * cut(n, 128) >= 128 ? 128 : 64;
+}
+
+// Parts of an expert's positions, where the tiles alone leave compute units idle.
+int sum_parts(const Shape& s, int k, int n) {
+  const int side = sum_side(s, k, n);
+  const int64_t tiles = s.N * cut(k, side) * cut(n, side), wanted = 512 / tiles, most = s.M / s.N / 512;
+  const int64_t parts = wanted < most ? wanted : most;
+  return parts < 1 ? 1 : parts > 32 ? 32 : (int)parts;
+}
+
+template <class T>
+hipError_t sums(const GroupedSumArgs& p, int side, hipStream_t st) {
+  auto go = [&](auto kernel, int threads) -> hipError_t {
+    const int64_t grid = (int64_t)p.N * p.parts * cut(p.k, side) * cut(p.n, side);
+    if (grid > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, st, p);
+    return hipGetLastError();
+  };
+  hipError_t e = hipSuccess;
+  if constexpr (T::kSize == 2) {
+    if (side == 256) e = go(grouped_sum_kernel<T, 256, 256, 2, 4>, 512);
+    else if (side == 128) e = go(grouped_sum_kernel<T, 128, 128, 2, 4>, 512);
+  }
+  if (side == 64) e = go(grouped_sum_kernel<T, 64, 64, 2, 2>, 256);
+  if (e || p.parts == 1) return e;
+  const int64_t size = (int64_t)p.N * p.n * p.k, blocks = cut(size, 1024);
+  hipLaunchKernelGGL(grouped_add_kernel<T>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, st, p.part, p.dw,
+                     size, p.parts);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_grouped_product(const Shape& s, const ProductShape& q, const void* x, const void* w,
+                                  const int32_t* offsets, const int32_t* perm, void* y, hipStream_t st) {
+  const GroupedArgs p{x, w, y, offsets, perm, (int)s.N, (int)s.M, q.n_in, q.n_out, s.hk, q.x_order, q.y_order};
+  return s.bf16 ? forward<BF16>(p, q.swiglu, st) : forward<F32>(p, q.swiglu, st);
+}
+
+hipError_t launch_grouped_dx(const Shape& s, const ProductShape& q, const void* dy, const void* w, const int32_t* offsets,
+                             const int32_t* perm, void* dx, hipStream_t st) {
+  const GroupedArgs p{dy, w, dx, offsets, perm, (int)s.N, (int)s.M, q.n_out, q.n_in, s.hk, q.y_order, q.x_order};
+  return s.bf16 ? tiles<BF16, true, false>(p, st) : tiles<F32, true, false>(p, st);
+}
+
+size_t grouped_dw_ws_bytes(const Shape& s, const ProductShape& q) {
+  const int parts = sum_parts(s, q.n_in, q.n_out);
+  return parts > 1 ? (size_t)parts * s.N * q.n_in * q.n_out * 4 : 0;
+}
+
+hipError_t launch_grouped_dw(const Shape& s, const ProductShape& q, const void* x, const void* dy, const int32_t* offsets,
+                             const int32_t* perm, void* dw, void* ws, hipStream_t st) {
+  const GroupedSumArgs p{x, dy, dw, (float*)ws, offsets, perm, (int)s.N, (int)s.M, q.n_out, q.n_in, s.hk, q.x_order,
+                         q.y_order, sum_parts(s, q.n_in, q.n_out)};
+  const int side = sum_side(s, q.n_in, q.n_out);
+  return s.bf16 ? sums<BF16>(p, side, st) : sums<F32>(p, side, st);
+}
+
+}  // namespace omnimoe

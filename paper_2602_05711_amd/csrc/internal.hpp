@@ -276,4 +276,38 @@ hipError_t launch_adapters(const Shape& s, int d_ff, const AdapterTables& t, con
                            const void* w_down, const int32_t* ids, const float* y_in, void* y, void* ws,
                            hipStream_t st);
 
+// The joint between a branch and the residual stream (block_join.hip) and its way back; NULL as in omnimoe_block.h.
+// Workspace of the way back: join_back_ws_bytes.
+hipError_t launch_join(int64_t T, int d, bool bf16, float eps, int gate_width, const void* x, const float* y,
+                       const void* gate, const float* w_out, const float* scale, const float* w_in, void* x_out, void* n,
+                       hipStream_t st);
+size_t join_back_ws_bytes(int64_t T, int d);
+hipError_t launch_join_back(int64_t T, int d, bool bf16, float eps, int gate_width, const void* x_out, const float* y,
+                            const void* gate, const float* w_out, const float* scale, const float* w_in,
+                            const void* dx_out, const void* dn, void* dx, float* dy, void* dgate, float* dw_out,
+                            float* dscale, float* dw_in, void* ws, hipStream_t st);
+
+// Products of rows grouped by expert (grouped_product.hip; with 4-bit weights weights4.hip). perm is NULL where both orders
+// are by position. Limits: kMaxExperts matrices of less than 4 GiB.
+struct ProductShape {
+  int n_in, n_out;
+  bool swiglu;
+  int x_order, y_order;  // 0 position, 1 task, 2 token
+};
+constexpr int kMaxExperts = 4096;
+hipError_t launch_grouped_product(const Shape& s, const ProductShape& q, const void* x, const void* w,
+                                  const int32_t* offsets, const int32_t* perm, void* y, hipStream_t st);
+hipError_t launch_grouped_dx(const Shape& s, const ProductShape& q, const void* dy, const void* w, const int32_t* offsets,
+                             const int32_t* perm, void* dx, hipStream_t st);
+size_t grouped_dw_ws_bytes(const Shape& s, const ProductShape& q);
+hipError_t launch_grouped_dw(const Shape& s, const ProductShape& q, const void* x, const void* dy, const int32_t* offsets,
+                             const int32_t* perm, void* dw, void* ws, hipStream_t st);
+hipError_t launch_weights4_store(const Shape& s, const ProductShape& q, const void* w, uint8_t* codes, uint8_t* scales,
+                                 hipStream_t st);
+hipError_t launch_weights4_load(const Shape& s, const ProductShape& q, const uint8_t* codes, const uint8_t* scales, void* w,
+                                hipStream_t st);
+hipError_t launch_grouped_product4(const Shape& s, const ProductShape& q, const void* x, const uint8_t* codes,
+                                   const uint8_t* scales, const int32_t* offsets, const int32_t* perm, void* y,
+                                   hipStream_t st);
+
 }  // namespace omnimoe
