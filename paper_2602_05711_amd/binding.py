@@ -539,6 +539,30 @@ EXPORTED_BLOCK = (
 ORDERS = {"position": 0, "task": 1, "token": 2}  # OMNIMOE_ORDER_*
 
 
+def _block_call(fn, desc, head, tensors, tail, stream):
+    """_ffn_call for fn(desc, *head, *(the tensors' addresses), *tail, stream): checks and addresses in one pass."""
+    import torch
+    dev, args = -1, [ctypes.byref(desc), *head]
+    for name, t, dtype, n in tensors:
+        if t is None:
+            args.append(None)
+            continue
+        at = t.get_device()
+        if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or at < 0 or (at != dev and dev >= 0):
+            _ffn_refuse(fn, dev, name, t, dtype, n)
+        dev = at
+        args.append(t.data_ptr())
+    call = getattr(_lib or load_library(), fn)
+    if stream is not None and dev >= 0 and stream.device_index != dev:
+        raise ValueError(f"{fn}: the stream belongs to GPU {stream.device_index}, the tensors to GPU {dev}")
+    at = torch.cuda.current_device()
+    if dev < 0 or dev == at:
+        _check(fn, call(*args, *tail, _raw_stream(at) if stream is None else stream.cuda_stream))
+        return
+    with torch.cuda.device(dev):
+        _check(fn, call(*args, *tail, _raw_stream(dev) if stream is None else stream.cuda_stream))
+
+
 def _gate_width(gate):
     return 0 if gate is None else 1 if gate.dim() == 1 else gate.shape[1]
 
@@ -549,10 +573,10 @@ def omnimoe_block_join(desc, eps, x, y, gate, w_out, scale, w_in, x_out, n, stre
     import torch
     T, d, dt, f32 = desc.T, desc.d, _layer_dtype(desc), torch.float32
     width = _gate_width(gate)
-    _ffn_call("omnimoe_block_join", desc, (
+    _block_call("omnimoe_block_join", desc, (eps, width), (
         ("x", x, dt, T * d), ("y", y, f32, T * d), ("gate", gate, dt, T * width), ("w_out", w_out, f32, d),
         ("scale", scale, f32, d), ("w_in", w_in, f32, d), ("x_out", x_out, dt, T * d), ("n", n, dt, T * d)),
-        (eps, width, x, y, gate, w_out, scale, w_in, x_out, n), stream)
+        (), stream)
 
 
 def omnimoe_block_join_backward_workspace_size(desc) -> int:
@@ -567,13 +591,12 @@ def omnimoe_block_join_backward(desc, eps, x_out, y, gate, w_out, scale, w_in, d
     ws = _ffn_workspace(ws, lambda: omnimoe_block_join_backward_workspace_size(desc), device, stream)
     T, d, dt, f32 = desc.T, desc.d, _layer_dtype(desc), torch.float32
     width = _gate_width(gate)
-    _ffn_call("omnimoe_block_join_backward", desc, (
+    _block_call("omnimoe_block_join_backward", desc, (eps, width), (
         ("x_out", x_out, dt, T * d), ("y", y, f32, T * d), ("gate", gate, dt, T * width), ("w_out", w_out, f32, d),
         ("scale", scale, f32, d), ("w_in", w_in, f32, d), ("dx_out", dx_out, dt, T * d), ("dn", dn, dt, T * d),
         ("dx", dx, dt, T * d), ("dy", dy, f32, T * d), ("dgate", dgate, dt, T * width), ("dw_out", dw_out, f32, d),
         ("dscale", dscale, f32, d), ("dw_in", dw_in, f32, d), ("ws", ws, torch.uint8, ws.numel())),
-        (eps, width, x_out, y, gate, w_out, scale, w_in, dx_out, dn, dx, dy, dgate, dw_out, dscale, dw_in, ws, ws.numel()),
-        stream)
+        (ws.numel(),), stream)
 
 
 def make_product(n_in, n_out, swiglu=False, x_order="position", y_order="position") -> OmnimoeProduct:
@@ -596,17 +619,17 @@ def _schedule_tensors(N, M, offsets, perm):
 def omnimoe_grouped_product(desc, product, x, w, offsets, perm, y, stream=None):
     """y = W_e x (or the SwiGLU of gate and up rows) for every position of every expert e; offsets, perm: omnimoe_schedule's."""
     dt, N, M, nx, ny, nw = _product_sizes(desc, product)
-    _ffn_call("omnimoe_grouped_product", desc, (
+    _block_call("omnimoe_grouped_product", desc, (ctypes.byref(product),), (
         ("x", x, dt, nx), ("w", w, dt, nw), *_schedule_tensors(N, M, offsets, perm), ("y", y, dt, ny)),
-        (ctypes.byref(product), x, w, offsets, perm, y), stream)
+        (), stream)
 
 
 def omnimoe_grouped_product_dx(desc, product, dy, w, offsets, perm, dx, stream=None):
     """dx = W_e^T dy for every position of every expert e."""
     dt, N, M, nx, ny, nw = _product_sizes(desc, product)
-    _ffn_call("omnimoe_grouped_product_dx", desc, (
+    _block_call("omnimoe_grouped_product_dx", desc, (ctypes.byref(product),), (
         ("dy", dy, dt, ny), ("w", w, dt, nw), *_schedule_tensors(N, M, offsets, perm), ("dx", dx, dt, nx)),
-        (ctypes.byref(product), dy, w, offsets, perm, dx), stream)
+        (), stream)
 
 
 def omnimoe_grouped_product_dw_workspace_size(desc, product) -> int:
@@ -618,33 +641,33 @@ def omnimoe_grouped_product_dw(desc, product, x, dy, offsets, perm, dw, ws=None,
     import torch
     ws = _ffn_workspace(ws, lambda: omnimoe_grouped_product_dw_workspace_size(desc, product), dw.device, stream)
     dt, N, M, nx, ny, nw = _product_sizes(desc, product)
-    _ffn_call("omnimoe_grouped_product_dw", desc, (
+    _block_call("omnimoe_grouped_product_dw", desc, (ctypes.byref(product),), (
         ("x", x, dt, nx), ("dy", dy, dt, ny), *_schedule_tensors(N, M, offsets, perm), ("dw", dw, dt, nw),
         ("ws", ws, torch.uint8, ws.numel())),
-        (ctypes.byref(product), x, dy, offsets, perm, dw, ws, ws.numel()), stream)
+        (ws.numel(),), stream)
 
 
 def omnimoe_weights4_store(desc, product, w, codes, scales, stream=None):
     import torch
     dt, _, _, _, _, nw = _product_sizes(desc, product)
-    _ffn_call("omnimoe_weights4_store", desc, (
+    _block_call("omnimoe_weights4_store", desc, (ctypes.byref(product),), (
         ("w", w, dt, nw), ("codes", codes, torch.uint8, nw // 2), ("scales", scales, torch.uint8, nw // 32)),
-        (ctypes.byref(product), w, codes, scales), stream)
+        (), stream)
 
 
 def omnimoe_weights4_load(desc, product, codes, scales, w, stream=None):
     import torch
     dt, _, _, _, _, nw = _product_sizes(desc, product)
-    _ffn_call("omnimoe_weights4_load", desc, (
+    _block_call("omnimoe_weights4_load", desc, (ctypes.byref(product),), (
         ("codes", codes, torch.uint8, nw // 2), ("scales", scales, torch.uint8, nw // 32), ("w", w, dt, nw)),
-        (ctypes.byref(product), codes, scales, w), stream)
+        (), stream)
 
 
 def omnimoe_grouped_product4(desc, product, x, codes, scales, offsets, perm, y, stream=None):
     """omnimoe_grouped_product with weights held in 4 bits (omnimoe_weights4_store)."""
     import torch
     dt, N, M, nx, ny, nw = _product_sizes(desc, product)
-    _ffn_call("omnimoe_grouped_product4", desc, (
+    _block_call("omnimoe_grouped_product4", desc, (ctypes.byref(product),), (
         ("x", x, dt, nx), ("codes", codes, torch.uint8, nw // 2), ("scales", scales, torch.uint8, nw // 32),
         *_schedule_tensors(N, M, offsets, perm), ("y", y, dt, ny)),
-        (ctypes.byref(product), x, codes, scales, offsets, perm, y), stream)
+        (), stream)

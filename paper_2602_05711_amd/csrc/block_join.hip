@@ -32,7 +32,8 @@ struct JoinArgs {
 
 // sigmoid(g) and what it leaves to 1, both to fp32's relative accuracy.
 __device__ __forceinline__ float sigmoid(float g, float& rest) {
-  const float e = expf(-fabsf(g)), big = 1.0f / (1.0f + e), small = e * big;
+  const float e = expf(-fabsf(g)), b = 1.0f + e, r = __builtin_amdgcn_rcpf(b);
+  const float big = fmaf(fmaf(-b, r, 1.0f), r, r), small = e * big;  // (1 <= b <= 2: a step of Newton's gives 1 / b)
   rest = g < 0.0f ? big : small;
   return g < 0.0f ? small : big;
 }
@@ -154,15 +155,42 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs p) {
   }
 }
 
-// R rows at a time a workgroup of W waves, eight values of each a thread. A thread keeps its columns' sums over the rows.
-template <bool BF16, int W, int R>
+// A row of the way back as it lies in memory, this thread's eight values of each.
+template <bool BF16>
+struct BackRow {
+  Raw8<BF16> x, dn, dx_out, gate;
+  Raw8<false> y;
+  float token;
+  __device__ __forceinline__ void load(const JoinArgs& p, int64_t t, int c0, bool in) {
+    if (p.y && p.gate_width == 1) token = BF16 ? bf16_lo(((const uint16_t*)p.gate)[t]) : ((const float*)p.gate)[t];
+    if (!in) return;
+    const int64_t at = t * p.d + c0;
+    if (p.w_in) {
+      x.load(p.x, at);
+      dn.load(p.dn, at);
+    }
+    if (p.dx_out) dx_out.load(p.dx_out, at);
+    if (p.y) y.load(p.y, at);
+    if (p.y && p.gate_width > 1) gate.load(p.gate, at);
+  }
+};
+
+// A row at a time a workgroup of W waves, eight values of each operand a thread; the next row's are on their way meanwhile.
+// A thread keeps its columns' sums over the rows.
+template <bool BF16, int W>
 __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
-  __shared__ float lds3[2][W][3 * R], lds1[2][W][R];
+  __shared__ float lds3[2][W][3], lds1[2][W][1];
   int turn3 = 0, turn1 = 0;
   const int c0 = threadIdx.x * 8;
   const bool in = c0 < p.d;
   const float d1 = 1.0f / (float)p.d;
   const bool channel = p.y && p.gate_width > 1, token = p.y && p.gate_width == 1;
+  BackRow<BF16> raw;
+  raw.x.zero(), raw.dn.zero(), raw.dx_out.zero(), raw.gate.zero(), raw.y.zero();
+  raw.token = 0.0f;
+  const int64_t stride = gridDim.x;
+  int64_t t = blockIdx.x;
+  raw.load(p, t, c0, in);
   float a[8], w_in[8], sum_s[8], sum_n[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) a[e] = 1.0f, w_in[e] = sum_s[e] = sum_n[e] = 0.0f;
@@ -176,103 +204,77 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
       for (int e = 0; e < 8; ++e) a[e] *= w[e];
     }
   }
-  for (int64_t t0 = (int64_t)blockIdx.x * R; t0 < p.T; t0 += (int64_t)gridDim.x * R) {
-    float x[R][8], y[R][8], dn[R][8], G[R][8], g[R][8];
+  for (; t < p.T; t += stride) {
+    float x[8], y[8], u[8], G[8], g[8], dn[8];
+    raw.x.values(x);
+    raw.dn.values(dn);
+    raw.dx_out.values(G);
+    raw.gate.values(g);
+    raw.y.values(y);
+    const float gate = raw.token;
+    if (t + stride < p.T) raw.load(p, t + stride, c0, in);
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[i][e] = y[i][e] = dn[i][e] = G[i][e] = g[i][e] = 0.0f;
-      const int64_t t = t0 + i;
-      if (t >= p.T) continue;
-      if (token) g[i][0] = BF16 ? bf16_lo(((const uint16_t*)p.gate)[t]) : ((const float*)p.gate)[t];
-      if (!in) continue;
-      const int64_t at = t * p.d + c0;
-      if (p.w_in) {
-        load8<BF16>(p.x, at, x[i]);
-        load8<BF16>(p.dn, at, dn[i]);
-      }
-      if (p.dx_out) load8<BF16>(p.dx_out, at, G[i]);
-      if (p.y) load8f(p.y, at, y[i]);
-      if (channel) load8<BF16>(p.gate, at, g[i]);
-    }
+    for (int e = 0; e < 8; ++e) u[e] = w_in[e] * dn[e];
     // sums of x'^2, u x' and y^2
-    float s3[3 * R], pre_x[R], pre_y[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) pre_x[i] = pre_y[i] = 1.0f;
+    float s3[3], pre_x = 1.0f, pre_y = 1.0f;
     for (bool again = false;;) {
-      bool over = false;
-#pragma unroll
-      for (int i = 0; i < R; ++i) {
-        float sx = 0.0f, su = 0.0f, sy = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float vx = x[i][e] * pre_x[i], vy = y[i][e] * pre_y[i];
-          sx = fmaf(vx, vx, sx);
-          su = fmaf(w_in[e] * dn[i][e], vx, su);
-          sy = fmaf(vy, vy, sy);
-        }
-        s3[3 * i] = sx;
-        s3[3 * i + 1] = su;
-        s3[3 * i + 2] = sy;
-      }
-      block_sums<W>(s3, lds3, turn3);
-#pragma unroll
-      for (int i = 0; i < R; ++i) {
-        if (!finite(s3[3 * i])) over = true, pre_x[i] = kSmall;
-        if (!finite(s3[3 * i + 2])) over = true, pre_y[i] = kSmall;
-      }
-      if (!over || again) break;  // (the sums are every thread's)
-      again = true;
-    }
-    float r[R], sq[R], s[R], rest[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const float ix = 1.0f / sqrtf(s3[3 * i] * d1 + p.eps * pre_x[i] * pre_x[i]);
-      const float iy = p.w_out ? 1.0f / sqrtf(s3[3 * i + 2] * d1 + p.eps * pre_y[i] * pre_y[i]) : 1.0f;
-      const float m = s3[3 * i + 1] * ix * d1;
-      if (!p.w_out) pre_y[i] = 1.0f;
-      r[i] = iy;
-      s[i] = token ? sigmoid(g[i][0], rest[i]) : 1.0f;
-      sq[i] = 0.0f;
+      s3[0] = s3[1] = s3[2] = 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if (p.w_in) {
-          const float xh = x[i][e] * pre_x[i] * ix;
-          G[i][e] += ix * (w_in[e] * dn[i][e] - xh * m) * pre_x[i];
-          sum_n[e] = fmaf(dn[i][e], xh, sum_n[e]);
-        }
-        y[i][e] = y[i][e] * pre_y[i] * iy;  // yh
-        const float Gs = G[i][e] * (channel ? sigmoid(g[i][e], g[i][e]) : s[i]);
-        sum_s[e] = fmaf(Gs, y[i][e], sum_s[e]);
-        x[i][e] = Gs * a[e];  // q
-        sq[i] = fmaf(x[i][e], y[i][e], sq[i]);
+        const float vx = x[e] * pre_x, vy = y[e] * pre_y;
+        s3[0] = fmaf(vx, vx, s3[0]);
+        s3[1] = fmaf(u[e], vx, s3[1]);
+        s3[2] = fmaf(vy, vy, s3[2]);
       }
+      block_sums<W>(s3, lds3, turn3);
+      if (again || (finite(s3[0]) && finite(s3[2]))) break;  // (the sums are every thread's)
+      if (!finite(s3[0])) pre_x = kSmall;
+      if (!finite(s3[2])) pre_y = kSmall;
+      again = true;
     }
-    if (p.y) block_sums<W>(sq, lds1, turn1);
+    const float ix = 1.0f / sqrtf(s3[0] * d1 + p.eps * pre_x * pre_x), m = s3[1] * ix * d1;
+    const float iy = p.w_out ? 1.0f / sqrtf(s3[2] * d1 + p.eps * pre_y * pre_y) : 1.0f;
+    if (!p.w_out) pre_y = 1.0f;
+    float rest = 0.0f;
+    const float s = token ? sigmoid(gate, rest) : 1.0f;
+    float sq[1] = {0.0f};
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int64_t t = t0 + i;
-      if (t >= p.T) break;
-      if (token && threadIdx.x == 0) {
-        const float v = rest[i] * sq[i];
-        if constexpr (BF16) ((uint16_t*)p.dgate)[t] = bf16_rne(v);
-        else ((float*)p.dgate)[t] = v;
+    for (int e = 0; e < 8; ++e) {
+      if (p.w_in) {
+        const float xh = x[e] * pre_x * ix;
+        G[e] += ix * (u[e] - xh * m) * pre_x;
+        sum_n[e] = fmaf(dn[e], xh, sum_n[e]);
       }
-      if (!in) continue;
-      const int64_t at = t * p.d + c0;
-      store8<BF16>(p.dx, at, G[i]);
-      if (!p.y) continue;
-      const float m = p.w_out ? sq[i] * d1 : 0.0f;
+      y[e] = y[e] * pre_y * iy;  // yh
+      const float Gs = G[e] * (channel ? sigmoid(g[e], g[e]) : s);
+      sum_s[e] = fmaf(Gs, y[e], sum_s[e]);
+      x[e] = Gs * a[e];  // q
+      sq[0] = fmaf(x[e], y[e], sq[0]);
+    }
+    const int64_t at = t * p.d + c0;
+    if (in) store8<BF16>(p.dx, at, G);
+    if (!p.y) continue;
+    if (channel && in) {
       float v[8];
-      if (channel) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = g[i][e] * (x[i][e] * y[i][e]);
-        store8<BF16>(p.dgate, at, v);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = r[i] * (x[i][e] - y[i][e] * m) * pre_y[i];
-      store8<false>(p.dy, at, v);
+      for (int e = 0; e < 8; ++e) v[e] = g[e] * (x[e] * y[e]);
+      store8<BF16>(p.dgate, at, v);
     }
+    if (!p.w_out && !token) {
+      if (in) store8<false>(p.dy, at, x);
+      continue;
+    }
+    block_sums<W>(sq, lds1, turn1);
+    if (token && threadIdx.x == 0) {
+      const float v = rest * sq[0];
+      if constexpr (BF16) ((uint16_t*)p.dgate)[t] = bf16_rne(v);
+      else ((float*)p.dgate)[t] = v;
+    }
+    if (!in) continue;
+    const float m2 = p.w_out ? sq[0] * d1 : 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = iy * (x[e] - y[e] * m2) * pre_y;
+    store8<false>(p.dy, at, y);
   }
   if (in) {
     float* const part = p.part + (int64_t)blockIdx.x * 2 * p.d + c0;
@@ -281,32 +283,41 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
   }
 }
 
-// The columns' sums of n workgroups, sixteen columns a workgroup: sixteen threads a column add every sixteenth one, then the
+// The columns' sums of n workgroups, 32 columns a workgroup: 32 threads, four columns each, add every 32nd one, then the
 // first of them those sums in order.
 __global__ __launch_bounds__(256) void join_columns_kernel(const float* __restrict__ part, int n, int d,
                                                            const float* __restrict__ w_out,
                                                            const float* __restrict__ scale, float* dw_out, float* dscale,
                                                            float* dw_in) {
-  __shared__ float lds[16][17];
-  const int col = threadIdx.x & 15, row = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
+  __shared__ float4 lds[32][8];
+  const int col = threadIdx.x & 7, row = threadIdx.x >> 3, c = blockIdx.x * 32 + col * 4;
   const int which = blockIdx.y;  // 0: dw_out and dscale, 1: dw_in
-  float v = 0.0f;
-  if (c < d)
-    for (int i = row; i < n; i += 16) v += part[((int64_t)i * 2 + which) * d + c];
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c < d) {
+    const float* const from = part + (int64_t)which * d + c;
+#pragma unroll 8
+    for (int i = row; i < n; i += 32) {
+      const float4 s = *(const float4*)(from + (int64_t)i * 2 * d);
+      v.x += s.x;
+      v.y += s.y;
+      v.z += s.z;
+      v.w += s.w;
+    }
+  }
   lds[row][col] = v;
   __syncthreads();
-  if (row || c >= d) return;
+  const int c1 = blockIdx.x * 32 + (int)threadIdx.x;
+  if (threadIdx.x >= 32 || c1 >= d) return;
+  float s = 0.0f;
 #pragma unroll
-  for (int i = 1; i < 16; ++i) v += lds[i][col];
+  for (int i = 0; i < 32; ++i) s += ((const float*)lds[i])[threadIdx.x];
   if (which) {
-    if (dw_in) dw_in[c] = v;
+    if (dw_in) dw_in[c1] = s;
     return;
   }
-  if (dscale) dscale[c] = w_out ? w_out[c] * v : v;
-  if (dw_out) dw_out[c] = scale ? scale[c] * v : v;
+  if (dscale) dscale[c1] = w_out ? w_out[c1] * s : s;
+  if (dw_out) dw_out[c1] = scale ? scale[c1] * s : s;
 }
-
-constexpr int kBackRows = 2;
 
 int back_waves(int d) {
   int w = 1;
@@ -315,8 +326,8 @@ int back_waves(int d) {
 }
 int back_groups(int64_t T, int d) {
   const int w = back_waves(d);
-  const int64_t n = (T + kBackRows - 1) / kBackRows, most = w > 8 ? 256 : 2048 / w;
-  return (int)(n < most ? n : most);
+  const int64_t most = w > 8 ? 256 : 3072 / w;
+  return (int)(T < most ? T : most);
 }
 
 template <bool BF16>
@@ -339,15 +350,15 @@ hipError_t join_back(const JoinArgs& p, float* dw_out, float* dscale, float* dw_
   const int n = back_groups(p.T, p.d), w = back_waves(p.d);
   if (n) {
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(64 * w), 0, st, p); };
-    if (w == 1) go(join_back_kernel<BF16, 1, kBackRows>);
-    else if (w == 2) go(join_back_kernel<BF16, 2, kBackRows>);
-    else if (w == 4) go(join_back_kernel<BF16, 4, kBackRows>);
-    else if (w == 8) go(join_back_kernel<BF16, 8, kBackRows>);
-    else go(join_back_kernel<BF16, 16, kBackRows>);
+    if (w == 1) go(join_back_kernel<BF16, 1>);
+    else if (w == 2) go(join_back_kernel<BF16, 2>);
+    else if (w == 4) go(join_back_kernel<BF16, 4>);
+    else if (w == 8) go(join_back_kernel<BF16, 8>);
+    else go(join_back_kernel<BF16, 16>);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   if (!dw_out && !dscale && !dw_in) return hipSuccess;
-  hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)((p.d + 15) / 16), 2), dim3(256), 0, st, p.part, n, p.d, p.w_out,
+  hipLaunchKernelGGL(join_columns_kernel, dim3((unsigned)((p.d + 31) / 32), 2), dim3(256), 0, st, p.part, n, p.d, p.w_out,
                      p.scale, dw_out, dscale, dw_in);
   return hipGetLastError();
 }

@@ -7,6 +7,7 @@
 // Few rows an expert: the time is that of reading the weights of the experts that have rows, and of little beside it
 // (few_tile.hpp): a unit is up to sixteen rows, a workgroup takes 32 weight rows and splits the summed index over its waves.
 // Sums are fp32, rounded once; every result has one order of summation, so that it is the same on every run.
+#include <stdlib.h>
 #include "few_tile.hpp"
 #include "grouped_rows.hpp"
 #include "internal.hpp"
@@ -48,22 +49,24 @@ struct RowOperand : TileOperand<T, R, false, NW> {
   }
 };
 
-// Rows as the summed index: stage kt holds positions first + kt kStep .. of `count`, R of their columns. Which row a copy
-// reads is looked up a stage ahead, so that the copies do not wait for it.
-template <class T, int R, int NW>
+// Rows as the summed index: stage kt holds positions first + kt kStep .. of `count`, R of their columns. GATHER: the entries
+// of perm that a stage's copies go by lie in LDS, tasks[kt % 2], from the stage before on: a load into registers would have
+// to be waited for behind the copies issued before it. Both operands go by the same entries, and the one that is copied
+// last (FETCH) has the next stage's brought by wave 0.
+template <class T, int R, int NW, bool GATHER, bool FETCH>
 struct SumOperand : TileOperand<T, R, true, NW> {
   typedef TileOperand<T, R, true, NW> Tile;
+  static_assert(T::kStep <= 64, "a wave's lanes");
   const char* from;
   int64_t ld;
   uint32_t col[Tile::kCopies];
-  const int32_t* perm;
-  int order, hk, M, first, count;
-  mutable int row[Tile::kCopies];  // of the next stage; -1: zeros
+  RowOrder rows;
+  int first, count;
+  int (*tasks)[64];
 
-  __device__ __forceinline__ void init(const void* p, int width, int c0, const int32_t* perm_, int order_, int hk_, int M_,
-                                       int first_, int count_, int wid, int lane) {
-    from = (const char*)p, ld = (int64_t)width * T::kSize, perm = perm_, order = order_, hk = hk_, M = M_;
-    first = first_, count = count_;
+  __device__ __forceinline__ void init(const void* p, int width, int c0, const RowOrder& rows_, int first_, int count_,
+                                       int (&tasks_)[2][64], int wid, int lane) {
+    from = (const char*)p, ld = (int64_t)width * T::kSize, rows = rows_, first = first_, count = count_, tasks = tasks_;
     this->lds = wid * Tile::kCopies * 1024;
 #pragma unroll
     for (int i = 0; i < Tile::kCopies; ++i) {
@@ -71,57 +74,46 @@ struct SumOperand : TileOperand<T, R, true, NW> {
       const int c = c0 + Tile::place(lrow, at % Tile::kRowChunks) * Tile::kPer;
       col[i] = (uint32_t)((c < width ? c : width - Tile::kPer) * T::kSize);
     }
-    look(0, wid, lane);
   }
-  __device__ __forceinline__ void look(int kt, int wid, int lane) const {
-#pragma unroll
-    for (int i = 0; i < Tile::kCopies; ++i) {
-      const int k = kt * T::kStep + ((wid * Tile::kCopies + i) * 64 + lane) / Tile::kRowChunks;
-      row[i] = k < count ? row_of(perm, order, hk, M, first + k) : -1;
-    }
-  }
+  __device__ __forceinline__ const int32_t* task_at(int k) const { return rows.perm + first + (k < count ? k : count - 1); }
   __device__ __forceinline__ void copy(unsigned char* st, int at, int64_t, int kt, int K, int wid, int lane) const {
     const int to = at + this->lds;
 #pragma unroll
     for (int i = 0; i < Tile::kCopies; ++i) {
-      const char* const p = K > 0 && row[i] >= 0 ? from + row[i] * ld + col[i] : (const char*)&tile_zeros;
+      const int lrow = ((wid * Tile::kCopies + i) * 64 + lane) / Tile::kRowChunks, k = kt * T::kStep + lrow;
+      int row = first + k;
+      bool there = k < K;
+      if constexpr (GATHER) {
+        row = rows.of(row, tasks[kt & 1][lrow]);
+        there &= row >= 0;
+      }
+      const char* const p = there ? from + (row * ld + col[i]) : (const char*)&tile_zeros;
       __builtin_amdgcn_global_load_lds((const void*)p, (tg_lds_ptr)(st + (to + i * 1024)), 16, 0, 0);
     }
-    if (K > 0) look(kt + 1, wid, lane);
+    if constexpr (GATHER && FETCH)
+      if (wid == 0 && (kt + 1) * T::kStep < K)
+        __builtin_amdgcn_global_load_lds((const void*)task_at((kt + 1) * T::kStep + lane), (tg_lds_ptr)tasks[(kt + 1) & 1], 4,
+                                         0, 0);
   }
 };
 
 struct GroupedArgs {
   const void *in, *w;
   void* out;
-  const int32_t *offsets, *perm;
+  const int32_t* offsets;
   int N, M, k, n;  // k: the summed width, n: the result's
-  int hk, in_order, out_order;
+  RowOrder in_rows, out_rows;
 };
 
-// TM positions x TN weight rows a workgroup (SWIGLU: TN / 2 gate rows and the same features' up rows, in blocks of 32 in
-// turn, so that a wave holds both). TRANSPOSED: the summed index is the weights' row (dx).
+// TM positions x TN weight rows of a workgroup of WR x WC waves (SWIGLU: TN / 2 gate rows and the same features' up rows, in
+// blocks of 32 in turn, so that a wave holds both). TRANSPOSED: the summed index is the weights' row (dx).
 template <class T, int TM, int TN, int WR, int WC, bool TRANSPOSED, bool SWIGLU>
-__global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs p) {
-  constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32, FN = SWIGLU ? TN / 2 : TN;
+__device__ __forceinline__ void grouped_tile(const GroupedArgs& p, const RowUnit& u, int n0, unsigned char* st0,
+                                             unsigned char* st1) {
+  constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
   static_assert(!SWIGLU || (NI % 2 == 0 && !TRANSPOSED), "a wave's gate and up rows");
   typedef typename T::elem elem;
-  __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
-  const int tiles_n = (p.n + FN - 1) / FN;
-  // neighbouring tiles, which share rows or weights, go to one XCD
-  RowUnit u;
-  int tile = -1;
-  find_unit<64 * NW>(p.offsets, p.N, p.M, TM, (int*)st0, [&](int total) {
-    const int64_t all = (int64_t)total * tiles_n;
-    if (blockIdx.x >= all) return -1;
-    const unsigned item = (unsigned)xcd_contiguous(blockIdx.x, all), unit = item / (unsigned)tiles_n;
-    tile = __builtin_amdgcn_readfirstlane((int)(item - unit * tiles_n));
-    return (int)unit;
-  }, u);
-  if (tile < 0) return;
-  __syncthreads();
-  const int n0 = tile * FN;
   int a0[NI], b0[MJ];
 #pragma unroll
   for (int j = 0; j < MJ; ++j) b0[j] = (wr * MJ + j) * 32;
@@ -131,7 +123,7 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs 
   tile_zero(acc);
   RowOperand<T, TM, NW> b;
   b.init(p.in, p.k, wid, lane, [&](int r) {
-    const int row = row_of(p.perm, p.in_order, p.hk, p.M, u.first + (r < u.count ? r : u.count - 1));
+    const int row = p.in_rows(u.first + (r < u.count ? r : u.count - 1));
     return row < 0 ? 0 : row;
   });
   TileOperand<T, TN, TRANSPOSED, NW> a;
@@ -149,7 +141,7 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs 
   for (int j = 0; j < MJ; ++j) {
     const int r = b0[j] + (lane & 31);
     if (r >= u.count) continue;
-    const int row = row_of(p.perm, p.out_order, p.hk, p.M, u.first + r);
+    const int row = p.out_rows(u.first + r);
     if (row < 0) continue;
     elem* const out = (elem*)p.out + (int64_t)row * p.n;
 #pragma unroll
@@ -169,18 +161,44 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs 
   }
 }
 
+// An expert's last unit is rarely whole: tiles of 256 rows take one of up to 128 or 64 as a tile of that many.
+template <class T, int TM, int TN, int WR, int WC, bool TRANSPOSED, bool SWIGLU>
+__global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs p) {
+  constexpr int FN = SWIGLU ? TN / 2 : TN;
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
+  const int tiles_n = (p.n + FN - 1) / FN;
+  // neighbouring tiles, which share rows or weights, go to one XCD
+  RowUnit u;
+  int tile = -1;
+  find_unit<64 * WR * WC>(p.offsets, p.N, p.M, TM, (int*)st0, [&](int total) {
+    const int64_t all = (int64_t)total * tiles_n;
+    if (blockIdx.x >= all) return -1;
+    const unsigned item = (unsigned)xcd_contiguous(blockIdx.x, all), unit = item / (unsigned)tiles_n;
+    tile = __builtin_amdgcn_readfirstlane((int)(item - unit * tiles_n));
+    return (int)unit;
+  }, u);
+  if (tile < 0) return;
+  __syncthreads();
+  if constexpr (TM == 256) {
+    if (u.count <= 64) return grouped_tile<T, 64, TN, WR, WC, TRANSPOSED, SWIGLU>(p, u, tile * FN, st0, st1);
+    if (u.count <= 128) return grouped_tile<T, 128, TN, WR, WC, TRANSPOSED, SWIGLU>(p, u, tile * FN, st0, st1);
+  }
+  grouped_tile<T, TM, TN, WR, WC, TRANSPOSED, SWIGLU>(p, u, tile * FN, st0, st1);
+}
+
 // 16 RB weight rows (SWIGLU: half of them gate rows, in turn) for a unit of up to sixteen positions.
-template <bool BF16, int RB, bool SWIGLU>
-__global__ __launch_bounds__(256) void grouped_few_kernel(GroupedArgs p, int groups) {
-  constexpr int W = 4, E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4, FB = SWIGLU ? RB / 2 : RB;
+template <bool BF16, int RB, bool SWIGLU, int W>
+__global__ __launch_bounds__(64 * W) void grouped_few_kernel(GroupedArgs p, int groups) {
+  constexpr int E = Chunk<BF16>::kElems, kSize = BF16 ? 2 : 4, FB = SWIGLU ? RB / 2 : RB;
   typedef typename std::conditional<BF16, uint16_t, float>::type elem;
   __shared__ f32x4 tiles[W][RB][64];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int want = blockIdx.x / (unsigned)groups, f0 = (int)(blockIdx.x % (unsigned)groups) * 16 * FB;
   RowUnit u;
-  if (find_unit<256>(p.offsets, p.N, p.M, 16, (int*)tiles, [&](int) { return want; }, u) <= want) return;
+  if (find_unit<64 * W>(p.offsets, p.N, p.M, 16, (int*)tiles, [&](int) { return want; }, u) <= want) return;
   __syncthreads();
-  const int at = row_of(p.perm, p.in_order, p.hk, p.M, u.first + ((l & 15) < u.count ? (l & 15) : u.count - 1));
+  const int pos = u.first + ((l & 15) < u.count ? (l & 15) : u.count - 1), task = p.in_rows.task(pos);
+  const int at = p.in_rows.of(pos, task);
   const uint4* const tok[1] = {(const uint4*)((const char*)p.in + (int64_t)(at < 0 ? 0 : at) * p.k * kSize)};
   const uint4* row[RB];
   const char* const weights = (const char*)p.w + (int64_t)u.expert * (SWIGLU ? 2 : 1) * p.n * p.k * kSize;
@@ -193,7 +211,7 @@ __global__ __launch_bounds__(256) void grouped_few_kernel(GroupedArgs p, int gro
   wave_tile<BF16, RB, 1, 1, W>(row, tok, p.k / E, w, acc);
   add_tiles(acc, tiles, w, l);
   if (w || (l & 15) >= u.count) return;
-  const int to = row_of(p.perm, p.out_order, p.hk, p.M, u.first + (l & 15));
+  const int to = p.out_rows.of(pos, task);
   if (to < 0) return;
   elem* const out = (elem*)p.out + (int64_t)to * p.n;
 #pragma unroll
@@ -204,7 +222,7 @@ __global__ __launch_bounds__(256) void grouped_few_kernel(GroupedArgs p, int gro
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[e] = acc[b][e];
-      if constexpr (SWIGLU) v[e] = activation(1, v[e]) * acc[b + 1][e];
+      if constexpr (SWIGLU) v[e] = activation(1, v[e]) * acc[b + (SWIGLU ? 1 : 0)][e];
     }
     store4(out + f, v[0], v[1], v[2], v[3]);
   }
@@ -214,23 +232,25 @@ struct GroupedSumArgs {
   const void *x, *dy;
   void* dw;
   float* part;  // [parts][N][n][k]
-  const int32_t *offsets, *perm;
-  int N, M, n, k, hk, x_order, y_order, parts;
+  const int32_t* offsets;
+  int N, M, n, k;
+  RowOrder x_rows, y_rows;
+  int parts;
 };
 
 // A tile of dW_e: TM of y's columns x TN of x's, one part of e's positions.
-template <class T, int TM, int TN, int WR, int WC>
+template <class T, int TM, int TN, int WR, int WC, bool GATHER>
 __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArgs p) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
   typedef typename T::elem elem;
   __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
   const int tiles_k = (p.k + TN - 1) / TN, tiles_n = (p.n + TM - 1) / TM;
-  const int64_t item = xcd_contiguous(blockIdx.x, gridDim.x);
-  const int tk = (int)(item % tiles_k), tn = (int)(item / tiles_k % tiles_n);
-  const int64_t rest = item / ((int64_t)tiles_k * tiles_n);
-  const int part = (int)(rest % p.parts), e = (int)(rest / p.parts);
-  const int lo = expert_start(p.offsets, e, p.N, p.M), hi = expert_start(p.offsets, e + 1, p.N, p.M);
+  const unsigned item = (unsigned)xcd_contiguous(blockIdx.x, gridDim.x), strip = item / (unsigned)tiles_k;
+  const unsigned rest = strip / (unsigned)tiles_n;
+  const int tk = (int)(item - strip * tiles_k), tn = (int)(strip - rest * tiles_n);
+  const int e = (int)(rest / (unsigned)p.parts), part = (int)(rest - e * (unsigned)p.parts);
+  const int lo = expert_start(p.offsets, e, p.M), hi = expert_start(p.offsets, e + 1, p.M);
   const int rows = hi > lo ? hi - lo : 0, per = ((rows + p.parts - 1) / p.parts + 63) / 64 * 64;
   const int64_t skip = (int64_t)part * per;
   const int first = (int)(lo + skip), count = skip >= rows ? 0 : rows - skip < per ? (int)(rows - skip) : per;
@@ -241,10 +261,15 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArg
   for (int i = 0; i < NI; ++i) a0[i] = (wc * NI + i) * 32;
   tg_f32x16 acc[NI][MJ];
   tile_zero(acc);
-  SumOperand<T, TN, NW> a;
-  SumOperand<T, TM, NW> b;
-  a.init(p.x, p.k, tk * TN, p.perm, p.x_order, p.hk, p.M, first, count, wid, lane);
-  b.init(p.dy, p.n, tn * TM, p.perm, p.y_order, p.hk, p.M, first, count, wid, lane);
+  __shared__ int tasks[2][64];
+  SumOperand<T, TN, NW, GATHER, false> a;
+  SumOperand<T, TM, NW, GATHER, true> b;
+  a.init(p.x, p.k, tk * TN, p.x_rows, first, count, tasks, wid, lane);
+  b.init(p.dy, p.n, tn * TM, p.y_rows, first, count, tasks, wid, lane);
+  if (GATHER && count) {
+    if (wid == 0) tasks[0][lane] = *b.task_at(lane);
+    __syncthreads();
+  }
   const TileRange all[2] = {{count, 0, 0}, {0, 0, 0}};
   tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
 #pragma unroll
@@ -286,6 +311,7 @@ int64_t most_units(int64_t M, int N, int R) {
   const int64_t n = M / R + N;
   return n < M ? n : M;
 }
+RowOrder rows(const Shape& s, const int32_t* perm, int order) { return RowOrder::make(perm, (int)s.M, order, s.hk); }
 int64_t cut(int64_t v, int64_t by) { return (v + by - 1) / by; }
 
 // The tile's side by how many tiles of 256 or 128 the sizes make.
@@ -311,15 +337,31 @@ hipError_t tiles(const GroupedArgs& p, hipStream_t st) {
     if (side == 256) return go(grouped_tile_kernel<T, 256, 256, 2, 4, TRANSPOSED, SWIGLU>, 256, 256, 512);
     if (side == 128) return go(grouped_tile_kernel<T, 128, 128, 4, 2, TRANSPOSED, SWIGLU>, 128, 128, 512);
   }
+  static const int env = getenv("TS") ? atoi(getenv("TS")) : 0;
+  if constexpr (!SWIGLU) {
+    if (env == 1) return go(grouped_tile_kernel<T, 64, 64, 2, 2, TRANSPOSED, SWIGLU>, 64, 64, 256);
+    if (env == 2) return go(grouped_tile_kernel<T, 32, 64, 1, 2, TRANSPOSED, SWIGLU>, 32, 64, 128);
+    if (env == 3) return go(grouped_tile_kernel<T, 32, 128, 1, 4, TRANSPOSED, SWIGLU>, 32, 128, 256);
+  }
   return go(grouped_tile_kernel<T, 64, 128, 2, 2, TRANSPOSED, SWIGLU>, 64, 128, 256);
 }
 
+template <bool BF16, bool SWIGLU, int RB, int W>
+hipError_t few_launch(const GroupedArgs& p, int64_t units, hipStream_t st) {
+  const int64_t groups = cut(p.n, SWIGLU ? 8 * RB : 16 * RB), grid = units * groups;
+  hipLaunchKernelGGL((grouped_few_kernel<BF16, RB, SWIGLU, W>), dim3((unsigned)grid), dim3(64 * W), 0, st, p, (int)groups);
+  return hipGetLastError();
+}
+// Two row blocks a workgroup, one where two would leave compute units idle (a matrix of 2048 x 8192, one token: 13.7 us
+// instead of 19.3); eight waves where each has four steps of its loads in flight (64 experts of 2048 x 2048, 4 and 64
+// tokens: 47 and 121 us, with four waves 54 and 126), else four (16 fp32 experts of 512 x 1024, 8 tokens: 8.4 us, with eight
+// 10.1). Four row blocks: 62 and 144 us.
 template <bool BF16, bool SWIGLU>
 hipError_t few(const GroupedArgs& p, hipStream_t st) {
-  constexpr int RB = 2;
-  const int64_t groups = cut(p.n, SWIGLU ? 8 * RB : 16 * RB), grid = most_units(p.M, p.N, 16) * groups;
-  hipLaunchKernelGGL((grouped_few_kernel<BF16, RB, SWIGLU>), dim3((unsigned)grid), dim3(256), 0, st, p, (int)groups);
-  return hipGetLastError();
+  const int64_t units = most_units(p.M, p.N, 16), blocks = units * cut((SWIGLU ? 2 : 1) * p.n, 16);
+  constexpr int kLeast = SWIGLU ? 2 : 1;
+  if (p.k / Chunk<BF16>::kElems < 256) return few_launch<BF16, SWIGLU, 2, 4>(p, units, st);
+  return blocks >= 512 ? few_launch<BF16, SWIGLU, 2, 8>(p, units, st) : few_launch<BF16, SWIGLU, kLeast, 8>(p, units, st);
 }
 
 template <class T>
@@ -342,7 +384,7 @@ int sum_parts(const Shape& s, int k, int n) {
   return parts < 1 ? 1 : parts > 32 ? 32 : (int)parts;
 }
 
-template <class T>
+template <class T, bool GATHER>
 hipError_t sums(const GroupedSumArgs& p, int side, hipStream_t st) {
   auto go = [&](auto kernel, int threads) -> hipError_t {
     const int64_t grid = (int64_t)p.N * p.parts * cut(p.k, side) * cut(p.n, side);
@@ -352,10 +394,10 @@ hipError_t sums(const GroupedSumArgs& p, int side, hipStream_t st) {
   };
   hipError_t e = hipSuccess;
   if constexpr (T::kSize == 2) {
-    if (side == 256) e = go(grouped_sum_kernel<T, 256, 256, 2, 4>, 512);
-    else if (side == 128) e = go(grouped_sum_kernel<T, 128, 128, 2, 4>, 512);
+    if (side == 256) e = go(grouped_sum_kernel<T, 256, 256, 2, 4, GATHER>, 512);
+    else if (side == 128) e = go(grouped_sum_kernel<T, 128, 128, 2, 4, GATHER>, 512);
   }
-  if (side == 64) e = go(grouped_sum_kernel<T, 64, 64, 2, 2>, 256);
+  if (side == 64) e = go(grouped_sum_kernel<T, 64, 64, 2, 2, GATHER>, 256);
   if (e || p.parts == 1) return e;
   const int64_t size = (int64_t)p.N * p.n * p.k, blocks = cut(size, 1024);
   hipLaunchKernelGGL(grouped_add_kernel<T>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, st, p.part, p.dw,
@@ -367,13 +409,13 @@ hipError_t sums(const GroupedSumArgs& p, int side, hipStream_t st) {
 
 hipError_t launch_grouped_product(const Shape& s, const ProductShape& q, const void* x, const void* w,
                                   const int32_t* offsets, const int32_t* perm, void* y, hipStream_t st) {
-  const GroupedArgs p{x, w, y, offsets, perm, (int)s.N, (int)s.M, q.n_in, q.n_out, s.hk, q.x_order, q.y_order};
+  const GroupedArgs p{x, w, y, offsets, (int)s.N, (int)s.M, q.n_in, q.n_out, rows(s, perm, q.x_order), rows(s, perm, q.y_order)};
   return s.bf16 ? forward<BF16>(p, q.swiglu, st) : forward<F32>(p, q.swiglu, st);
 }
 
 hipError_t launch_grouped_dx(const Shape& s, const ProductShape& q, const void* dy, const void* w, const int32_t* offsets,
                              const int32_t* perm, void* dx, hipStream_t st) {
-  const GroupedArgs p{dy, w, dx, offsets, perm, (int)s.N, (int)s.M, q.n_out, q.n_in, s.hk, q.y_order, q.x_order};
+  const GroupedArgs p{dy, w, dx, offsets, (int)s.N, (int)s.M, q.n_out, q.n_in, rows(s, perm, q.y_order), rows(s, perm, q.x_order)};
   return s.bf16 ? tiles<BF16, true, false>(p, st) : tiles<F32, true, false>(p, st);
 }
 
@@ -384,10 +426,11 @@ size_t grouped_dw_ws_bytes(const Shape& s, const ProductShape& q) {
 
 hipError_t launch_grouped_dw(const Shape& s, const ProductShape& q, const void* x, const void* dy, const int32_t* offsets,
                              const int32_t* perm, void* dw, void* ws, hipStream_t st) {
-  const GroupedSumArgs p{x, dy, dw, (float*)ws, offsets, perm, (int)s.N, (int)s.M, q.n_out, q.n_in, s.hk, q.x_order,
-                         q.y_order, sum_parts(s, q.n_in, q.n_out)};
+  const GroupedSumArgs p{x, dy, dw, (float*)ws, offsets, (int)s.N, (int)s.M, q.n_out, q.n_in, rows(s, perm, q.x_order),
+                         rows(s, perm, q.y_order), sum_parts(s, q.n_in, q.n_out)};
   const int side = sum_side(s, q.n_in, q.n_out);
-  return s.bf16 ? sums<BF16>(p, side, st) : sums<F32>(p, side, st);
+  if (perm) return s.bf16 ? sums<BF16, true>(p, side, st) : sums<F32, true>(p, side, st);
+  return s.bf16 ? sums<BF16, false>(p, side, st) : sums<F32, false>(p, side, st);
 }
 
 }  // namespace omnimoe

@@ -18,18 +18,51 @@ __device__ __forceinline__ void load8(const void* x, int64_t i, float (&v)[8]) {
   }
 }
 
+// Two values rounded to bf16, to nearest even, in one instruction (v_cvt_pk_bf16_f32).
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
+}
+
 // (bf16: rounded to nearest even)
 template <bool BF16>
 __device__ __forceinline__ void store8(void* x, int64_t i, const float (&v)[8]) {
   if constexpr (BF16) {
-    uint32_t w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)bf16_rne(v[2 * e]) | ((uint32_t)bf16_rne(v[2 * e + 1]) << 16);
-    *(uint4*)((uint16_t*)x + i) = make_uint4(w[0], w[1], w[2], w[3]);
+    *(uint4*)((uint16_t*)x + i) =
+        make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
   } else {
     *(float4*)((float*)x + i) = make_float4(v[0], v[1], v[2], v[3]);
     *(float4*)((float*)x + i + 4) = make_float4(v[4], v[5], v[6], v[7]);
   }
 }
+
+// The same as they lie in memory, for a load that is used later.
+template <bool BF16>
+struct Raw8 {
+  uint4 q[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const void* x, int64_t i) {
+    const uint4* const p = (const uint4*)((const char*)x + i * (BF16 ? 2 : 4));
+#pragma unroll
+    for (int k = 0; k < (BF16 ? 1 : 2); ++k) q[k] = p[k];
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int k = 0; k < (BF16 ? 1 : 2); ++k) q[k] = make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    if constexpr (BF16) {
+      v[0] = bf16_lo(q[0].x); v[1] = bf16_hi(q[0].x); v[2] = bf16_lo(q[0].y); v[3] = bf16_hi(q[0].y);
+      v[4] = bf16_lo(q[0].z); v[5] = bf16_hi(q[0].z); v[6] = bf16_lo(q[0].w); v[7] = bf16_hi(q[0].w);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        v[4 * k] = __uint_as_float(q[k].x);
+        v[4 * k + 1] = __uint_as_float(q[k].y);
+        v[4 * k + 2] = __uint_as_float(q[k].z);
+        v[4 * k + 3] = __uint_as_float(q[k].w);
+      }
+    }
+  }
+};
 
 }  // namespace omnimoe

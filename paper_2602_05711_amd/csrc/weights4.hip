@@ -81,8 +81,9 @@ struct Product4Args {
   const void* x;
   const uint8_t *codes, *scales;
   void* y;
-  const int32_t *offsets, *perm;
-  int N, M, k, n, hk, x_order, y_order;
+  const int32_t* offsets;
+  int N, M, k, n;
+  RowOrder x_rows, y_rows;
 };
 
 // Eight codes of a lane's block against eight values of each operand's block.
@@ -119,21 +120,50 @@ struct Codes8<false> {
   }
 };
 
+// The scale bytes of U steps of a lane's row (4 U neighbouring blocks, WIDE: one aligned load, the same on the row's four
+// lanes), and a step's as the float 2^s of this lane's block.
+template <int U, bool WIDE>
+struct Scales {
+  uint32_t word[U];
+  __device__ __forceinline__ void load(const uint8_t* row, int block, int quad, int last) {
+    if constexpr (WIDE) {
+      if constexpr (U == 4) {
+        const uint4 v = *(const uint4*)(row + block);
+        word[0] = v.x, word[1] = v.y, word[2] = v.z, word[3] = v.w;
+      } else if constexpr (U == 2) {
+        const uint2 v = *(const uint2*)(row + block);
+        word[0] = v.x, word[1] = v.y;
+      } else {
+        word[0] = *(const uint32_t*)(row + block);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int at = block + 4 * i + quad;
+        word[i] = row[at < last ? at : last];
+      }
+    }
+  }
+  __device__ __forceinline__ float of(int i, int quad) const {
+    const uint32_t v = WIDE ? word[i] >> (8 * quad) : word[i];
+    return __uint_as_float((v << 23) & 0x7F800000u);
+  }
+};
+
 // 16 RB weight rows (SWIGLU: half of them gate rows, in turn) for a unit of up to sixteen positions. A step is 128 values
-// of k, a block of 32 a lane (16 bytes of codes and their scale); a workgroup's waves take steps in turn, U at a time in
-// flight, and their tiles are added in wave order.
-template <bool BF16, int RB, bool SWIGLU, int U>
-__global__ __launch_bounds__(256) void product4_kernel(Product4Args p, int groups) {
-  constexpr int W = 4, kSize = BF16 ? 2 : 4, FB = SWIGLU ? RB / 2 : RB, kChunks = Codes8<BF16>::kChunks;
+// of k, a block of 32 a lane (16 bytes of codes); a workgroup's W waves take U neighbouring steps in turn, all of their codes
+// and scales in flight together, and their tiles are added in wave order.
+template <bool BF16, int RB, bool SWIGLU, int W, int U, bool WIDE>
+__global__ __launch_bounds__(64 * W) void product4_kernel(Product4Args p, int groups) {
+  constexpr int kSize = BF16 ? 2 : 4, FB = SWIGLU ? RB / 2 : RB, kChunks = Codes8<BF16>::kChunks;
   typedef typename std::conditional<BF16, uint16_t, float>::type elem;
   __shared__ f32x4 tiles[W][RB][64];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = l >> 4;
   const int want = blockIdx.x / (unsigned)groups, f0 = (int)(blockIdx.x % (unsigned)groups) * 16 * FB;
   RowUnit u;
-  if (find_unit<256>(p.offsets, p.N, p.M, 16, (int*)tiles, [&](int) { return want; }, u) <= want) return;
+  if (find_unit<64 * W>(p.offsets, p.N, p.M, 16, (int*)tiles, [&](int) { return want; }, u) <= want) return;
   __syncthreads();
-  const int at = row_of(p.perm, p.x_order, p.hk, p.M, u.first + ((l & 15) < u.count ? (l & 15) : u.count - 1));
-  const char* const tok = (const char*)p.x + (int64_t)(at < 0 ? 0 : at) * p.k * kSize;
+  const int pos = u.first + ((l & 15) < u.count ? (l & 15) : u.count - 1), task = p.x_rows.task(pos);
   const int nb = p.k / 32;
   int64_t row[RB];  // blocks before this lane's weight rows
 #pragma unroll
@@ -144,43 +174,48 @@ __global__ __launch_bounds__(256) void product4_kernel(Product4Args p, int group
   f32x4 acc[RB];
 #pragma unroll
   for (int b = 0; b < RB; ++b) acc[b] = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = w * U; s0 * 4 < nb; s0 += W * U) {
+  auto steps = [&](int s0, auto whole) {
+    constexpr bool kWhole = decltype(whole)::value;
     uint4 code[U][RB];
-    float scale[U][RB];
+    Scales<U, WIDE> scale[RB];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int block = (s0 + i) * 4 + quad, there = block < nb ? block : nb - 1;
+    for (int b = 0; b < RB; ++b) {
+      scale[b].load(p.scales + row[b], s0 * 4, quad, nb - 1);
 #pragma unroll
-      for (int b = 0; b < RB; ++b) {
-        code[i][b] = *(const uint4*)(p.codes + (row[b] + there) * 16);
-        scale[i][b] = __uint_as_float((uint32_t)p.scales[row[b] + there] << 23);
-        if (block >= nb) {
-          code[i][b] = make_uint4(0, 0, 0, 0);
-          scale[i][b] = 1.0f;
-        }
+      for (int i = 0; i < U; ++i) {
+        const int block = (s0 + i) * 4 + quad;
+        code[i][b] = *(const uint4*)(p.codes + (row[b] + (kWhole || block < nb ? block : nb - 1)) * 16);
       }
     }
+    const int at = p.x_rows.of(pos, task);
+    const char* const tok = (const char*)p.x + (int64_t)(at < 0 ? 0 : at) * p.k * kSize;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int block = (s0 + i) * 4 + quad, there = block < nb ? block : nb - 1;
+      const int block = (s0 + i) * 4 + quad;
+      const bool there = kWhole || block < nb;
       uint4 x[kChunks];
 #pragma unroll
-      for (int c = 0; c < kChunks; ++c) {
-        x[c] = *(const uint4*)(tok + (int64_t)there * 32 * kSize + c * 16);
-        if (block >= nb) x[c] = make_uint4(0, 0, 0, 0);
-      }
+      for (int c = 0; c < kChunks; ++c) x[c] = *(const uint4*)(tok + (int64_t)(there ? block : nb - 1) * 32 * kSize + c * 16);
+      if (!there)  // (both operands: an infinity times a zero would not be one)
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) x[c] = make_uint4(0, 0, 0, 0);
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
-        Codes8<BF16>::mma(acc[b], code[i][b].x, scale[i][b], x, 0);
-        Codes8<BF16>::mma(acc[b], code[i][b].y, scale[i][b], x, 1);
-        Codes8<BF16>::mma(acc[b], code[i][b].z, scale[i][b], x, 2);
-        Codes8<BF16>::mma(acc[b], code[i][b].w, scale[i][b], x, 3);
+        const float f = there ? scale[b].of(i, quad) : 1.0f;
+        const uint4 q = there ? code[i][b] : make_uint4(0, 0, 0, 0);
+        Codes8<BF16>::mma(acc[b], q.x, f, x, 0);
+        Codes8<BF16>::mma(acc[b], q.y, f, x, 1);
+        Codes8<BF16>::mma(acc[b], q.z, f, x, 2);
+        Codes8<BF16>::mma(acc[b], q.w, f, x, 3);
       }
     }
-  }
+  };
+  int s0 = w * U;
+  for (; (s0 + U) * 4 <= nb; s0 += W * U) steps(s0, std::true_type{});
+  if (s0 * 4 < nb) steps(s0, std::false_type{});
   add_tiles(acc, tiles, w, l);
   if (w || (l & 15) >= u.count) return;
-  const int to = row_of(p.perm, p.y_order, p.hk, p.M, u.first + (l & 15));
+  const int to = p.y_rows.of(pos, task);
   if (to < 0) return;
   elem* const out = (elem*)p.y + (int64_t)to * p.n;
 #pragma unroll
@@ -191,20 +226,40 @@ __global__ __launch_bounds__(256) void product4_kernel(Product4Args p, int group
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[e] = acc[b][e];
-      if constexpr (SWIGLU) v[e] = activation(1, v[e]) * acc[b + 1][e];
+      if constexpr (SWIGLU) v[e] = activation(1, v[e]) * acc[b + (SWIGLU ? 1 : 0)][e];
     }
     store4(out + f, v[0], v[1], v[2], v[3]);
   }
 }
 
+template <bool BF16, bool SWIGLU, int RB, int W, int U>
+hipError_t product4_launch(const Product4Args& p, int64_t units, hipStream_t st) {
+  const int64_t per = SWIGLU ? 8 * RB : 16 * RB, groups = (p.n + per - 1) / per, grid = units * groups;
+  if (grid > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+  const dim3 blocks((unsigned)grid), threads(64 * W);
+  if (p.k / 32 % (4 * U) == 0)
+    hipLaunchKernelGGL((product4_kernel<BF16, RB, SWIGLU, W, U, true>), blocks, threads, 0, st, p, (int)groups);
+  else
+    hipLaunchKernelGGL((product4_kernel<BF16, RB, SWIGLU, W, U, false>), blocks, threads, 0, st, p, (int)groups);
+  return hipGetLastError();
+}
+
+// Row blocks a workgroup: four where that leaves a thousand workgroups (four a compute unit), two from 256 on, or one (the
+// SwiGLU's two), with the steps spread over eight waves. 64 experts, n_in = 2048, n_out = 1024, SwiGLU: 16 tokens 29.6 us
+// with four blocks and 32.3 with two, one token 8.6 and 7.7; one matrix of 2048 x 8192, one token: 18.3, 12.0 and, with
+// one, 7.8 us. fp32 weights keep the matrix cores busy (eight products for one of bf16): one block, 7 tokens,
+// 2080 x 2056: 7.2 us, with two blocks on four waves 10.5.
 template <bool BF16, bool SWIGLU>
 hipError_t product4(const Product4Args& p, hipStream_t st) {
-  constexpr int RB = 2, U = 2;
-  const int64_t units = p.M / 16 + p.N < p.M ? p.M / 16 + p.N : p.M, per = SWIGLU ? 8 * RB : 16 * RB;
-  const int64_t groups = (p.n + per - 1) / per, grid = units * groups;
-  if (grid > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((product4_kernel<BF16, RB, SWIGLU, U>), dim3((unsigned)grid), dim3(256), 0, st, p, (int)groups);
-  return hipGetLastError();
+  const int64_t units = p.M / 16 + p.N < p.M ? p.M / 16 + p.N : p.M, blocks = units * (((SWIGLU ? 2 : 1) * p.n + 15) / 16);
+  constexpr int kLeast = SWIGLU ? 2 : 1;
+  if constexpr (BF16) {
+    if (blocks >= 4096) return product4_launch<true, SWIGLU, 4, 4, 4>(p, units, st);
+    if (blocks >= 512) return product4_launch<true, SWIGLU, 2, 4, 2>(p, units, st);
+    return product4_launch<true, SWIGLU, kLeast, 8, 2>(p, units, st);
+  } else {
+    return product4_launch<false, SWIGLU, kLeast, 8, 1>(p, units, st);
+  }
 }
 
 unsigned grid_of(int64_t threads) {
@@ -235,7 +290,8 @@ hipError_t launch_weights4_load(const Shape& s, const ProductShape& q, const uin
 hipError_t launch_grouped_product4(const Shape& s, const ProductShape& q, const void* x, const uint8_t* codes,
                                    const uint8_t* scales, const int32_t* offsets, const int32_t* perm, void* y,
                                    hipStream_t st) {
-  const Product4Args p{x, codes, scales, y, offsets, perm, (int)s.N, (int)s.M, q.n_in, q.n_out, s.hk, q.x_order, q.y_order};
+  const Product4Args p{x, codes, scales, y, offsets, (int)s.N, (int)s.M, q.n_in, q.n_out,
+                       RowOrder::make(perm, (int)s.M, q.x_order, s.hk), RowOrder::make(perm, (int)s.M, q.y_order, s.hk)};
   if (s.bf16) return q.swiglu ? product4<true, true>(p, st) : product4<true, false>(p, st);
   return q.swiglu ? product4<false, true>(p, st) : product4<false, false>(p, st);
 }
