@@ -7,11 +7,12 @@
 // Few rows an expert: the time is that of reading the weights of the experts that have rows, and of little beside it
 // (few_tile.hpp): a unit is up to sixteen rows, a workgroup takes 32 weight rows and splits the summed index over its waves.
 // Sums are fp32, rounded once; every result has one order of summation, so that it is the same on every run.
-#include <stdlib.h>
 #include "few_tile.hpp"
 #include "grouped_rows.hpp"
 #include "internal.hpp"
 #include "tile_gemm.hpp"
+#include "tile_turns.hpp"
+#include "vec8.hpp"
 
 namespace omnimoe {
 namespace {
@@ -49,51 +50,57 @@ struct RowOperand : TileOperand<T, R, false, NW> {
   }
 };
 
-// Rows as the summed index: stage kt holds positions first + kt kStep .. of `count`, R of their columns. GATHER: the entries
-// of perm that a stage's copies go by lie in LDS, tasks[kt % 2], from the stage before on: a load into registers would have
-// to be waited for behind the copies issued before it. Both operands go by the same entries, and the one that is copied
-// last (FETCH) has the next stage's brought by wave 0.
-template <class T, int R, int NW, bool GATHER, bool FETCH>
+// The rows that the stages' positions name, by x's order and by dy's, in LDS: rows[kt % 2] from the stage before kt on. Wave 0
+// brings them, a position a lane: the entry of perm for stage kt + 2 is loaded while stage kt is copied, and looked at a
+// stage later, when nothing has to be waited for (loads return in order, behind the copies issued before them).
+struct SumRows {
+  RowOrder x, dy;
+  int first, count;
+  int2 (*rows)[64];
+  int next;  // (lane's entry of the stage after the next)
+
+  __device__ __forceinline__ void fetch(int k) {
+    if (x.perm) next = x.perm[first + (k < count ? k : count - 1)];
+  }
+  __device__ __forceinline__ void put(int slot, int k) {
+    const int p = first + k, t = x.perm ? next : p;
+    rows[slot][lane_id()] = k < count ? make_int2(x.of(p, t), dy.of(p, t)) : make_int2(-1, -1);
+  }
+};
+
+// Rows as the summed index: stage kt holds positions first + kt kStep .. of `count`, R of their columns.
+template <class T, int R, int NW, bool DY>
 struct SumOperand : TileOperand<T, R, true, NW> {
   typedef TileOperand<T, R, true, NW> Tile;
   static_assert(T::kStep <= 64, "a wave's lanes");
-  const char* from;
-  int64_t ld;
-  uint32_t col[Tile::kCopies];
-  RowOrder rows;
-  int first, count;
-  int (*tasks)[64];
+  const char* from[Tile::kCopies];
+  int ld;
+  SumRows* rows;
 
-  __device__ __forceinline__ void init(const void* p, int width, int c0, const RowOrder& rows_, int first_, int count_,
-                                       int (&tasks_)[2][64], int wid, int lane) {
-    from = (const char*)p, ld = (int64_t)width * T::kSize, rows = rows_, first = first_, count = count_, tasks = tasks_;
+  __device__ __forceinline__ void init(const void* p, int width, int c0, SumRows* rows_, int wid, int lane) {
+    ld = width * T::kSize, rows = rows_;
     this->lds = wid * Tile::kCopies * 1024;
 #pragma unroll
     for (int i = 0; i < Tile::kCopies; ++i) {
       const int at = (wid * Tile::kCopies + i) * 64 + lane, lrow = at / Tile::kRowChunks;
       const int c = c0 + Tile::place(lrow, at % Tile::kRowChunks) * Tile::kPer;
-      col[i] = (uint32_t)((c < width ? c : width - Tile::kPer) * T::kSize);
+      from[i] = (const char*)p + (int64_t)(c < width ? c : width - Tile::kPer) * T::kSize;
     }
   }
-  __device__ __forceinline__ const int32_t* task_at(int k) const { return rows.perm + first + (k < count ? k : count - 1); }
   __device__ __forceinline__ void copy(unsigned char* st, int at, int64_t, int kt, int K, int wid, int lane) const {
     const int to = at + this->lds;
 #pragma unroll
     for (int i = 0; i < Tile::kCopies; ++i) {
-      const int lrow = ((wid * Tile::kCopies + i) * 64 + lane) / Tile::kRowChunks, k = kt * T::kStep + lrow;
-      int row = first + k;
-      bool there = k < K;
-      if constexpr (GATHER) {
-        row = rows.of(row, tasks[kt & 1][lrow]);
-        there &= row >= 0;
-      }
-      const char* const p = there ? from + (row * ld + col[i]) : (const char*)&tile_zeros;
+      const int2 both = rows->rows[kt & 1][((wid * Tile::kCopies + i) * 64 + lane) / Tile::kRowChunks];
+      const int row = K > 0 ? (DY ? both.y : both.x) : -1;
+      const char* const p = row >= 0 ? from[i] + (int64_t)row * ld : (const char*)&tile_zeros;
       __builtin_amdgcn_global_load_lds((const void*)p, (tg_lds_ptr)(st + (to + i * 1024)), 16, 0, 0);
     }
-    if constexpr (GATHER && FETCH)
-      if (wid == 0 && (kt + 1) * T::kStep < K)
-        __builtin_amdgcn_global_load_lds((const void*)task_at((kt + 1) * T::kStep + lane), (tg_lds_ptr)tasks[(kt + 1) & 1], 4,
-                                         0, 0);
+    if constexpr (DY)
+      if (wid == 0 && (kt + 1) * T::kStep < K) {
+        rows->put((kt + 1) & 1, (kt + 1) * T::kStep + lane);
+        rows->fetch((kt + 2) * T::kStep + lane);
+      }
   }
 };
 
@@ -109,7 +116,9 @@ struct GroupedArgs {
 // blocks of 32 in turn, so that a wave holds both). TRANSPOSED: the summed index is the weights' row (dx).
 template <class T, int TM, int TN, int WR, int WC, bool TRANSPOSED, bool SWIGLU>
 __device__ __forceinline__ void grouped_tile(const GroupedArgs& p, const RowUnit& u, int n0, unsigned char* st0,
-                                             unsigned char* st1) {
+                                             unsigned char* st1, unsigned char* st2 = nullptr, unsigned char* st3 = nullptr,
+                                             unsigned char* st4 = nullptr, unsigned char* st5 = nullptr) {
+  constexpr bool kTurns = T::kSize == 2 && TM == 256 && TN == 256 && WR == 2 && WC == 4;
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
   static_assert(!SWIGLU || (NI % 2 == 0 && !TRANSPOSED), "a wave's gate and up rows");
   typedef typename T::elem elem;
@@ -121,11 +130,10 @@ __device__ __forceinline__ void grouped_tile(const GroupedArgs& p, const RowUnit
   for (int i = 0; i < NI; ++i) a0[i] = (wc * NI + i) * 32;
   tg_f32x16 acc[NI][MJ];
   tile_zero(acc);
-  RowOperand<T, TM, NW> b;
-  b.init(p.in, p.k, wid, lane, [&](int r) {
+  auto in_row = [&](int r) {
     const int row = p.in_rows(u.first + (r < u.count ? r : u.count - 1));
     return row < 0 ? 0 : row;
-  });
+  };
   TileOperand<T, TN, TRANSPOSED, NW> a;
   const elem* const w = (const elem*)p.w + (int64_t)u.expert * (SWIGLU ? 2 : 1) * p.n * p.k;
   if constexpr (TRANSPOSED)
@@ -135,8 +143,17 @@ __device__ __forceinline__ void grouped_tile(const GroupedArgs& p, const RowUnit
       const int f = n0 + (SWIGLU ? (r >> 6) * 32 + (r & 31) : r), c = f < p.n ? f : p.n - 1;
       return SWIGLU && (r & 32) ? p.n + c : c;
     });
-  const TileRange all[2] = {{p.k, 0, 0}, {0, 0, 0}};
-  tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
+  if constexpr (kTurns) {
+    RowOperand<T, 128, NW> part0, part1;
+    part0.init(p.in, p.k, wid, lane, [&](int r) { return in_row(turn_row(0, r)); });
+    part1.init(p.in, p.k, wid, lane, [&](int r) { return in_row(turn_row(1, r)); });
+    tile_sum_turns<T>(a, part0, part1, p.k, a0, wr, st0, st1, st2, st3, st4, st5, wid, lane, acc);
+  } else {
+    RowOperand<T, TM, NW> b;
+    b.init(p.in, p.k, wid, lane, in_row);
+    const TileRange all[2] = {{p.k, 0, 0}, {0, 0, 0}};
+    tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
+  }
 #pragma unroll
   for (int j = 0; j < MJ; ++j) {
     const int r = b0[j] + (lane & 31);
@@ -154,9 +171,9 @@ __device__ __forceinline__ void grouped_tile(const GroupedArgs& p, const RowUnit
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           v[e] = acc[i][j][4 * q + e];
-          if constexpr (SWIGLU) v[e] = activation(1, v[e]) * acc[i + 1][j][4 * q + e];
+          if constexpr (SWIGLU) v[e] = swiglu<T::kSize == 2>(v[e], acc[i + 1][j][4 * q + e]);
         }
-        store4(out + f, v[0], v[1], v[2], v[3]);
+        put4(out + f, v[0], v[1], v[2], v[3]);
       }
   }
 }
@@ -165,7 +182,11 @@ __device__ __forceinline__ void grouped_tile(const GroupedArgs& p, const RowUnit
 template <class T, int TM, int TN, int WR, int WC, bool TRANSPOSED, bool SWIGLU>
 __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs p) {
   constexpr int FN = SWIGLU ? TN / 2 : TN;
-  __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
+  constexpr bool kTurns = TM == 256;
+  // (by turns: a stage of a in st0 or st1, b's parts in the others; else a stage of both in st0 or st1)
+  constexpr int kStage = kTurns ? 256 * 128 : (TM + TN) * 128, kPart = kTurns ? 128 * 128 : 16;
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[kStage], st1[kStage];
+  __shared__ __attribute__((aligned(1024))) unsigned char st2[kPart], st3[kPart], st4[kPart], st5[kPart];
   const int tiles_n = (p.n + FN - 1) / FN;
   // neighbouring tiles, which share rows or weights, go to one XCD
   RowUnit u;
@@ -179,11 +200,7 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs 
   }, u);
   if (tile < 0) return;
   __syncthreads();
-  if constexpr (TM == 256) {
-    if (u.count <= 64) return grouped_tile<T, 64, TN, WR, WC, TRANSPOSED, SWIGLU>(p, u, tile * FN, st0, st1);
-    if (u.count <= 128) return grouped_tile<T, 128, TN, WR, WC, TRANSPOSED, SWIGLU>(p, u, tile * FN, st0, st1);
-  }
-  grouped_tile<T, TM, TN, WR, WC, TRANSPOSED, SWIGLU>(p, u, tile * FN, st0, st1);
+  grouped_tile<T, TM, TN, WR, WC, TRANSPOSED, SWIGLU>(p, u, tile * FN, st0, st1, st2, st3, st4, st5);
 }
 
 // 16 RB weight rows (SWIGLU: half of them gate rows, in turn) for a unit of up to sixteen positions.
@@ -222,9 +239,9 @@ __global__ __launch_bounds__(64 * W) void grouped_few_kernel(GroupedArgs p, int 
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[e] = acc[b][e];
-      if constexpr (SWIGLU) v[e] = activation(1, v[e]) * acc[b + (SWIGLU ? 1 : 0)][e];
+      if constexpr (SWIGLU) v[e] = swiglu<BF16>(v[e], acc[b + (SWIGLU ? 1 : 0)][e]);
     }
-    store4(out + f, v[0], v[1], v[2], v[3]);
+    put4(out + f, v[0], v[1], v[2], v[3]);
   }
 }
 
@@ -238,22 +255,46 @@ struct GroupedSumArgs {
   int parts;
 };
 
+// Up to 64 experts, a multiple of eight, whose rows may be very uneven: they go to the XCDs by their rank in rows, to and fro
+// (the first eight to XCDs 0 to 7, the next to 7 to 0, ...), so that each has about as many rows, the longest first. All of
+// an expert's tiles stay on one XCD, whose L2 they share. Returns the expert of rank `want`.
+__device__ __forceinline__ int expert_of_rank(const int32_t* offsets, int N, int M, int want) {
+  const int l = lane_id(), e = l < N ? l : N - 1;
+  const int lo = expert_start(offsets, e, M), hi = expert_start(offsets, e + 1, M), rows = l < N ? (hi > lo ? hi - lo : 0) : -1;
+  int rank = 0;
+  for (int i = 0; i < N; ++i) {
+    const int other = __builtin_amdgcn_readlane(rows, i);
+    rank += other > rows || (other == rows && i < l);
+  }
+  return __builtin_ctzll(__ballot(rank == want));
+}
+
 // A tile of dW_e: TM of y's columns x TN of x's, one part of e's positions.
-template <class T, int TM, int TN, int WR, int WC, bool GATHER>
+template <class T, int TM, int TN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArgs p) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
   typedef typename T::elem elem;
   __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
+  __shared__ int2 slots[2][64];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
-  const int tiles_k = (p.k + TN - 1) / TN, tiles_n = (p.n + TM - 1) / TM;
-  const unsigned item = (unsigned)xcd_contiguous(blockIdx.x, gridDim.x), strip = item / (unsigned)tiles_k;
-  const unsigned rest = strip / (unsigned)tiles_n;
-  const int tk = (int)(item - strip * tiles_k), tn = (int)(strip - rest * tiles_n);
-  const int e = (int)(rest / (unsigned)p.parts), part = (int)(rest - e * (unsigned)p.parts);
+  const unsigned tiles_k = (p.k + TN - 1) / TN, tiles_n = (p.n + TM - 1) / TM, each = tiles_k * tiles_n * p.parts;
+  unsigned item;
+  int e;
+  if (p.offsets && p.N <= 64 && p.N % 8 == 0) {
+    const unsigned xcd = blockIdx.x % 8, at = blockIdx.x / 8, turn = at / each;
+    item = at - turn * each;
+    e = __builtin_amdgcn_readfirstlane(expert_of_rank(p.offsets, p.N, p.M, (int)(8 * turn + (turn & 1 ? 7 - xcd : xcd))));
+  } else {
+    const unsigned at = (unsigned)xcd_contiguous(blockIdx.x, gridDim.x);
+    e = (int)(at / each);
+    item = at - e * each;
+  }
+  const unsigned part_ = item / (tiles_k * tiles_n), tile = item - part_ * tiles_k * tiles_n;
+  const int part = (int)part_, tn = (int)(tile / tiles_k), tk = (int)(tile - tn * tiles_k);
   const int lo = expert_start(p.offsets, e, p.M), hi = expert_start(p.offsets, e + 1, p.M);
-  const int rows = hi > lo ? hi - lo : 0, per = ((rows + p.parts - 1) / p.parts + 63) / 64 * 64;
+  const int all_rows = hi > lo ? hi - lo : 0, per = ((all_rows + p.parts - 1) / p.parts + 63) / 64 * 64;
   const int64_t skip = (int64_t)part * per;
-  const int first = (int)(lo + skip), count = skip >= rows ? 0 : rows - skip < per ? (int)(rows - skip) : per;
+  const int first = (int)(lo + skip), count = skip >= all_rows ? 0 : all_rows - skip < per ? (int)(all_rows - skip) : per;
   int a0[NI], b0[MJ];
 #pragma unroll
   for (int j = 0; j < MJ; ++j) b0[j] = (wr * MJ + j) * 32;
@@ -261,13 +302,17 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArg
   for (int i = 0; i < NI; ++i) a0[i] = (wc * NI + i) * 32;
   tg_f32x16 acc[NI][MJ];
   tile_zero(acc);
-  __shared__ int tasks[2][64];
-  SumOperand<T, TN, NW, GATHER, false> a;
-  SumOperand<T, TM, NW, GATHER, true> b;
-  a.init(p.x, p.k, tk * TN, p.x_rows, first, count, tasks, wid, lane);
-  b.init(p.dy, p.n, tn * TM, p.y_rows, first, count, tasks, wid, lane);
-  if (GATHER && count) {
-    if (wid == 0) tasks[0][lane] = *b.task_at(lane);
+  SumRows rows{p.x_rows, p.y_rows, first, count, slots, 0};
+  SumOperand<T, TN, NW, false> a;
+  SumOperand<T, TM, NW, true> b;
+  a.init(p.x, p.k, (int)tk * TN, &rows, wid, lane);
+  b.init(p.dy, p.n, (int)tn * TM, &rows, wid, lane);
+  if (count) {
+    if (wid == 0) {
+      rows.fetch(lane);
+      rows.put(0, lane);
+      rows.fetch(T::kStep + lane);
+    }
     __syncthreads();
   }
   const TileRange all[2] = {{count, 0, 0}, {0, 0, 0}};
@@ -285,7 +330,7 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArg
         const int64_t at = ((int64_t)e * p.n + n) * p.k + k;
         const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
         if (p.parts > 1) *(float4*)(p.part + (int64_t)part * p.N * p.n * p.k + at) = make_float4(v[0], v[1], v[2], v[3]);
-        else store4((elem*)p.dw + at, v[0], v[1], v[2], v[3]);
+        else put4((elem*)p.dw + at, v[0], v[1], v[2], v[3]);
       }
   }
 }
@@ -302,7 +347,7 @@ __global__ __launch_bounds__(256) void grouped_add_kernel(const float* __restric
       v.z += s.z;
       v.w += s.w;
     }
-    store4((typename T::elem*)dw + i, v.x, v.y, v.z, v.w);
+    put4((typename T::elem*)dw + i, v.x, v.y, v.z, v.w);
   }
 }
 
@@ -337,12 +382,7 @@ hipError_t tiles(const GroupedArgs& p, hipStream_t st) {
     if (side == 256) return go(grouped_tile_kernel<T, 256, 256, 2, 4, TRANSPOSED, SWIGLU>, 256, 256, 512);
     if (side == 128) return go(grouped_tile_kernel<T, 128, 128, 4, 2, TRANSPOSED, SWIGLU>, 128, 128, 512);
   }
-  static const int env = getenv("TS") ? atoi(getenv("TS")) : 0;
-  if constexpr (!SWIGLU) {
-    if (env == 1) return go(grouped_tile_kernel<T, 64, 64, 2, 2, TRANSPOSED, SWIGLU>, 64, 64, 256);
-    if (env == 2) return go(grouped_tile_kernel<T, 32, 64, 1, 2, TRANSPOSED, SWIGLU>, 32, 64, 128);
-    if (env == 3) return go(grouped_tile_kernel<T, 32, 128, 1, 4, TRANSPOSED, SWIGLU>, 32, 128, 256);
-  }
+  if constexpr (!SWIGLU) return go(grouped_tile_kernel<T, 64, 64, 2, 2, TRANSPOSED, SWIGLU>, 64, 64, 256);
   return go(grouped_tile_kernel<T, 64, 128, 2, 2, TRANSPOSED, SWIGLU>, 64, 128, 256);
 }
 
@@ -366,7 +406,10 @@ hipError_t few(const GroupedArgs& p, hipStream_t st) {
 
 template <class T>
 hipError_t forward(const GroupedArgs& p, bool swiglu, hipStream_t st) {
-  if (p.M <= 16 * (int64_t)p.N) return swiglu ? few<T::kSize == 2, true>(p, st) : few<T::kSize == 2, false>(p, st);
+  // Up to 64 positions, or six an expert, a pass over the weights for every sixteen of them; then tiles. 2048 x 2048: one
+  // expert, 64 positions 8.5 us, as tiles 12.5; 16 experts, 64 35 and 36, 128 44 and 37; 64 experts, 512 118 and 129, 768 137
+  // and 132. (One expert's tiles are few: 128 positions 13.8 and 18.8, 256 25 and 19.)
+  if (p.M <= 64 || p.M <= 6 * (int64_t)p.N) return swiglu ? few<T::kSize == 2, true>(p, st) : few<T::kSize == 2, false>(p, st);
   return swiglu ? tiles<T, false, true>(p, st) : tiles<T, false, false>(p, st);
 }
 
@@ -384,7 +427,7 @@ int sum_parts(const Shape& s, int k, int n) {
   return parts < 1 ? 1 : parts > 32 ? 32 : (int)parts;
 }
 
-template <class T, bool GATHER>
+template <class T>
 hipError_t sums(const GroupedSumArgs& p, int side, hipStream_t st) {
   auto go = [&](auto kernel, int threads) -> hipError_t {
     const int64_t grid = (int64_t)p.N * p.parts * cut(p.k, side) * cut(p.n, side);
@@ -394,10 +437,10 @@ hipError_t sums(const GroupedSumArgs& p, int side, hipStream_t st) {
   };
   hipError_t e = hipSuccess;
   if constexpr (T::kSize == 2) {
-    if (side == 256) e = go(grouped_sum_kernel<T, 256, 256, 2, 4, GATHER>, 512);
-    else if (side == 128) e = go(grouped_sum_kernel<T, 128, 128, 2, 4, GATHER>, 512);
+    if (side == 256) e = go(grouped_sum_kernel<T, 256, 256, 2, 4>, 512);
+    else if (side == 128) e = go(grouped_sum_kernel<T, 128, 128, 2, 4>, 512);
   }
-  if (side == 64) e = go(grouped_sum_kernel<T, 64, 64, 2, 2, GATHER>, 256);
+  if (side == 64) e = go(grouped_sum_kernel<T, 64, 64, 2, 2>, 256);
   if (e || p.parts == 1) return e;
   const int64_t size = (int64_t)p.N * p.n * p.k, blocks = cut(size, 1024);
   hipLaunchKernelGGL(grouped_add_kernel<T>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, st, p.part, p.dw,
@@ -429,8 +472,7 @@ hipError_t launch_grouped_dw(const Shape& s, const ProductShape& q, const void* 
   const GroupedSumArgs p{x, dy, dw, (float*)ws, offsets, (int)s.N, (int)s.M, q.n_out, q.n_in, rows(s, perm, q.x_order),
                          rows(s, perm, q.y_order), sum_parts(s, q.n_in, q.n_out)};
   const int side = sum_side(s, q.n_in, q.n_out);
-  if (perm) return s.bf16 ? sums<BF16, true>(p, side, st) : sums<F32, true>(p, side, st);
-  return s.bf16 ? sums<BF16, false>(p, side, st) : sums<F32, false>(p, side, st);
+  return s.bf16 ? sums<BF16>(p, side, st) : sums<F32>(p, side, st);
 }
 
 }  // namespace omnimoe

@@ -6,7 +6,6 @@
 #include "few_tile.hpp"
 #include "grouped_rows.hpp"
 #include "internal.hpp"
-#include "tile_gemm.hpp"
 #include "vec8.hpp"
 
 namespace omnimoe {
@@ -226,9 +225,9 @@ __global__ __launch_bounds__(64 * W) void product4_kernel(Product4Args p, int gr
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[e] = acc[b][e];
-      if constexpr (SWIGLU) v[e] = activation(1, v[e]) * acc[b + (SWIGLU ? 1 : 0)][e];
+      if constexpr (SWIGLU) v[e] = swiglu<BF16>(v[e], acc[b + (SWIGLU ? 1 : 0)][e]);
     }
-    store4(out + f, v[0], v[1], v[2], v[3]);
+    put4(out + f, v[0], v[1], v[2], v[3]);
   }
 }
 
