@@ -557,10 +557,12 @@ def _block_call(fn, desc, head, tensors, tail, stream):
         raise ValueError(f"{fn}: the stream belongs to GPU {stream.device_index}, the tensors to GPU {dev}")
     at = torch.cuda.current_device()
     if dev < 0 or dev == at:
-        _check(fn, call(*args, *tail, _raw_stream(at) if stream is None else stream.cuda_stream))
-        return
-    with torch.cuda.device(dev):
-        _check(fn, call(*args, *tail, _raw_stream(dev) if stream is None else stream.cuda_stream))
+        status = call(*args, *tail, _raw_stream(at) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            status = call(*args, *tail, _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if status:
+        _check(fn, status)
 
 
 def _gate_width(gate):

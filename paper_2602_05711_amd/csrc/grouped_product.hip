@@ -11,7 +11,7 @@
 #include "grouped_rows.hpp"
 #include "internal.hpp"
 #include "tile_gemm.hpp"
-#include "tile_turns.hpp"
+#include "tile_spread.hpp"
 #include "vec8.hpp"
 
 namespace omnimoe {
@@ -33,43 +33,54 @@ struct RowOperand : TileOperand<T, R, false, NW> {
       ptr[i] = (const char*)p + ((int64_t)row(lrow) * ld + Tile::place(lrow, at % 8) * Tile::kPer) * T::kSize;
     }
   }
-  __device__ __forceinline__ void copy(unsigned char* st, int at, int64_t, int kt, int K, int wid, int lane) const {
-    const int to = at + this->lds;
+  __device__ __forceinline__ void copy(unsigned char* st, int at, int kt, int K, int wid, int lane) const {
     const int64_t skip = (int64_t)kt * T::kStep * T::kSize;
-    if ((kt + 1) * T::kStep <= K) {
+    const int left = K - kt * T::kStep;
 #pragma unroll
-      for (int i = 0; i < Tile::kCopies; ++i)
-        __builtin_amdgcn_global_load_lds((const void*)(ptr[i] + skip), (tg_lds_ptr)(st + (to + i * 1024)), 16, 0, 0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < Tile::kCopies; ++i) {
-        const char* const p = kt * T::kStep + Tile::chunk_k(i, lane, wid) < K ? ptr[i] + skip : (const char*)&tile_zeros;
-        __builtin_amdgcn_global_load_lds((const void*)p, (tg_lds_ptr)(st + (to + i * 1024)), 16, 0, 0);
-      }
+    for (int i = 0; i < Tile::kCopies; ++i) {
+      const char* p = ptr[i] + skip;
+      p = Tile::chunk_k(i, lane, wid) < left ? p : (const char*)&tile_zeros;
+      __builtin_amdgcn_global_load_lds((const void*)p, (tg_lds_ptr)(st + (at + this->lds + i * 1024)), 16, 0, 0);
     }
+  }
+  __device__ __forceinline__ void copy(unsigned char* st, int at, int64_t, int kt, int K, int wid, int lane) const {
+    copy(st, at, kt, K, wid, lane);
   }
 };
 
-// The rows that the stages' positions name, by x's order and by dy's, in LDS: rows[kt % 2] from the stage before kt on. Wave 0
-// brings them, a position a lane: the entry of perm for stage kt + 2 is loaded while stage kt is copied, and looked at a
-// stage later, when nothing has to be waited for (loads return in order, behind the copies issued before them).
+// The rows that the stages' positions name, by x's order and by dy's, in LDS: rows[kt % 4] from before stage kt's copies on.
+// Wave 0 brings them, a position a lane: an entry of perm is loaded a stage before it is looked at, when nothing has to be
+// waited for (loads return in order, behind the copies issued before them).
 struct SumRows {
   RowOrder x, dy;
   int first, count;
   int2 (*rows)[64];
-  int next;  // (lane's entry of the stage after the next)
+  int next;  // (the lane's entry that was loaded last)
 
-  __device__ __forceinline__ void fetch(int k) {
-    if (x.perm) next = x.perm[first + (k < count ? k : count - 1)];
-  }
-  __device__ __forceinline__ void put(int slot, int k) {
+  __device__ __forceinline__ int entry(int k) const { return x.perm ? x.perm[first + (k < count ? k : count - 1)] : 0; }
+  __device__ __forceinline__ void fetch(int k) { next = entry(k); }
+  __device__ __forceinline__ void put(int kt, int k) {
     const int p = first + k, t = x.perm ? next : p;
-    rows[slot][lane_id()] = k < count ? make_int2(x.of(p, t), dy.of(p, t)) : make_int2(-1, -1);
+    rows[kt & 3][lane_id()] = k < count ? make_int2(x.of(p, t), dy.of(p, t)) : make_int2(-1, -1);
+  }
+  // The first N stages' rows, and the next one's entries of perm, all loaded together.
+  template <int STEP, int N>
+  __device__ __forceinline__ void begin() {
+    int t[N + 1];
+#pragma unroll
+    for (int kt = 0; kt <= N; ++kt) t[kt] = entry(kt * STEP + lane_id());
+#pragma unroll
+    for (int kt = 0; kt < N; ++kt) {
+      next = t[kt];
+      put(kt, kt * STEP + lane_id());
+    }
+    next = t[N];
   }
 };
 
-// Rows as the summed index: stage kt holds positions first + kt kStep .. of `count`, R of their columns.
-template <class T, int R, int NW, bool DY>
+// Rows as the summed index: stage kt holds positions first + kt kStep .. of `count`, R of their columns. BRINGS: its copies
+// bring the next stage's rows.
+template <class T, int R, int NW, bool DY, bool BRINGS>
 struct SumOperand : TileOperand<T, R, true, NW> {
   typedef TileOperand<T, R, true, NW> Tile;
   static_assert(T::kStep <= 64, "a wave's lanes");
@@ -87,18 +98,21 @@ struct SumOperand : TileOperand<T, R, true, NW> {
       from[i] = (const char*)p + (int64_t)(c < width ? c : width - Tile::kPer) * T::kSize;
     }
   }
-  __device__ __forceinline__ void copy(unsigned char* st, int at, int64_t, int kt, int K, int wid, int lane) const {
-    const int to = at + this->lds;
+  __device__ __forceinline__ void copy(unsigned char* st, int at, int kt, int K, int wid, int lane) const {
 #pragma unroll
     for (int i = 0; i < Tile::kCopies; ++i) {
-      const int2 both = rows->rows[kt & 1][((wid * Tile::kCopies + i) * 64 + lane) / Tile::kRowChunks];
-      const int row = K > 0 ? (DY ? both.y : both.x) : -1;
-      const char* const p = row >= 0 ? from[i] + (int64_t)row * ld : (const char*)&tile_zeros;
-      __builtin_amdgcn_global_load_lds((const void*)p, (tg_lds_ptr)(st + (to + i * 1024)), 16, 0, 0);
+      const int2 both = rows->rows[kt & 3][((wid * Tile::kCopies + i) * 64 + lane) / Tile::kRowChunks];
+      const int row = DY ? both.y : both.x;
+      const char* p = from[i] + (int64_t)row * ld;
+      p = row >= 0 && K > 0 ? p : (const char*)&tile_zeros;
+      __builtin_amdgcn_global_load_lds((const void*)p, (tg_lds_ptr)(st + (at + this->lds + i * 1024)), 16, 0, 0);
     }
-    if constexpr (DY)
+  }
+  __device__ __forceinline__ void copy(unsigned char* st, int at, int64_t, int kt, int K, int wid, int lane) const {
+    copy(st, at, kt, K, wid, lane);
+    if constexpr (BRINGS)
       if (wid == 0 && (kt + 1) * T::kStep < K) {
-        rows->put((kt + 1) & 1, (kt + 1) * T::kStep + lane);
+        rows->put(kt + 1, (kt + 1) * T::kStep + lane);
         rows->fetch((kt + 2) * T::kStep + lane);
       }
   }
@@ -112,86 +126,49 @@ struct GroupedArgs {
   RowOrder in_rows, out_rows;
 };
 
-// TM positions x TN weight rows of a workgroup of WR x WC waves (SWIGLU: TN / 2 gate rows and the same features' up rows, in
-// blocks of 32 in turn, so that a wave holds both). TRANSPOSED: the summed index is the weights' row (dx).
-template <class T, int TM, int TN, int WR, int WC, bool TRANSPOSED, bool SWIGLU>
-__device__ __forceinline__ void grouped_tile(const GroupedArgs& p, const RowUnit& u, int n0, unsigned char* st0,
-                                             unsigned char* st1, unsigned char* st2 = nullptr, unsigned char* st3 = nullptr,
-                                             unsigned char* st4 = nullptr, unsigned char* st5 = nullptr) {
-  constexpr bool kTurns = T::kSize == 2 && TM == 256 && TN == 256 && WR == 2 && WC == 4;
-  constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
-  static_assert(!SWIGLU || (NI % 2 == 0 && !TRANSPOSED), "a wave's gate and up rows");
-  typedef typename T::elem elem;
-  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
-  int a0[NI], b0[MJ];
+// A wave's 32 x 32 block of results, of which this lane has sixteen values of b's row lane % 32 in fours (a's rows 8 q + 4 (lane /
+// 32) + e), to the memory of that row; there(c): whether columns c .. c + 7 (fp32: c + 3) exist and are wanted. Rounded to
+// bf16, fours change places between the lanes (v_permlane32_swap) so that a store is 16 bytes a lane, 32 a row instead of 16:
+// gate and up projection of 131072 rows 1064 -> 1001 us. (64 a row, with v_permlane16_swap: 1018.)
+template <class T, class There>
+__device__ __forceinline__ void put_block(const float (&v)[16], int lane, void* to, There there) {
+  if constexpr (T::kSize == 2) {
 #pragma unroll
-  for (int j = 0; j < MJ; ++j) b0[j] = (wr * MJ + j) * 32;
+    for (int h = 0; h < 2; ++h) {
+      uint32_t w[4];
 #pragma unroll
-  for (int i = 0; i < NI; ++i) a0[i] = (wc * NI + i) * 32;
-  tg_f32x16 acc[NI][MJ];
-  tile_zero(acc);
-  auto in_row = [&](int r) {
-    const int row = p.in_rows(u.first + (r < u.count ? r : u.count - 1));
-    return row < 0 ? 0 : row;
-  };
-  TileOperand<T, TN, TRANSPOSED, NW> a;
-  const elem* const w = (const elem*)p.w + (int64_t)u.expert * (SWIGLU ? 2 : 1) * p.n * p.k;
-  if constexpr (TRANSPOSED)
-    a.init(w, p.n, wid, lane, [&](int r) { return n0 + r < p.n ? n0 + r : p.n - a.kPer; });
-  else
-    a.init(w, p.k, wid, lane, [&](int r) {
-      const int f = n0 + (SWIGLU ? (r >> 6) * 32 + (r & 31) : r), c = f < p.n ? f : p.n - 1;
-      return SWIGLU && (r & 32) ? p.n + c : c;
-    });
-  if constexpr (kTurns) {
-    RowOperand<T, 128, NW> part0, part1;
-    part0.init(p.in, p.k, wid, lane, [&](int r) { return in_row(turn_row(0, r)); });
-    part1.init(p.in, p.k, wid, lane, [&](int r) { return in_row(turn_row(1, r)); });
-    tile_sum_turns<T>(a, part0, part1, p.k, a0, wr, st0, st1, st2, st3, st4, st5, wid, lane, acc);
-  } else {
-    RowOperand<T, TM, NW> b;
-    b.init(p.in, p.k, wid, lane, in_row);
-    const TileRange all[2] = {{p.k, 0, 0}, {0, 0, 0}};
-    tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
-  }
-#pragma unroll
-  for (int j = 0; j < MJ; ++j) {
-    const int r = b0[j] + (lane & 31);
-    if (r >= u.count) continue;
-    const int row = p.out_rows(u.first + r);
-    if (row < 0) continue;
-    elem* const out = (elem*)p.out + (int64_t)row * p.n;
-#pragma unroll
-    for (int i = 0; i < NI; i += SWIGLU ? 2 : 1)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int f = n0 + (SWIGLU ? a0[i] / 2 : a0[i]) + 8 * q + 4 * (lane >> 5);
-        if (f >= p.n) continue;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = acc[i][j][4 * q + e];
-          if constexpr (SWIGLU) v[e] = swiglu<T::kSize == 2>(v[e], acc[i + 1][j][4 * q + e]);
-        }
-        put4(out + f, v[0], v[1], v[2], v[3]);
+      for (int e = 0; e < 2; ++e) {
+        const auto x = __builtin_amdgcn_permlane32_swap(bf16_pair(v[8 * h + 2 * e], v[8 * h + 2 * e + 1]),
+                                                        bf16_pair(v[8 * h + 4 + 2 * e], v[8 * h + 5 + 2 * e]), false, false);
+        w[e] = x[0], w[2 + e] = x[1];
       }
+      const int c = 16 * h + 8 * (lane >> 5);
+      if (there(c)) *(uint4*)((uint16_t*)to + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int c = 8 * q + 4 * (lane >> 5);
+      if (there(c)) *(float4*)((float*)to + c) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    }
   }
 }
 
-// An expert's last unit is rarely whole: tiles of 256 rows take one of up to 128 or 64 as a tile of that many.
+// TM positions x TN weight rows (SWIGLU: TN / 2 gate rows and the same features' up rows, in blocks of 32 in turn, so that a
+// wave holds both) a workgroup of WR x WC waves. TRANSPOSED: the summed index is the weights' row (dx).
 template <class T, int TM, int TN, int WR, int WC, bool TRANSPOSED, bool SWIGLU>
 __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs p) {
-  constexpr int FN = SWIGLU ? TN / 2 : TN;
-  constexpr bool kTurns = TM == 256;
-  // (by turns: a stage of a in st0 or st1, b's parts in the others; else a stage of both in st0 or st1)
-  constexpr int kStage = kTurns ? 256 * 128 : (TM + TN) * 128, kPart = kTurns ? 128 * 128 : 16;
-  __shared__ __attribute__((aligned(1024))) unsigned char st0[kStage], st1[kStage];
-  __shared__ __attribute__((aligned(1024))) unsigned char st2[kPart], st3[kPart], st4[kPart], st5[kPart];
+  constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32, FN = SWIGLU ? TN / 2 : TN;
+  constexpr bool kSpread = TM == 256 && SWIGLU;
+  static_assert(!SWIGLU || (NI % 2 == 0 && !TRANSPOSED), "a wave's gate and up rows");
+  typedef typename T::elem elem;
+  __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
   const int tiles_n = (p.n + FN - 1) / FN;
   // neighbouring tiles, which share rows or weights, go to one XCD
   RowUnit u;
   int tile = -1;
-  find_unit<64 * WR * WC>(p.offsets, p.N, p.M, TM, (int*)st0, [&](int total) {
+  find_unit<64 * NW>(p.offsets, p.N, p.M, TM, (int*)st0, [&](int total) {
     const int64_t all = (int64_t)total * tiles_n;
     if (blockIdx.x >= all) return -1;
     const unsigned item = (unsigned)xcd_contiguous(blockIdx.x, all), unit = item / (unsigned)tiles_n;
@@ -200,7 +177,55 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs 
   }, u);
   if (tile < 0) return;
   __syncthreads();
-  grouped_tile<T, TM, TN, WR, WC, TRANSPOSED, SWIGLU>(p, u, tile * FN, st0, st1, st2, st3, st4, st5);
+  const int n0 = tile * FN;
+  int a0[NI], b0[MJ];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) a0[i] = (wc * NI + i) * 32;
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) b0[j] = (wr * MJ + j) * 32;
+  tg_f32x16 acc[NI][MJ];
+  tile_zero(acc);
+  RowOperand<T, TM, NW> b;
+  b.init(p.in, p.k, wid, lane, [&](int r) {
+    const int row = p.in_rows(u.first + (r < u.count ? r : u.count - 1));
+    return row < 0 ? 0 : row;
+  });
+  typename std::conditional<kSpread, SpreadOperand<T, TN, TRANSPOSED, NW>, TileOperand<T, TN, TRANSPOSED, NW>>::type a;
+  const elem* const w = (const elem*)p.w + (int64_t)u.expert * (SWIGLU ? 2 : 1) * p.n * p.k;
+  if constexpr (TRANSPOSED)
+    a.init(w, p.n, wid, lane, [&](int r) { return n0 + r < p.n ? n0 + r : p.n - a.kPer; });
+  else
+    a.init(w, p.k, wid, lane, [&](int r) {
+      const int f = n0 + (SWIGLU ? (r >> 6) * 32 + (r & 31) : r), c = f < p.n ? f : p.n - 1;
+      return SWIGLU && (r & 32) ? p.n + c : c;
+    });
+  if constexpr (kSpread) {
+    spread_sum<T>(a, b, p.k, a0, b0, wr * (TM / WR) < u.count, st0, st1, wid, lane, acc, [](int) {});
+  } else {
+    const TileRange all[2] = {{p.k, 0, 0}, {0, 0, 0}};
+    tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
+  }
+  int out[MJ];  // (looked up together: a wait for each would be a fifth of the stores' time)
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) {
+    const int r = b0[j] + (lane & 31);
+    out[j] = p.out_rows.task(u.first + (r < u.count ? r : u.count - 1));
+  }
+#pragma unroll
+  for (int j = 0; j < MJ; ++j) {
+    const int r = b0[j] + (lane & 31), row = r < u.count ? p.out_rows.of(u.first + r, out[j]) : -1;
+#pragma unroll
+    for (int i = 0; i < NI; i += SWIGLU ? 2 : 1) {
+      float v[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        v[e] = acc[i][j][e];
+        if constexpr (SWIGLU) v[e] = swiglu<T::kSize == 2>(v[e], acc[i + 1][j][e]);
+      }
+      const int f = n0 + (SWIGLU ? a0[i] / 2 : a0[i]);
+      put_block<T>(v, lane, (elem*)p.out + (int64_t)row * p.n + f, [&](int c) { return row >= 0 && f + c < p.n; });
+    }
+  }
 }
 
 // 16 RB weight rows (SWIGLU: half of them gate rows, in turn) for a unit of up to sixteen positions.
@@ -275,7 +300,7 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArg
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
   typedef typename T::elem elem;
   __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
-  __shared__ int2 slots[2][64];
+  __shared__ int2 slots[4][64];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
   const unsigned tiles_k = (p.k + TN - 1) / TN, tiles_n = (p.n + TM - 1) / TM, each = tiles_k * tiles_n * p.parts;
   unsigned item;
@@ -303,35 +328,38 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArg
   tg_f32x16 acc[NI][MJ];
   tile_zero(acc);
   SumRows rows{p.x_rows, p.y_rows, first, count, slots, 0};
-  SumOperand<T, TN, NW, false> a;
-  SumOperand<T, TM, NW, true> b;
+  SumOperand<T, TN, NW, false, false> a;
+  SumOperand<T, TM, NW, true, true> b;
   a.init(p.x, p.k, (int)tk * TN, &rows, wid, lane);
   b.init(p.dy, p.n, (int)tn * TM, &rows, wid, lane);
   if (count) {
-    if (wid == 0) {
-      rows.fetch(lane);
-      rows.put(0, lane);
-      rows.fetch(T::kStep + lane);
-    }
+    if (wid == 0) rows.begin<T::kStep, TM == 256 ? 3 : 1>();
     __syncthreads();
   }
-  const TileRange all[2] = {{count, 0, 0}, {0, 0, 0}};
-  tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
+  if constexpr (TM == 256) {
+    spread_sum<T>(a, b, count, a0, b0, true, st0, st1, wid, lane, acc, [&](int s) {
+      if (wid) return;
+      rows.put(s + 3, (s + 3) * T::kStep + lane);
+      rows.fetch((s + 4) * T::kStep + lane);
+    });
+  } else {
+    const TileRange all[2] = {{count, 0, 0}, {0, 0, 0}};
+    tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
+  }
 #pragma unroll
   for (int j = 0; j < MJ; ++j) {
     const int n = tn * TM + b0[j] + (lane & 31);
-    if (n >= p.n) continue;
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int i = 0; i < NI; ++i) {
+      const int k = tk * TN + a0[i];
+      const int64_t at = ((int64_t)e * p.n + n) * p.k + k;
+      const auto there = [&](int c) { return n < p.n && k + c < p.k; };
+      float v[16];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int k = tk * TN + a0[i] + 8 * q + 4 * (lane >> 5);
-        if (k >= p.k) continue;
-        const int64_t at = ((int64_t)e * p.n + n) * p.k + k;
-        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        if (p.parts > 1) *(float4*)(p.part + (int64_t)part * p.N * p.n * p.k + at) = make_float4(v[0], v[1], v[2], v[3]);
-        else put4((elem*)p.dw + at, v[0], v[1], v[2], v[3]);
-      }
+      for (int c = 0; c < 16; ++c) v[c] = acc[i][j][c];
+      if (p.parts > 1) put_block<F32>(v, lane, p.part + (int64_t)part * p.N * p.n * p.k + at, there);
+      else put_block<T>(v, lane, (elem*)p.dw + at, there);
+    }
   }
 }
 

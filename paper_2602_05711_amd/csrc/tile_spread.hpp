@@ -1,0 +1,121 @@
+// The sum of a 256 x 256 tile with tile_gemm.hpp's products and places in LDS and the copies spread over a stage's time.
+//
+// A stage's copies, all at once behind the barrier, keep the waves from their products for as long as the copies take to be
+// issued (64 bytes a cycle: half the time of the stage's products). Here a's are issued among the last quarter's products of
+// the stage before the last, b's among the next stage's first, one for every two products; no branch divides these: past
+// the sum's end the copies are of zeros.
+#pragma once
+
+#include "tile_gemm.hpp"
+
+namespace omnimoe {
+
+// An operand of rows (k contiguous) or columns (MNC) at fixed places of one matrix, TileOperand's without branches.
+template <class T, int R, bool MNC, int NW>
+struct SpreadOperand : TileOperand<T, R, MNC, NW> {
+  typedef TileOperand<T, R, MNC, NW> Tile;
+  __device__ __forceinline__ void copy(unsigned char* st, int at, int kt, int K, int wid, int lane) const {
+    const char* const from = this->base + kt * this->step;
+    const int left = K - kt * T::kStep;
+#pragma unroll
+    for (int i = 0; i < Tile::kCopies; ++i) {
+      const char* p = from + this->off[i];
+      p = Tile::chunk_k(i, lane, wid) < left ? p : (const char*)&tile_zeros;
+      __builtin_amdgcn_global_load_lds((const void*)p, (tg_lds_ptr)(st + (at + this->lds + i * 1024)), 16, 0, 0);
+    }
+  }
+};
+
+// acc += the sum over K values of k. Waves with work == false (none of their rows of b exists) copy only. ahead(s) runs in
+// stage s behind its barrier, before the copies of a's stage s + 2 (for what the operands look up). Every thread of the
+// workgroup takes part; on return the LDS is free.
+template <class T, class OA, class OB, int MI, int NJ, class Ahead>
+__device__ __forceinline__ void spread_sum(const OA& a, const OB& b, int K, const int (&a0)[MI], const int (&b0)[NJ],
+                                           bool work, unsigned char* st0, unsigned char* st1, int wid, int lane,
+                                           tg_f32x16 (&acc)[MI][NJ], Ahead ahead) {
+  if (K <= 0) return;
+  const int n = ((K + T::kStep - 1) / T::kStep + 1) & ~1;  // an odd number of stages ends with one of zeros
+  auto wait_copies = []() { __builtin_amdgcn_s_waitcnt(0x0F70); };  // vmcnt(0)
+  typename T::frag fa[2][MI], fb[2][NJ];
+  auto read = [&](const unsigned char* st, int ks) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) fb[ks & 1][j] = OB::frag(st, OA::kBytes, b0[j], ks, lane);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) fa[ks & 1][i] = OA::frag(st, 0, a0[i], ks, lane);
+  };
+  auto mma = [&](int ks) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) tile_mma(acc[i][j], fa[ks & 1][i], fb[ks & 1][j]);
+  };
+  constexpr int kReads = MI * OA::kReads + NJ * OB::kReads, kMma = MI * NJ * T::kMma;
+  constexpr int kPer = (kReads + kMma - 1) / kMma;
+  // products of one quarter with the next one's reads, and copies, between them
+  auto interleave = [&](auto copies) {
+#pragma unroll
+    for (int i = 0; i < kMma; ++i) {
+      if constexpr (decltype(copies)::value) {
+        if (i % 2 == 0) {
+          __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // VALU
+          __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);  // VMEM
+        }
+      }
+      __builtin_amdgcn_sched_group_barrier(0x100, kPer, 0);  // LDS reads
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);     // a product
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto stage = [&](unsigned char* cur, unsigned char* next, int s) {
+    __builtin_amdgcn_sched_barrier(0);
+    b.copy(next, OA::kBytes, s + 1, K, wid, lane);
+    read(cur, 1);
+    mma(0);
+    interleave(std::true_type{});
+    read(cur, 2);
+    mma(1);
+    interleave(std::false_type{});
+    read(cur, 3);
+    mma(2);
+    interleave(std::false_type{});
+    // the wave's copies of stage s + 1 and its reads of stage s are done, and with the barrier everyone's
+    wait_copies();
+    __syncthreads();
+    ahead(s);
+    __builtin_amdgcn_sched_barrier(0);
+    a.copy(cur, 0, s + 2, K, wid, lane);
+    read(next, 0);  // (after the last stage: what is there, unused)
+    mma(3);
+    interleave(std::true_type{});
+  };
+  auto idle = [&](unsigned char* cur, unsigned char* next, int s) {
+    b.copy(next, OA::kBytes, s + 1, K, wid, lane);
+    wait_copies();
+    __syncthreads();
+    ahead(s);
+    a.copy(cur, 0, s + 2, K, wid, lane);
+  };
+  a.copy(st0, 0, 0, K, wid, lane);
+  b.copy(st0, OA::kBytes, 0, K, wid, lane);
+  wait_copies();
+  __syncthreads();
+  a.copy(st1, 0, 1, K, wid, lane);
+  if (work) {
+    read(st0, 0);
+#pragma unroll 1
+    for (int s = 0; s < n; s += 2) {
+      stage(st0, st1, s);
+      stage(st1, st0, s + 1);
+    }
+  } else {
+#pragma unroll 1
+    for (int s = 0; s < n; s += 2) {
+      idle(st0, st1, s);
+      idle(st1, st0, s + 1);
+    }
+  }
+  wait_copies();
+  __syncthreads();
+}
+
+}  // namespace omnimoe
