@@ -32,7 +32,7 @@ extern "C" {
  *   w_in   [d] fp32, the weight of the norm before the next branch; NULL: n is not written (with y NULL: invalid)
  *   x_out  [T, d]  dtype out, may be x itself
  *   n      [T, d]  dtype out
- *   eps    > 0, finite
+ *   eps    1e-30 or more (squares that fp32 does not hold are then nothing beside it), finite
  * Of the descriptor T, d and dtype. Arithmetic is fp32; x_out and n are rounded once each, n from x_out before it is
  * rounded. Rows whose mean square is past fp32's largest value are normed as others. T = 0 is a no-op. */
 omnimoe_status omnimoe_block_join(const omnimoe_layer_desc* desc, float eps, int32_t gate_width, const void* x,
@@ -107,7 +107,7 @@ omnimoe_status omnimoe_grouped_product_dw(const omnimoe_layer_desc* desc, const 
  *                                       max |w| <= 6 2^s
  * store: code = w 2^-s rounded to the nearest of the list, ties to the even place; magnitudes past 6 2^125 become that. A
  * block that holds a value which is not finite has scale byte 255, and all of its values are NaN.
- * load: w = code 2^s, exact in both types. Of the descriptor N and dtype, of the product n_in (n_in % 32 == 0), n_out and
+ * load: w = code 2^s, exact in both types, for the scale bytes that store writes: 2 to 252, and 255. Of the descriptor N and dtype, of the product n_in (n_in % 32 == 0), n_out and
  * swiglu. */
 omnimoe_status omnimoe_weights4_store(const omnimoe_layer_desc* desc, const omnimoe_product* product, const void* w,
                                       uint8_t* codes, uint8_t* scales, void* stream);

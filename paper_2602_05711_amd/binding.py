@@ -566,6 +566,8 @@ def _block_call(fn, desc, head, tensors, tail, stream):
 
 
 def _gate_width(gate):
+    if gate is not None and gate.dim() not in (1, 2):
+        raise ValueError(f"omnimoe_block_join: gate has the shape {tuple(gate.shape)}, not [T], [T, 1] or [T, d]")
     return 0 if gate is None else 1 if gate.dim() == 1 else gate.shape[1]
 
 

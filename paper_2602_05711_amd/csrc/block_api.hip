@@ -12,7 +12,7 @@ omnimoe_status check_join(const omnimoe_layer_desc* desc, float eps, int32_t gat
                           Shape* s) {
   const omnimoe_status st = check_desc(desc, s);
   if (st) return st;
-  if (!(eps > 0.0f) || eps > 3.402823466e38f) return OMNIMOE_ERR_INVALID_ARG;
+  if (!(eps >= 1e-30f) || eps > 3.402823466e38f) return OMNIMOE_ERR_INVALID_ARG;
   if (gate_width != 0 && gate_width != 1 && gate_width != s->d) return OMNIMOE_ERR_INVALID_ARG;
   return y || w_in || s->T == 0 ? OMNIMOE_OK : OMNIMOE_ERR_INVALID_ARG;
 }

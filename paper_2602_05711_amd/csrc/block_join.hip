@@ -190,7 +190,8 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
   raw.token = 0.0f;
   const int64_t stride = gridDim.x;
   int64_t t = blockIdx.x;
-  raw.load(p, t, c0, in);
+  constexpr bool kAhead = W < 16;  // (sixteen waves' registers do not hold two rows)
+  if (kAhead) raw.load(p, t, c0, in);
   float a[8], w_in[8], sum_s[8], sum_n[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) a[e] = 1.0f, w_in[e] = sum_s[e] = sum_n[e] = 0.0f;
@@ -206,13 +207,14 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
   }
   for (; t < p.T; t += stride) {
     float x[8], y[8], u[8], G[8], g[8], dn[8];
+    if (!kAhead) raw.load(p, t, c0, in);
     raw.x.values(x);
     raw.dn.values(dn);
     raw.dx_out.values(G);
     raw.gate.values(g);
     raw.y.values(y);
     const float gate = raw.token;
-    if (t + stride < p.T) raw.load(p, t + stride, c0, in);
+    if (kAhead && t + stride < p.T) raw.load(p, t + stride, c0, in);
 #pragma unroll
     for (int e = 0; e < 8; ++e) u[e] = w_in[e] * dn[e];
     // sums of x'^2, u x' and y^2

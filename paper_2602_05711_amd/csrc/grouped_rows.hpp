@@ -132,7 +132,7 @@ struct RowOrder {
   int M, by_position;  // by_position: all bits, or none
   FastDiv div;         // tasks of a row
   static RowOrder make(const int32_t* perm, int M, int order, int hk) {
-    return {perm, M, order == 0 ? -1 : 0, FastDiv::by(order == 2 ? (uint32_t)hk : 1u)};
+    return {perm, M, order == 0 ? -1 : 0, FastDiv::by(order == 2 && hk > 0 ? (uint32_t)hk : 1u)};
   }
   __device__ __forceinline__ int task(int p) const { return perm ? perm[p] : p; }
   // Row of position p, whose task is t; -1 where there is no such task.

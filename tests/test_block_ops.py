@@ -61,7 +61,7 @@ def test_join_refusals():
         assert _join(d, change) == INVALID, i
     for i in range(8):
         assert _join(d, [(i, BAD)]) == ALIGN, i
-    for eps in (0.0, -1e-6, float("inf"), float("nan")):
+    for eps in (0.0, 1e-31, -1e-6, float("inf"), float("nan")):
         assert _join(d, eps=eps) == INVALID
     for width in (-1, 2, 63, 65):
         assert _join(d, gate_width=width) == INVALID
@@ -184,6 +184,8 @@ def test_binding_refuses_before_the_call():
     x, y, w = torch.zeros(4, 64, dtype=bf), torch.zeros(4, 64), torch.zeros(64)
     with pytest.raises(ValueError, match="not on a GPU"):
         P.omnimoe_block_join(d, 1e-6, x, y, None, w, None, w, x, x)
+    with pytest.raises(ValueError, match="gate has the shape"):
+        P.omnimoe_block_join(d, 1e-6, x, y, torch.zeros((), dtype=bf), w, None, w, x, x)
     with pytest.raises(ValueError, match="x is torch.float32"):
         P.omnimoe_block_join(d, 1e-6, y, y, None, w, None, w, x, x)
     with pytest.raises(ValueError, match="not on a GPU"):
@@ -192,6 +194,15 @@ def test_binding_refuses_before_the_call():
     assert (q.n_in, q.n_out, q.swiglu, q.x_order, q.y_order) == (64, 32, 1, 2, 0)
     with pytest.raises(KeyError):
         P.make_product(64, 32, x_order="expert")
+
+
+def test_heads_times_experts_past_32_bits_without_tokens():
+    # no tokens: nothing is divided by H K, which has no 32-bit value here
+    d = _desc(T=0, n_rows=64, n_cols=64, K=4096, H=1 << 20)
+    assert _product("omnimoe_grouped_product", d, _q(x_order=2), [(i, None) for i in range(5)]) == OK
+    n = ctypes.c_size_t(1)
+    size = _lib().omnimoe_grouped_product_dw_workspace_size
+    assert size(ctypes.byref(d), ctypes.byref(_q(x_order=2)), ctypes.byref(n)) == OK and n.value == 0
 
 
 # ------------------------------------------------------------------ the plain forms

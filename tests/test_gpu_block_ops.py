@@ -381,6 +381,11 @@ def test_product_of_no_tokens():
     dw = torch.full_like(c.w, 3.0)
     P.omnimoe_grouped_product_dw(c.D, c.q, None, None, None, None, dw)
     assert int(dw.count_nonzero()) == 0
+    # no tokens: nothing is divided by H K, which has no 32-bit value here
+    D = S.desc(0, 64, BF16, n_rows=64, n_cols=64, K=4096, H=1 << 20)
+    dw = torch.full((4096, 8, 8), 3.0, dtype=BF16, device="cuda")
+    P.omnimoe_grouped_product_dw(D, P.make_product(8, 8, False, "token", "task"), None, None, None, None, dw)
+    assert int(dw.count_nonzero()) == 0
 
 
 def test_product_rows_past_4_gib():
