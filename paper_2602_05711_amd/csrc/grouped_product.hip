@@ -1,11 +1,17 @@
 // Products of rows grouped by expert: position p of expert e has y_p = W_e x_p (or silu(G_e x_p) (U_e x_p), W_e being G_e's
 // rows and then U_e's), dx_p = W_e^T dy_p and dW_e = sum over e's positions of dy_p x_p^T.
 //
-// Many rows an expert: tile products (tile_gemm.hpp) whose rows are gathered by position, task or token while they are
-// copied to LDS. The experts' positions are cut into units of a tile's rows; a workgroup finds its unit from the offsets
-// itself, so that the grid depends on the sizes alone: units past the last leave at once.
+// Many rows an expert: tile products (tile_gemm.hpp, tile_spread.hpp) whose rows are gathered by position, task or token while
+// they are copied to LDS. The experts' positions are cut into units of a tile's rows; a workgroup finds its unit from the
+// offsets itself, so that the grid depends on the sizes alone: units past the last leave at once. Bound by the matrix cores
+// beside the copies and by the tiles' starts and ends (8 to 14 us of a 256 x 256 tile's 60, 2048 summed values): 131072 rows
+// of 2048 on 64 experts of 2048 x 2048 with SwiGLU 1010 us, 1.09 PFLOP/s, 65536 rows' dx 570 and dW 655 us, 0.96 and 0.84;
+// the library's dense product of 131072 x 2048 x 2048 reaches 1.36. Without its copies the loop runs at 1.34 to 1.54, so that
+// what the copies take is the difference; two groups of waves taking turns, four times as many waits of a quarter the length
+// and workgroups that go from tile to tile were no faster (1065 us, 1107, 1074), the last for want of registers.
 // Few rows an expert: the time is that of reading the weights of the experts that have rows, and of little beside it
-// (few_tile.hpp): a unit is up to sixteen rows, a workgroup takes 32 weight rows and splits the summed index over its waves.
+// (few_tile.hpp): a unit is up to sixteen rows, a workgroup takes 16 or 32 weight rows and splits the summed index over its
+// waves. 128 rows on 64 experts of 2048 x 2048: 86 us, 5.5 TB/s.
 // Sums are fp32, rounded once; every result has one order of summation, so that it is the same on every run.
 #include "few_tile.hpp"
 #include "grouped_rows.hpp"
@@ -294,7 +300,8 @@ __device__ __forceinline__ int expert_of_rank(const int32_t* offsets, int N, int
   return __builtin_ctzll(__ballot(rank == want));
 }
 
-// A tile of dW_e: TM of y's columns x TN of x's, one part of e's positions.
+// A tile of dW_e: TM of y's columns x TN of x's, one part of e's positions. 65536 rows on 64 experts of 2048 x 2048, some with
+// three times others' rows: 655 us (with every copy looking up its row by itself 1560, experts in their own order 846).
 template <class T, int TM, int TN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArgs p) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;
@@ -387,7 +394,9 @@ int64_t most_units(int64_t M, int N, int R) {
 RowOrder rows(const Shape& s, const int32_t* perm, int order) { return RowOrder::make(perm, (int)s.M, order, s.hk); }
 int64_t cut(int64_t v, int64_t by) { return (v + by - 1) / by; }
 
-// The tile's side by how many tiles of 256 or 128 the sizes make.
+// The tile's side by how many tiles of 256 or 128 the sizes make: as many as keep three quarters, or half, of the compute
+// units busy, of experts that fill at least half of one. fp32: 64 (its products take eight times bf16's time, so that a
+// tile's copies are nothing beside them: 8192 rows, 1024 x 1024, 16 experts 165 us, 104 TFLOP/s; with 128 x 128 197).
 int tile_side(bool bf16, int64_t M, int N, int n) {
   if (!bf16) return 64;
   const int64_t rows = M / N;  // of an expert
@@ -441,13 +450,14 @@ hipError_t forward(const GroupedArgs& p, bool swiglu, hipStream_t st) {
   return swiglu ? tiles<T, false, true>(p, st) : tiles<T, false, false>(p, st);
 }
 
+// The weight gradients' tiles, by the same measure; their number does not depend on the rows.
 int sum_side(const Shape& s, int k, int n) {
   if (!s.bf16) return 64;
   if (s.N * cut(k, 256) * cut(n, 256) >= 192) return 256;
   return s.N * cut(k, 128) * cut(n, 128) >= 128 ? 128 : 64;
 }
 
-// Parts of an expert's positions, where the tiles alone leave compute units idle.
+// Parts of an expert's positions, of 512 at least, where the tiles alone leave compute units idle.
 int sum_parts(const Shape& s, int k, int n) {
   const int side = sum_side(s, k, n);
   const int64_t tiles = s.N * cut(k, side) * cut(n, side), wanted = 512 / tiles, most = s.M / s.N / 512;

@@ -3,7 +3,8 @@
 // A stage's copies, all at once behind the barrier, keep the waves from their products for as long as the copies take to be
 // issued (64 bytes a cycle: half the time of the stage's products). Here a's are issued among the last quarter's products of
 // the stage before the last, b's among the next stage's first, one for every two products; no branch divides these: past
-// the sum's end the copies are of zeros.
+// the sum's end the copies are of zeros. Gate and up projection of 131072 rows, 64 experts, 2048 x 2048: 1041 us where tile_sum's
+// loop takes 1080; without SwiGLU, whose accumulators leave it fewer registers, 544 for 65536 rows where tile_sum takes 523.
 #pragma once
 
 #include "tile_gemm.hpp"
