@@ -540,35 +540,38 @@ ORDERS = {"position": 0, "task": 1, "token": 2}  # OMNIMOE_ORDER_*
 
 
 def _block_call(fn, desc, head, tensors, tail, stream):
-    """_ffn_call for fn(desc, *head, *(the tensors' addresses), *tail, stream): checks and addresses in one pass."""
-    import torch
-    dev, args = -1, [ctypes.byref(desc), *head]
-    for name, t, dtype, n in tensors:
+    """_ffn_call for fn(desc, *head, *(the tensors' addresses), *tail, stream), with checks and addresses in one pass where all
+    tensors are on the current GPU."""
+    args = [ctypes.byref(desc), *head]
+    add, dev = args.append, -1
+    for _, t, dtype, n in tensors:
         if t is None:
-            args.append(None)
+            add(None)
             continue
         at = t.get_device()
-        if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or at < 0 or (at != dev and dev >= 0):
-            _ffn_refuse(fn, dev, name, t, dtype, n)
-        dev = at
-        args.append(t.data_ptr())
-    call = getattr(_lib or load_library(), fn)
-    if stream is not None and dev >= 0 and stream.device_index != dev:
-        raise ValueError(f"{fn}: the stream belongs to GPU {stream.device_index}, the tensors to GPU {dev}")
-    at = torch.cuda.current_device()
-    if dev < 0 or dev == at:
-        status = call(*args, *tail, _raw_stream(at) if stream is None else stream.cuda_stream)
+        if dev < 0:
+            dev = at
+        if at != dev or at < 0 or t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+            break
+        add(t.data_ptr())
     else:
-        with torch.cuda.device(dev):
-            status = call(*args, *tail, _raw_stream(dev) if stream is None else stream.cuda_stream)
-    if status:
-        _check(fn, status)
+        if dev >= 0 and (stream is None or stream.device_index == dev) and dev == _current_device():
+            args += tail
+            add(_raw_stream(dev) if stream is None else stream.cuda_stream)
+            status = getattr(_lib or load_library(), fn)(*args)
+            if status:
+                _check(fn, status)
+            return
+    _ffn_call(fn, desc, tensors, (*head, *(t for _, t, _, _ in tensors), *tail), stream)
 
 
-def _gate_width(gate):
-    if gate is not None and gate.dim() not in (1, 2):
-        raise ValueError(f"omnimoe_block_join: gate has the shape {tuple(gate.shape)}, not [T], [T, 1] or [T, d]")
-    return 0 if gate is None else 1 if gate.dim() == 1 else gate.shape[1]
+def _current_device():
+    import torch
+    return torch._C._cuda_getDevice()
+
+
+def _gate_width(desc, gate):
+    return 0 if gate is None else 1 if gate.numel() == desc.T else desc.d
 
 
 def omnimoe_block_join(desc, eps, x, y, gate, w_out, scale, w_in, x_out, n, stream=None):
@@ -576,7 +579,7 @@ def omnimoe_block_join(desc, eps, x, y, gate, w_out, scale, w_in, x_out, n, stre
     alone; w_out, scale, w_in may be None."""
     import torch
     T, d, dt, f32 = desc.T, desc.d, _layer_dtype(desc), torch.float32
-    width = _gate_width(gate)
+    width = _gate_width(desc, gate)
     _block_call("omnimoe_block_join", desc, (eps, width), (
         ("x", x, dt, T * d), ("y", y, f32, T * d), ("gate", gate, dt, T * width), ("w_out", w_out, f32, d),
         ("scale", scale, f32, d), ("w_in", w_in, f32, d), ("x_out", x_out, dt, T * d), ("n", n, dt, T * d)),
@@ -594,7 +597,7 @@ def omnimoe_block_join_backward(desc, eps, x_out, y, gate, w_out, scale, w_in, d
     device = (dx if dx is not None else dw_in).device
     ws = _ffn_workspace(ws, lambda: omnimoe_block_join_backward_workspace_size(desc), device, stream)
     T, d, dt, f32 = desc.T, desc.d, _layer_dtype(desc), torch.float32
-    width = _gate_width(gate)
+    width = _gate_width(desc, gate)
     _block_call("omnimoe_block_join_backward", desc, (eps, width), (
         ("x_out", x_out, dt, T * d), ("y", y, f32, T * d), ("gate", gate, dt, T * width), ("w_out", w_out, f32, d),
         ("scale", scale, f32, d), ("w_in", w_in, f32, d), ("dx_out", dx_out, dt, T * d), ("dn", dn, dt, T * d),

@@ -184,8 +184,8 @@ def test_binding_refuses_before_the_call():
     x, y, w = torch.zeros(4, 64, dtype=bf), torch.zeros(4, 64), torch.zeros(64)
     with pytest.raises(ValueError, match="not on a GPU"):
         P.omnimoe_block_join(d, 1e-6, x, y, None, w, None, w, x, x)
-    with pytest.raises(ValueError, match="gate has the shape"):
-        P.omnimoe_block_join(d, 1e-6, x, y, torch.zeros((), dtype=bf), w, None, w, x, x)
+    with pytest.raises(ValueError, match="gate must be contiguous"):  # (a gate of the wrong size, on the same device)
+        B._ffn_refuse("omnimoe_block_join", 0, "gate", torch.zeros(5, 1, dtype=bf), bf, 4)
     with pytest.raises(ValueError, match="x is torch.float32"):
         P.omnimoe_block_join(d, 1e-6, y, y, None, w, None, w, x, x)
     with pytest.raises(ValueError, match="not on a GPU"):
