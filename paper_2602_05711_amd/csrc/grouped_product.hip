@@ -19,6 +19,8 @@
 #include "tile_spread.hpp"
 #include "vec8.hpp"
 
+#include <math.h>
+
 namespace omnimoe {
 namespace {
 
@@ -285,9 +287,10 @@ struct GroupedSumArgs {
   int parts;
 };
 
-// Up to 64 experts, a multiple of eight, whose rows may be very uneven: they go to the XCDs by their rank in rows, to and fro
-// (the first eight to XCDs 0 to 7, the next to 7 to 0, ...), so that each has about as many rows, the longest first. All of
-// an expert's tiles stay on one XCD, whose L2 they share. Returns the expert of rank `want`.
+// Experts' rows may be very uneven. 16 to 64 of them, a multiple of eight, go to the XCDs by their rank in rows, to and fro
+// (the first eight to XCDs 0 to 7, the next to 7 to 0, ...), so that each has about as many rows, the longest first; all of
+// an expert's tiles stay on one XCD, whose L2 they share. Fewer experts' tiles go over all XCDs, the longest expert's first
+// (eight experts of 2048 x 2048, 16384 rows, an XCD each: 270 us). Returns the expert of rank `want`.
 __device__ __forceinline__ int expert_of_rank(const int32_t* offsets, int N, int M, int want) {
   const int l = lane_id(), e = l < N ? l : N - 1;
   const int lo = expert_start(offsets, e, M), hi = expert_start(offsets, e + 1, M), rows = l < N ? (hi > lo ? hi - lo : 0) : -1;
@@ -311,7 +314,11 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArg
   const unsigned tiles_k = (p.k + TN - 1) / TN, tiles_n = (p.n + TM - 1) / TM, each = tiles_k * tiles_n * p.parts;
   unsigned item;
   int e;
-  if (p.offsets && p.N <= 64 && p.N % 8 == 0) {
+  if (p.offsets && p.N > 1 && p.N < 16) {
+    const unsigned rank = blockIdx.x / each;
+    item = blockIdx.x - rank * each;
+    e = __builtin_amdgcn_readfirstlane(expert_of_rank(p.offsets, p.N, p.M, (int)rank));
+  } else if (p.offsets && p.N <= 64 && p.N % 8 == 0) {
     const unsigned xcd = blockIdx.x % 8, at = blockIdx.x / 8, turn = at / each;
     item = at - turn * each;
     e = __builtin_amdgcn_readfirstlane(expert_of_rank(p.offsets, p.N, p.M, (int)(8 * turn + (turn & 1 ? 7 - xcd : xcd))));
@@ -393,15 +400,39 @@ int64_t most_units(int64_t M, int N, int R) {
 RowOrder rows(const Shape& s, const int32_t* perm, int order) { return RowOrder::make(perm, (int)s.M, order, s.hk); }
 int64_t cut(int64_t v, int64_t by) { return (v + by - 1) / by; }
 
-// The tile's side by how many tiles of 256 or 128 the sizes make: as many as keep three quarters, or half, of the compute
-// units busy, of experts that fill at least half of one. fp32: 64 (its products take eight times bf16's time, so that a
-// tile's copies are nothing beside them: 8192 rows, 1024 x 1024, 16 experts 165 us, 104 TFLOP/s; with 128 x 128 197).
-int tile_side(bool bf16, int64_t M, int N, int n) {
+// What bf16 tiles take, in us: a stage of r workgroups that share a compute unit stage[r] (between whole r a straight line;
+// stage[0]: of a few workgroups on the whole card), at most `most` of them, and a tile's start and end `ends`. `tiles`
+// workgroups of `stages` stages run in whole rounds of 256 `most` and a rest.
+struct TileTime {
+  int most;
+  double stage[6], ends;
+};
+constexpr TileTime kTime256 = {1, {1.25, 1.65}, 9}, kTime128 = {2, {0.6, 0.75, 1.1}, 5};
+constexpr TileTime kTime64 = {5, {0.45, 0.45, 0.55, 0.75, 0.95, 1.15}, 4}, kTime64Swiglu = {3, {0.6, 0.62, 0.84, 1.05}, 4};
+double tiles_time(const TileTime& t, double tiles, double stages) {
+  const double slots = 256.0 * t.most, rounds = floor(tiles / slots), r = (tiles - rounds * slots) / 256.0;
+  const double whole = rounds * (stages * t.stage[t.most] + t.ends);
+  if (r <= 0) return whole;
+  const int at = (int)r;
+  return whole + stages * (t.stage[at] + (r - at) * (t.stage[at + 1] - t.stage[at])) + t.ends;
+}
+
+// The tile's side, by these times with half a unit more an expert than its rows fill. Rows, experts, width, of 2048 x 2048
+// matrices (us for 64, 128, 256): 1024, 1: 22, 25, 50; 4096, 1: 55, 40, 52; 4096, 16: 89, 78, 64; 16384, 64: 320, 237, 223;
+// of 1024 x 1024: 16384, 16: 63, 51, 60.
+// fp32: 64 (its products take eight times bf16's time, so that a tile's copies are nothing beside them: 8192 rows,
+// 1024 x 1024, 16 experts 165 us, 104 TFLOP/s; with 128 x 128 197).
+int tile_side(bool bf16, bool swiglu, int64_t M, int N, int k, int n) {
   if (!bf16) return 64;
-  const int64_t rows = M / N;  // of an expert
-  if (rows >= 128 && cut(M, 256) * cut(n, 256) >= 192) return 256;
-  if (rows >= 64 && cut(M, 128) * cut(n, 128) >= 128) return 128;
-  return 64;
+  int best = 64;
+  double least = 0;
+  for (const int side : {64, 128, 256}) {
+    const double some = (double)M / side + (N > 1 ? 0.5 * N : 0.0), units = some < (double)M ? some : (double)M;
+    const TileTime& t = side == 256 ? kTime256 : side == 128 ? kTime128 : swiglu ? kTime64Swiglu : kTime64;
+    const double us = tiles_time(t, ceil(units) * cut(n, side == 64 && swiglu ? 128 : side), cut(k, 64));
+    if (side == 64 || us < least) best = side, least = us;
+  }
+  return best;
 }
 
 template <class T, bool TRANSPOSED, bool SWIGLU>
@@ -413,7 +444,7 @@ hipError_t tiles(const GroupedArgs& p, hipStream_t st) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, st, p);
     return hipGetLastError();
   };
-  const int side = tile_side(T::kSize == 2, p.M, p.N, width);
+  const int side = tile_side(T::kSize == 2, SWIGLU, p.M, p.N, p.k, width);
   if constexpr (T::kSize == 2) {
     if (side == 256) return go(grouped_tile_kernel<T, 256, 256, 2, 4, TRANSPOSED, SWIGLU>, 256, 256, 512);
     if (side == 128) return go(grouped_tile_kernel<T, 128, 128, 4, 2, TRANSPOSED, SWIGLU>, 128, 128, 512);
@@ -449,19 +480,27 @@ hipError_t forward(const GroupedArgs& p, bool swiglu, hipStream_t st) {
   return swiglu ? tiles<T, false, true>(p, st) : tiles<T, false, false>(p, st);
 }
 
-// The weight gradients' tiles, by the same measure; their number does not depend on the rows.
-int sum_side(const Shape& s, int k, int n) {
-  if (!s.bf16) return 64;
-  if (s.N * cut(k, 256) * cut(n, 256) >= 192) return 256;
-  return s.N * cut(k, 128) * cut(n, 128) >= 128 ? 128 : 64;
-}
-
-// Parts of an expert's positions, of 512 at least, where the tiles alone leave compute units idle.
-int sum_parts(const Shape& s, int k, int n) {
-  const int side = sum_side(s, k, n);
-  const int64_t tiles = s.N * cut(k, side) * cut(n, side), wanted = 512 / tiles, most = s.M / s.N / 512;
-  const int64_t parts = wanted < most ? wanted : most;
-  return parts < 1 ? 1 : parts > 32 ? 32 : (int)parts;
+// The weight gradients' tiles, and parts of an expert's positions, of 512 at least, where the tiles leave compute units idle:
+// by the same times, with a tile's more for the experts' unevenness, and parts' way through memory. 16384 rows, 16 experts of
+// 1024 x 1024, both gradients: 119 us with tiles of 128, 171 with 256.
+struct SumPlan {
+  int side, parts;
+};
+SumPlan sum_plan(const Shape& s, int k, int n) {
+  SumPlan best{64, 1};
+  double least = 0;
+  for (const int side : {64, 128, 256}) {
+    if (side > 64 && !s.bf16) break;
+    const int64_t tiles = s.N * cut(k, side) * cut(n, side), wanted = 512 / tiles, most = s.M / s.N / 512;
+    const int64_t cuts = wanted < most ? wanted : most;
+    const int parts = cuts < 1 ? 1 : cuts > 32 ? 32 : (int)cuts;
+    const TileTime& t = side == 256 ? kTime256 : side == 128 ? kTime128 : kTime64;
+    const double stages = (double)s.M / s.N / parts / 64, slots = 256.0 * t.most;
+    const double us = tiles * parts / slots * (stages * t.stage[t.most - 1] + t.ends) + stages * t.stage[1] + t.ends +
+                      (parts > 1 ? 3 + (2.0 * parts * 4 + 2) * s.N * k * n / 4e6 : 0.0);
+    if (side == 64 || us < least) best = {side, parts}, least = us;
+  }
+  return best;
 }
 
 template <class T>
@@ -500,16 +539,16 @@ hipError_t launch_grouped_dx(const Shape& s, const ProductShape& q, const void* 
 }
 
 size_t grouped_dw_ws_bytes(const Shape& s, const ProductShape& q) {
-  const int parts = sum_parts(s, q.n_in, q.n_out);
+  const int parts = sum_plan(s, q.n_in, q.n_out).parts;
   return parts > 1 ? (size_t)parts * s.N * q.n_in * q.n_out * 4 : 0;
 }
 
 hipError_t launch_grouped_dw(const Shape& s, const ProductShape& q, const void* x, const void* dy, const int32_t* offsets,
                              const int32_t* perm, void* dw, void* ws, hipStream_t st) {
+  const SumPlan plan = sum_plan(s, q.n_in, q.n_out);
   const GroupedSumArgs p{x, dy, dw, (float*)ws, offsets, (int)s.N, (int)s.M, q.n_out, q.n_in, rows(s, perm, q.x_order),
-                         rows(s, perm, q.y_order), sum_parts(s, q.n_in, q.n_out)};
-  const int side = sum_side(s, q.n_in, q.n_out);
-  return s.bf16 ? sums<BF16>(p, side, st) : sums<F32>(p, side, st);
+                         rows(s, perm, q.y_order), plan.parts};
+  return s.bf16 ? sums<BF16>(p, plan.side, st) : sums<F32>(p, plan.side, st);
 }
 
 }  // namespace omnimoe
