@@ -48,7 +48,9 @@ omnimoe_status omnimoe_block_join(const omnimoe_layer_desc* desc, float eps, int
  *   dgate  [T, gate_width] dtype out
  *   dw_out, dscale, dw_in  [d] fp32 out, sums over the tokens
  * Outputs whose input is NULL (or with y NULL: not used) are not written and may be NULL. The norms are formed again from
- * x_out and y. T = 0 writes zeros to those of the three sums that are not NULL and uses nothing else. Workspace:
+ * x_out and y. A row's sums are fp32: squares past its largest value are no matter, products of the row's gradients (w_in dn,
+ * and those of w_out norm(y)) with x_out and norm(y) that are past it are. T = 0 writes zeros to those of the three sums that
+ * are not NULL and uses nothing else. Workspace:
  * omnimoe_block_join_backward_workspace_size bytes. */
 omnimoe_status omnimoe_block_join_backward_workspace_size(const omnimoe_layer_desc* desc, size_t* bytes);
 omnimoe_status omnimoe_block_join_backward(const omnimoe_layer_desc* desc, float eps, int32_t gate_width,
@@ -58,7 +60,8 @@ omnimoe_status omnimoe_block_join_backward(const omnimoe_layer_desc* desc, float
                                            void* workspace, size_t workspace_bytes, void* stream);
 
 /* Products of rows grouped by expert: experts that have a matrix each, run on omnimoe_schedule's order. Of the descriptor
- * T, n_rows * n_cols = N experts (at most 4096, else OMNIMOE_ERR_UNSUPPORTED), H, K and dtype; M = T H K tasks.
+ * T, n_rows * n_cols = N experts (at most 4096), H, K and dtype; M = T H K tasks (at most 2^31 - 1024; else
+ * OMNIMOE_ERR_UNSUPPORTED).
  *   offsets [N + 1] int32  expert e's positions are offsets[e] .. offsets[e + 1] - 1 (omnimoe_schedule's dense_offsets, with
  *                          group_size 1): ascending, from 0 to M at most; an expert may have none. Positions from offsets[N]
  *                          on belong to nobody: they are not read and their outputs are left as they were. With N = 1 it
@@ -107,8 +110,8 @@ omnimoe_status omnimoe_grouped_product_dw(const omnimoe_layer_desc* desc, const 
  *                                       max |w| <= 6 2^s
  * store: code = w 2^-s rounded to the nearest of the list, ties to the even place; magnitudes past 6 2^125 become that. A
  * block that holds a value which is not finite has scale byte 255, and all of its values are NaN.
- * load: w = code 2^s, exact in both types, for the scale bytes that store writes: 2 to 252, and 255. Of the descriptor N and dtype, of the product n_in (n_in % 32 == 0), n_out and
- * swiglu. */
+ * load: w = code 2^s, exact in both types, for the scale bytes that store writes: 2 to 252, and 255.
+ * Of the descriptor N and dtype, of the product n_in (n_in % 32 == 0), n_out and swiglu. */
 omnimoe_status omnimoe_weights4_store(const omnimoe_layer_desc* desc, const omnimoe_product* product, const void* w,
                                       uint8_t* codes, uint8_t* scales, void* stream);
 omnimoe_status omnimoe_weights4_load(const omnimoe_layer_desc* desc, const omnimoe_product* product,

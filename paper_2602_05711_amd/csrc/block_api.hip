@@ -17,6 +17,8 @@ omnimoe_status check_join(const omnimoe_layer_desc* desc, float eps, int32_t gat
   return y || w_in || s->T == 0 ? OMNIMOE_OK : OMNIMOE_ERR_INVALID_ARG;
 }
 
+constexpr int64_t kMostRows = kIntMax - 1023;  // (a tile past the last position still counts in 32 bits)
+
 bool valid_width(int32_t n) { return n >= 8 && n <= kMaxFeatures && n % 8 == 0; }
 
 omnimoe_status check_product(const omnimoe_layer_desc* desc, const omnimoe_product* product, Shape* s, ProductShape* q) {
@@ -28,7 +30,7 @@ omnimoe_status check_product(const omnimoe_layer_desc* desc, const omnimoe_produ
       product->y_order < OMNIMOE_ORDER_POSITION || product->y_order > OMNIMOE_ORDER_TASK)
     return OMNIMOE_ERR_INVALID_ARG;
   *q = {product->n_in, product->n_out, product->swiglu == 1, product->x_order, product->y_order};
-  if (s->N > kMaxExperts) return OMNIMOE_ERR_UNSUPPORTED;
+  if (s->N > kMaxExperts || s->M > kMostRows) return OMNIMOE_ERR_UNSUPPORTED;
   const int64_t matrix = (int64_t)(q->swiglu ? 2 : 1) * q->n_out * q->n_in * (s->bf16 ? 2 : 4);
   return matrix >= (int64_t(1) << 32) ? OMNIMOE_ERR_UNSUPPORTED : OMNIMOE_OK;
 }

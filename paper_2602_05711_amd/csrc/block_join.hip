@@ -109,7 +109,8 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs p) {
           s[0] = fmaf(z, z, s[0]);
         }
       block_sums<W>(s, lds, turn);
-      inv = 1.0f / sqrtf(s[0] / (float)p.d + p.eps * pre * pre);
+      s[0] = s[0] / (float)p.d + p.eps * pre * pre;
+      inv = 1.0f / sqrtf(s[0]);
       if (finite(s[0]) || pre != 1.0f) return;
       pre = kSmall;
     }
@@ -233,13 +234,14 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
         s3[2] = fmaf(vy, vy, s3[2]);
       }
       block_sums<W>(s3, lds3, turn3);
+      s3[0] = s3[0] * d1 + p.eps * pre_x * pre_x, s3[2] = s3[2] * d1 + p.eps * pre_y * pre_y;
       if (again || (finite(s3[0]) && finite(s3[2]))) break;  // (the sums are every thread's)
       if (!finite(s3[0])) pre_x = kSmall;
       if (!finite(s3[2])) pre_y = kSmall;
       again = true;
     }
-    const float ix = 1.0f / sqrtf(s3[0] * d1 + p.eps * pre_x * pre_x), m = s3[1] * ix * d1;
-    const float iy = p.w_out ? 1.0f / sqrtf(s3[2] * d1 + p.eps * pre_y * pre_y) : 1.0f;
+    const float ix = 1.0f / sqrtf(s3[0]), m = s3[1] * ix * d1;
+    const float iy = p.w_out ? 1.0f / sqrtf(s3[2]) : 1.0f;
     if (!p.w_out) pre_y = 1.0f;
     float rest = 0.0f;
     const float s = token ? sigmoid(gate, rest) : 1.0f;

@@ -131,6 +131,7 @@ struct GroupedArgs {
   const int32_t* offsets;
   int N, M, k, n;  // k: the summed width, n: the result's
   RowOrder in_rows, out_rows;
+  unsigned block0;
 };
 
 // A wave's 32 x 32 block of results, of which this lane has sixteen values of b's row lane % 32 in fours (a's rows 8 q + 4 (lane /
@@ -177,8 +178,9 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs 
   int tile = -1;
   find_unit<64 * NW>(p.offsets, p.N, p.M, TM, (int*)st0, [&](int total) {
     const int64_t all = (int64_t)total * tiles_n;
-    if (blockIdx.x >= all) return -1;
-    const unsigned item = (unsigned)xcd_contiguous(blockIdx.x, all), unit = item / (unsigned)tiles_n;
+    const unsigned block = p.block0 + blockIdx.x;
+    if (block >= all) return -1;
+    const unsigned item = (unsigned)xcd_contiguous(block, all), unit = item / (unsigned)tiles_n;
     tile = __builtin_amdgcn_readfirstlane((int)(item - unit * tiles_n));
     return (int)unit;
   }, u);
@@ -242,7 +244,8 @@ __global__ __launch_bounds__(64 * W) void grouped_few_kernel(GroupedArgs p, int 
   typedef typename std::conditional<BF16, uint16_t, float>::type elem;
   __shared__ f32x4 tiles[W][RB][64];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int want = blockIdx.x / (unsigned)groups, f0 = (int)(blockIdx.x % (unsigned)groups) * 16 * FB;
+  const unsigned block = p.block0 + blockIdx.x;
+  const int want = block / (unsigned)groups, f0 = (int)(block % (unsigned)groups) * 16 * FB;
   RowUnit u;
   if (find_unit<64 * W>(p.offsets, p.N, p.M, 16, (int*)tiles, [&](int) { return want; }, u) <= want) return;
   __syncthreads();
@@ -285,6 +288,7 @@ struct GroupedSumArgs {
   int N, M, n, k;
   RowOrder x_rows, y_rows;
   int parts;
+  unsigned block0, blocks;
 };
 
 // Experts' rows may be very uneven. 16 to 64 of them, a multiple of eight, go to the XCDs by their rank in rows, to and fro
@@ -312,18 +316,19 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArg
   __shared__ int2 slots[4][64];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
   const unsigned tiles_k = (p.k + TN - 1) / TN, tiles_n = (p.n + TM - 1) / TM, each = tiles_k * tiles_n * p.parts;
+  const unsigned block = p.block0 + blockIdx.x;
   unsigned item;
   int e;
   if (p.offsets && p.N > 1 && p.N < 16) {
-    const unsigned rank = blockIdx.x / each;
-    item = blockIdx.x - rank * each;
+    const unsigned rank = block / each;
+    item = block - rank * each;
     e = __builtin_amdgcn_readfirstlane(expert_of_rank(p.offsets, p.N, p.M, (int)rank));
   } else if (p.offsets && p.N <= 64 && p.N % 8 == 0) {
-    const unsigned xcd = blockIdx.x % 8, at = blockIdx.x / 8, turn = at / each;
+    const unsigned xcd = block % 8, at = block / 8, turn = at / each;
     item = at - turn * each;
     e = __builtin_amdgcn_readfirstlane(expert_of_rank(p.offsets, p.N, p.M, (int)(8 * turn + (turn & 1 ? 7 - xcd : xcd))));
   } else {
-    const unsigned at = (unsigned)xcd_contiguous(blockIdx.x, gridDim.x);
+    const unsigned at = (unsigned)xcd_contiguous(block, p.blocks);
     e = (int)(at / each);
     item = at - e * each;
   }
@@ -439,10 +444,7 @@ template <class T, bool TRANSPOSED, bool SWIGLU>
 hipError_t tiles(const GroupedArgs& p, hipStream_t st) {
   const int width = SWIGLU ? 2 * p.n : p.n;
   auto go = [&](auto kernel, int tm, int tn, int threads) -> hipError_t {
-    const int64_t grid = most_units(p.M, p.N, tm) * cut(p.n, SWIGLU ? tn / 2 : tn);
-    if (grid > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, st, p);
-    return hipGetLastError();
+    return launch_numbered(kernel, most_units(p.M, p.N, tm) * cut(p.n, SWIGLU ? tn / 2 : tn), threads, st, p);
   };
   const int side = tile_side(T::kSize == 2, SWIGLU, p.M, p.N, p.k, width);
   if constexpr (T::kSize == 2) {
@@ -455,9 +457,8 @@ hipError_t tiles(const GroupedArgs& p, hipStream_t st) {
 
 template <bool BF16, bool SWIGLU, int RB, int W>
 hipError_t few_launch(const GroupedArgs& p, int64_t units, hipStream_t st) {
-  const int64_t groups = cut(p.n, SWIGLU ? 8 * RB : 16 * RB), grid = units * groups;
-  hipLaunchKernelGGL((grouped_few_kernel<BF16, RB, SWIGLU, W>), dim3((unsigned)grid), dim3(64 * W), 0, st, p, (int)groups);
-  return hipGetLastError();
+  const int64_t groups = cut(p.n, SWIGLU ? 8 * RB : 16 * RB);
+  return launch_numbered(grouped_few_kernel<BF16, RB, SWIGLU, W>, units * groups, 64 * W, st, p, (int)groups);
 }
 // Two row blocks a workgroup, one where two would leave compute units idle (a matrix of 2048 x 8192, one token: 13.7 us
 // instead of 19.3); eight waves where each has four steps of its loads in flight (64 experts of 2048 x 2048, 4 and 64
@@ -504,12 +505,11 @@ SumPlan sum_plan(const Shape& s, int k, int n) {
 }
 
 template <class T>
-hipError_t sums(const GroupedSumArgs& p, int side, hipStream_t st) {
+hipError_t sums(GroupedSumArgs p, int side, hipStream_t st) {
   auto go = [&](auto kernel, int threads) -> hipError_t {
     const int64_t grid = (int64_t)p.N * p.parts * cut(p.k, side) * cut(p.n, side);
-    if (grid > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, st, p);
-    return hipGetLastError();
+    p.blocks = (unsigned)grid;
+    return launch_numbered(kernel, grid, threads, st, p);
   };
   hipError_t e = hipSuccess;
   if constexpr (T::kSize == 2) {
@@ -528,13 +528,13 @@ hipError_t sums(const GroupedSumArgs& p, int side, hipStream_t st) {
 
 hipError_t launch_grouped_product(const Shape& s, const ProductShape& q, const void* x, const void* w,
                                   const int32_t* offsets, const int32_t* perm, void* y, hipStream_t st) {
-  const GroupedArgs p{x, w, y, offsets, (int)s.N, (int)s.M, q.n_in, q.n_out, rows(s, perm, q.x_order), rows(s, perm, q.y_order)};
+  const GroupedArgs p{x, w, y, offsets, (int)s.N, (int)s.M, q.n_in, q.n_out, rows(s, perm, q.x_order), rows(s, perm, q.y_order), 0};
   return s.bf16 ? forward<BF16>(p, q.swiglu, st) : forward<F32>(p, q.swiglu, st);
 }
 
 hipError_t launch_grouped_dx(const Shape& s, const ProductShape& q, const void* dy, const void* w, const int32_t* offsets,
                              const int32_t* perm, void* dx, hipStream_t st) {
-  const GroupedArgs p{dy, w, dx, offsets, (int)s.N, (int)s.M, q.n_out, q.n_in, rows(s, perm, q.y_order), rows(s, perm, q.x_order)};
+  const GroupedArgs p{dy, w, dx, offsets, (int)s.N, (int)s.M, q.n_out, q.n_in, rows(s, perm, q.y_order), rows(s, perm, q.x_order), 0};
   return s.bf16 ? tiles<BF16, true, false>(p, st) : tiles<F32, true, false>(p, st);
 }
 
@@ -547,7 +547,7 @@ hipError_t launch_grouped_dw(const Shape& s, const ProductShape& q, const void* 
                              const int32_t* perm, void* dw, void* ws, hipStream_t st) {
   const SumPlan plan = sum_plan(s, q.n_in, q.n_out);
   const GroupedSumArgs p{x, dy, dw, (float*)ws, offsets, (int)s.N, (int)s.M, q.n_out, q.n_in, rows(s, perm, q.x_order),
-                         rows(s, perm, q.y_order), plan.parts};
+                         rows(s, perm, q.y_order), plan.parts, 0, 0};
   return s.bf16 ? sums<BF16>(p, plan.side, st) : sums<F32>(p, plan.side, st);
 }
 

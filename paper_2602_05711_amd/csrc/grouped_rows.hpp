@@ -33,7 +33,7 @@ struct RowUnit {
 // `scratch` (NT / 64 + 4 ints of LDS) is free again after the caller's next barrier.
 template <int NT, class Unit>
 __device__ __forceinline__ int find_unit(const int32_t* offsets, int N, int M, int R, int* scratch, Unit unit, RowUnit& u) {
-  auto units = [&](int lo, int hi) { return hi > lo ? (unsigned)(hi - lo + R - 1) / (unsigned)R : 0u; };
+  auto units = [&](int lo, int hi) { return hi > lo ? ((unsigned)(hi - lo) + (unsigned)R - 1u) / (unsigned)R : 0u; };
   u = {-1, 0, 0};
   if (!offsets) {
     const int total = (int)units(0, M), want = unit(total);
@@ -142,5 +142,20 @@ struct RowOrder {
   }
   __device__ __forceinline__ int operator()(int p) const { return of(p, task(p)); }
 };
+
+// `grid` workgroups of kernel(p, more ..), whose number is p.block0 + blockIdx.x: in several launches where one would have 2^32
+// threads or more, which the runtime does not start. Each but the last is of a multiple of eight, so that a number still names
+// its XCD.
+template <class Kernel, class Args, class... More>
+hipError_t launch_numbered(Kernel kernel, int64_t grid, int threads, hipStream_t st, Args p, More... more) {
+  if (grid > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+  const int64_t most = (int64_t)(0xFFFFFFFFu / (unsigned)threads) & ~(int64_t)7;
+  for (int64_t at = 0; at < grid; at += most) {
+    p.block0 = (unsigned)at;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(grid - at < most ? grid - at : most)), dim3(threads), 0, st, p, more...);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
+}
 
 }  // namespace omnimoe

@@ -87,6 +87,7 @@ struct Product4Args {
   const int32_t* offsets;
   int N, M, k, n;
   RowOrder x_rows, y_rows;
+  unsigned block0;
 };
 
 // Eight codes of a lane's block against eight values of each operand's block.
@@ -162,7 +163,8 @@ __global__ __launch_bounds__(64 * W) void product4_kernel(Product4Args p, int gr
   typedef typename std::conditional<BF16, uint16_t, float>::type elem;
   __shared__ f32x4 tiles[W][RB][64];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quad = l >> 4;
-  const int want = blockIdx.x / (unsigned)groups, f0 = (int)(blockIdx.x % (unsigned)groups) * 16 * FB;
+  const unsigned block = p.block0 + blockIdx.x;
+  const int want = block / (unsigned)groups, f0 = (int)(block % (unsigned)groups) * 16 * FB;
   RowUnit u;
   if (find_unit<64 * W>(p.offsets, p.N, p.M, 16, (int*)tiles, [&](int) { return want; }, u) <= want) return;
   __syncthreads();
@@ -238,13 +240,9 @@ __global__ __launch_bounds__(64 * W) void product4_kernel(Product4Args p, int gr
 template <bool BF16, bool SWIGLU, int RB, int W, int U>
 hipError_t product4_launch(const Product4Args& p, int64_t units, hipStream_t st) {
   const int64_t per = SWIGLU ? 8 * RB : 16 * RB, groups = (p.n + per - 1) / per, grid = units * groups;
-  if (grid > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-  const dim3 blocks((unsigned)grid), threads(64 * W);
   if (p.k / 32 % (4 * U) == 0)
-    hipLaunchKernelGGL((product4_kernel<BF16, RB, SWIGLU, W, U, true>), blocks, threads, 0, st, p, (int)groups);
-  else
-    hipLaunchKernelGGL((product4_kernel<BF16, RB, SWIGLU, W, U, false>), blocks, threads, 0, st, p, (int)groups);
-  return hipGetLastError();
+    return launch_numbered(product4_kernel<BF16, RB, SWIGLU, W, U, true>, grid, 64 * W, st, p, (int)groups);
+  return launch_numbered(product4_kernel<BF16, RB, SWIGLU, W, U, false>, grid, 64 * W, st, p, (int)groups);
 }
 
 // Row blocks a workgroup: four where that leaves a thousand workgroups (four a compute unit), two from 256 on, or one (the
@@ -294,7 +292,7 @@ hipError_t launch_grouped_product4(const Shape& s, const ProductShape& q, const 
                                    const uint8_t* scales, const int32_t* offsets, const int32_t* perm, void* y,
                                    hipStream_t st) {
   const Product4Args p{x, codes, scales, y, offsets, (int)s.N, (int)s.M, q.n_in, q.n_out,
-                       RowOrder::make(perm, (int)s.M, q.x_order, s.hk), RowOrder::make(perm, (int)s.M, q.y_order, s.hk)};
+                       RowOrder::make(perm, (int)s.M, q.x_order, s.hk), RowOrder::make(perm, (int)s.M, q.y_order, s.hk), 0};
   if (s.bf16) return q.swiglu ? product4<true, true>(p, st) : product4<true, false>(p, st);
   return q.swiglu ? product4<false, true>(p, st) : product4<false, false>(p, st);
 }

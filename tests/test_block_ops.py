@@ -132,6 +132,8 @@ def test_product_refusals(fn):
     assert _product(fn, _desc(n_rows=64, n_cols=65), _q()) == UNSUPPORTED
     assert _product(fn, d, _q(n_in=65536, n_out=32768)) == UNSUPPORTED  # 4 GiB
     assert _product(fn, _desc(dtype=torch.float32), _q(n_in=32768, n_out=32768)) == UNSUPPORTED
+    # 2^31 - 4 tasks
+    assert _product(fn, _desc(T=2304167, H=233, K=4, n_rows=2, n_cols=2, query_mode="shared"), _q()) == UNSUPPORTED
     assert _product(fn, _desc(T=0), _q(), [(i, None) for i in range(CALLS[fn])]) == OK
     assert _product(fn, _desc(d=60), _q()) == INVALID
     if fn.endswith("dx"):

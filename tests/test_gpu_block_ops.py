@@ -150,6 +150,16 @@ def test_join_extreme_rows(dtype):
     _check_back(i, x_out, "extreme")
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=tid)
+def test_join_with_the_largest_eps(dtype):
+    # a finite mean square and eps whose sum is past fp32's largest value
+    i = _join_inputs(5, 72, dtype, "channel", seed=45)
+    i.eps = float(torch.finfo(F32).max)
+    i.x *= 2.0 ** 59
+    i.y *= 2.0 ** 61
+    _check_back(i, _check_join(i, "eps"), "eps")
+
+
 @pytest.mark.parametrize("bad", [INF, -INF, NAN])
 @pytest.mark.parametrize("where", ["x", "y", "gate"])
 def test_join_keeps_what_is_not_finite_in_its_row(where, bad):
@@ -207,7 +217,8 @@ def test_join_of_a_long_batch():
 ORDERS = [("position", "position"), ("token", "position"), ("task", "task"), ("position", "task"), ("token", "task")]
 
 
-def _case(T, H, Kk, grid, n_in, n_out, dtype, swiglu=False, orders=("token", "position"), idx=None, seed=0):
+def _case(T, H, Kk, grid, n_in, n_out, dtype, swiglu=False, orders=("token", "position"), idx=None, seed=0,
+          weights=True):
     N, M = grid[0] * grid[1], T * H * Kk
     g = torch.Generator().manual_seed(seed + 77)
     if idx is None:
@@ -217,7 +228,8 @@ def _case(T, H, Kk, grid, n_in, n_out, dtype, swiglu=False, orders=("token", "po
                         D=S.desc(T, 64, dtype, n_rows=grid[0], n_cols=grid[1], H=H, K=Kk, query_mode="shared"),
                         q=P.make_product(n_in, n_out, swiglu, *orders), perm=perm.cuda(), offsets=offsets.cuda(),
                         x=S.randn(seed, T if orders[0] == "token" else M, n_in, dtype=dtype),
-                        w=S.randn(seed + 1, N, (2 if swiglu else 1) * n_out, n_in, scale=n_in ** -0.5, dtype=dtype),
+                        w=None if not weights else S.randn(seed + 1, N, (2 if swiglu else 1) * n_out, n_in, scale=n_in ** -0.5,
+                                                           dtype=dtype),
                         dy=S.randn(seed + 2, M, n_out, dtype=dtype))
     if N == 1 and M:
         c.offsets = None
@@ -263,6 +275,10 @@ def _check_product_back(c):
     dx = _run(c, "omnimoe_grouped_product_dx", c.dy, c.w, shape=(c.M, c.k), orders=(x_order, c.orders[1]), q=q)
     dy = _by_position(c, c.dy, c.orders[1])
     within(_written(c, dx, x_order), *K.product_dx(dy, c.w, _ends(c), c.dtype), "dx")
+    return dx, _check_dw(c)
+
+
+def _check_dw(c):
     dw = Guarded((c.N, c.n, c.k), c.dtype)
     dw.t.fill_(float("nan"))
     ws = Guarded((max(256, P.omnimoe_grouped_product_dw_workspace_size(c.D, c.q)),), torch.uint8)
@@ -271,8 +287,9 @@ def _check_product_back(c):
     torch.cuda.synchronize()
     dw.check()
     ws.check()
+    dy = _by_position(c, c.dy, c.orders[1])
     within(dw.t, *K.product_dw(_by_position(c, c.x, c.orders[0]), dy, _ends(c), c.dtype), "dw")
-    return dx, dw.t
+    return dw.t
 
 
 # one token, few rows, ragged tiles of every side, one expert (no offsets), many experts, heads
@@ -310,6 +327,34 @@ def test_product_gradient_orders(dtype, orders):
                          ids=lambda s: "x".join(map(str, s[:3])) + f"-{s[4]}-{s[5]}")
 def test_product_gradient_sizes(shape, dtype):
     _check_product_back(_case(*shape, dtype))
+
+
+# sizes at which the products take tiles of each side
+@pytest.mark.parametrize("swiglu", [False, True], ids=["plain", "swiglu"])
+@pytest.mark.parametrize("shape", [(9000, 1, 1, (2, 4), 264, 776), (4000, 1, 1, (4, 4), 264, 1032),
+                                   (4000, 1, 1, (1, 1), 264, 1032), (4500, 1, 2, (4, 10), 264, 264)],
+                         ids=lambda s: f"{s[0]}-{s[4]}-{s[5]}")
+def test_product_tiles(shape, swiglu):
+    for orders in (("token", "position"), ("task", "task")):
+        _check_product(_case(*shape, BF16, swiglu, orders, seed=11))
+
+
+@pytest.mark.parametrize("shape", [(9000, 1, 1, (2, 4), 776, 264), (4000, 1, 1, (4, 4), 1032, 264), (4000, 1, 1, (1, 1), 264, 264)],
+                         ids=lambda s: f"{s[0]}-{s[4]}-{s[5]}")
+def test_product_gradient_tiles(shape):
+    for orders in (("position", "position"), ("task", "task")):
+        _check_product_back(_case(*shape, BF16, False, orders, seed=12))
+
+
+# dW's tiles of each side, its experts by rank over all XCDs, to and fro, or in order, whole and in parts
+@pytest.mark.parametrize("orders", [("token", "position"), ("position", "task")], ids="-".join)
+@pytest.mark.parametrize("shape", [(4000, 1, 1, (4, 10), 520, 520), (4000, 1, 1, (3, 5), 520, 776), (9000, 1, 1, (1, 1), 520, 776),
+                                   (20000, 1, 1, (1, 3), 264, 520), (3000, 1, 1, (2, 4), 4104, 4104),
+                                   (3000, 1, 1, (3, 8), 2056, 4104), (1500, 1, 2, (2, 13), 2056, 4104),
+                                   (12000, 1, 1, (1, 1), 2056, 2056), (20000, 1, 1, (1, 2), 1288, 1544)],
+                         ids=lambda s: f"{s[0]}-{s[3][0] * s[3][1]}-{s[4]}-{s[5]}")
+def test_weight_gradient_tiles(shape, orders):
+    _check_dw(_case(*shape, BF16, False, orders, seed=13, weights=False))
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=tid)
@@ -407,6 +452,45 @@ def test_product_rows_past_4_gib():
     assert bool((dw[0, :, 3] == 3).all()) and bool((dw[1, :, -1] == 2).all()) and int(dw.count_nonzero()) == 16
 
 
+def _check_rows(x, w, experts, y, at, swiglu=False):
+    """Positions `at` of y, whose rows of x lie there too, by themselves."""
+    one = torch.tensor([0, 1], device="cuda")
+    for p, e in zip(at, experts):
+        want, bound = K.product(x[p:p + 1].to(F64), w[e:e + 1], one, swiglu, BF16)
+        within(y[p:p + 1], want, bound, f"position {p}")
+
+
+def _no_nan(y, rows):
+    assert not any(bool(torch.isnan(y[i:i + rows]).any()) for i in range(0, len(y), rows))
+
+
+def test_few_rows_past_2_32_threads():
+    T, N, n = 4096, 4096, 65536
+    D = S.desc(T, 64, BF16, n_rows=64, n_cols=64, K=2, query_mode="shared")
+    x, w = S.randn(1, 2 * T, 8, dtype=BF16), torch.randn((N, 2 * n, 8), dtype=BF16, device="cuda")
+    offsets = torch.arange(0, 2 * N + 1, 2, dtype=torch.int32, device="cuda")
+    y = torch.full((2 * T, n), NAN, dtype=BF16, device="cuda")
+    P.omnimoe_grouped_product(D, P.make_product(8, n, True, "position", "position"), x, w, offsets, None, y)
+    at = [0, 1, 2, 4095, 6000, 7279, 7280, 7281, 7282, 8000, 8190, 8191]
+    _check_rows(x, w, [p // 2 for p in at], y, at, True)
+    _no_nan(y, 2048)
+
+
+def test_tiles_past_2_32_threads():
+    T, H = 4194307, 128
+    M = T * H * 2
+    D = S.desc(T, 64, BF16, n_rows=1, n_cols=2, H=H, K=2, query_mode="shared")
+    x = torch.ones((M, 8), dtype=BF16, device="cuda")
+    x[M - 1], x[M // 2], x[0] = 3.0, 5.0, 7.0
+    w = S.randn(3, 2, 8, 8, dtype=BF16)
+    offsets = torch.tensor([0, M // 2 + 100, M], dtype=torch.int32, device="cuda")
+    y = torch.full((M, 8), NAN, dtype=BF16, device="cuda")
+    P.omnimoe_grouped_product(D, P.make_product(8, 8, False, "position", "position"), x, w, offsets, None, y)
+    at = [0, 1, M // 2, M // 2 + 99, M // 2 + 100, M - 129, M - 2, M - 1]
+    _check_rows(x, w, [int(p >= M // 2 + 100) for p in at], y, at)
+    assert bool((y[1:M // 2] == y[1]).all()) and bool((y[M // 2 + 100:M - 1] == y[M - 2]).all())
+
+
 # ------------------------------------------------------------------ 4-bit weights
 
 def _store(D, q, w):
@@ -482,6 +566,17 @@ def test_product4_with_every_code_and_scale(dtype):
     want = K.dequantise4(codes, scales)[0].t()
     assert torch.equal(torch.nan_to_num(y.to(F64), nan=1234.5), torch.nan_to_num(want, nan=1234.5))
     assert bool(torch.isnan(y[:, 255]).all()) and bool(torch.isfinite(y[:, :255]).all())
+
+
+def test_product4_past_2_32_threads():
+    M, n = 131088, 65536
+    D, q = S.desc(M, 64, BF16, n_rows=1, n_cols=1, K=1, query_mode="shared"), P.make_product(32, n, True, "position", "position")
+    codes, scales, w = _store(D, q, S.randn(5, 1, 2 * n, 32, dtype=BF16))
+    x, y = S.randn(6, M, 32, dtype=BF16), torch.full((M, n), NAN, dtype=BF16, device="cuda")
+    P.omnimoe_grouped_product4(D, q, x, codes, scales, None, None, y)
+    at = [0, 17, 65535, 131055, 131056, 131071, 131072, 131087]
+    _check_rows(x, w, [0] * len(at), y, at, True)
+    _no_nan(y, 8192)
 
 
 def test_product4_positions_of_nobody():
