@@ -167,10 +167,11 @@ __device__ __forceinline__ void put_block(const float (&v)[16], int lane, void* 
 template <class T, int TM, int TN, int WR, int WC, bool TRANSPOSED, bool SWIGLU>
 __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs p) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32, FN = SWIGLU ? TN / 2 : TN;
-  constexpr bool kSpread = TM == 256 && SWIGLU;
+  constexpr bool kSpread = TM == 256 && SWIGLU, kRing = TM < 256;
   static_assert(!SWIGLU || (NI % 2 == 0 && !TRANSPOSED), "a wave's gate and up rows");
   typedef typename T::elem elem;
   __shared__ __attribute__((aligned(1024))) unsigned char st0[(TM + TN) * 128], st1[(TM + TN) * 128];
+  __shared__ __attribute__((aligned(1024))) unsigned char st2[kRing ? (TM + TN) * 128 : 16], st3[kRing ? (TM + TN) * 128 : 16];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wid / WC, wc = wid % WC;
   const int tiles_n = (p.n + FN - 1) / FN;
   // neighbouring tiles, which share rows or weights, go to one XCD
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs 
     const int row = p.in_rows(u.first + (r < u.count ? r : u.count - 1));
     return row < 0 ? 0 : row;
   });
-  typename std::conditional<kSpread, SpreadOperand<T, TN, TRANSPOSED, NW>, TileOperand<T, TN, TRANSPOSED, NW>>::type a;
+  typename std::conditional<kSpread || kRing, SpreadOperand<T, TN, TRANSPOSED, NW>, TileOperand<T, TN, TRANSPOSED, NW>>::type a;
   const elem* const w = (const elem*)p.w + (int64_t)u.expert * (SWIGLU ? 2 : 1) * p.n * p.k;
   if constexpr (TRANSPOSED)
     a.init(w, p.n, wid, lane, [&](int r) { return n0 + r < p.n ? n0 + r : p.n - a.kPer; });
@@ -210,6 +211,8 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs 
     });
   if constexpr (kSpread) {
     spread_sum<T>(a, b, p.k, a0, b0, wr * (TM / WR) < u.count, st0, st1, wid, lane, acc, [](int) {});
+  } else if constexpr (kRing) {
+    ring_sum<T>(a, b, p.k, a0, b0, st0, st1, st2, st3, wid, lane, acc, [](int) {});
   } else {
     const TileRange all[2] = {{p.k, 0, 0}, {0, 0, 0}};
     tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);

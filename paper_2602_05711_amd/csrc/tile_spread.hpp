@@ -119,4 +119,71 @@ __device__ __forceinline__ void spread_sum(const OA& a, const OB& b, int K, cons
   __syncthreads();
 }
 
+// The same sum for small tiles, whose stages are shorter than a copy's way: four stages in LDS, three of them on their way.
+// Four __shared__ arrays st0 .. st3 hold a stage of both operands each; ahead(s) runs in stage s behind its barrier, before
+// the copies of stage s + 3. Every thread of the workgroup takes part; on return the LDS is free.
+template <class T, class OA, class OB, int MI, int NJ, class Ahead>
+__device__ __forceinline__ void ring_sum(const OA& a, const OB& b, int K, const int (&a0)[MI], const int (&b0)[NJ],
+                                         unsigned char* st0, unsigned char* st1, unsigned char* st2, unsigned char* st3,
+                                         int wid, int lane, tg_f32x16 (&acc)[MI][NJ], Ahead ahead) {
+  if (K <= 0) return;
+  const int n = (K + T::kStep - 1) / T::kStep;  // (and stages of zeros to a multiple of four)
+  constexpr int kTwo = 2 * (OA::kCopies + OB::kCopies);  // a wave's copies of two stages
+  static_assert(kTwo < 64, "vmcnt");
+  typename T::frag fa[4][MI], fb[4][NJ];
+  auto copy = [&](unsigned char* st, int s) {  // (past the end: zeros, so that the count of copies holds)
+    a.copy(st, 0, s, K, wid, lane);
+    b.copy(st, OA::kBytes, s, K, wid, lane);
+  };
+  auto read = [&](const unsigned char* st, int ks) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) fb[ks][j] = OB::frag(st, OA::kBytes, b0[j], ks, lane);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) fa[ks][i] = OA::frag(st, 0, a0[i], ks, lane);
+  };
+  auto mma = [&](int ks) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) tile_mma(acc[i][j], fa[ks][i], fb[ks][j]);
+  };
+  auto stage = [&](unsigned char* cur, unsigned char* last, int s) {
+    // This stage's copies have arrived, and with the barrier everyone's; nobody reads the last stage's (its reads were
+    // waited for by its products). A fence would wait for the copies on their way too, which __syncthreads has.
+    __builtin_amdgcn_s_waitcnt(0x0070 | (kTwo & 15) | (kTwo >> 4 << 14));  // vmcnt(kTwo) lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    ahead(s);
+    __builtin_amdgcn_sched_barrier(0);
+    copy(last, s + 3);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) read(cur, ks);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) mma(ks);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  copy(st0, 0);
+  copy(st1, 1);
+  copy(st2, 2);
+  auto four = [&](int s) {
+    stage(st0, st3, s);
+    stage(st1, st0, s + 1);
+    stage(st2, st1, s + 2);
+    stage(st3, st2, s + 3);
+  };
+  // (the compiler waits for all copies at a loop's head, whose array it can not tell)
+  int s = 0;
+#pragma unroll 1
+  for (; s + 8 <= n; s += 8) {
+    four(s);
+    four(s + 4);
+  }
+#pragma unroll 1
+  for (; s < n; s += 4) four(s);
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  __syncthreads();
+}
+
 }  // namespace omnimoe
