@@ -212,7 +212,7 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs 
   if constexpr (kSpread) {
     spread_sum<T>(a, b, p.k, a0, b0, wr * (TM / WR) < u.count, st0, st1, wid, lane, acc, [](int) {});
   } else if constexpr (kRing) {
-    ring_sum<T>(a, b, p.k, a0, b0, st0, st1, st2, st3, wid, lane, acc, [](int) {});
+    ring_sum<T>(a, b, p.k, a0, b0, st0, st1, st2, st3, wid, lane, acc);
   } else {
     const TileRange all[2] = {{p.k, 0, 0}, {0, 0, 0}};
     tile_sum<T>(a, b, all, a0, b0, st0, st1, wid, lane, acc);
@@ -415,8 +415,9 @@ struct TileTime {
   int most;
   double stage[6], ends;
 };
-constexpr TileTime kTime256 = {1, {1.25, 1.65}, 9}, kTime128 = {2, {0.6, 0.75, 1.1}, 5};
-constexpr TileTime kTime64 = {5, {0.45, 0.45, 0.55, 0.75, 0.95, 1.15}, 4}, kTime64Swiglu = {3, {0.6, 0.62, 0.84, 1.05}, 4};
+constexpr TileTime kTime256 = {1, {1.25, 1.65}, 9}, kTime128 = {1, {0.5, 0.66}, 2.7}, kTime64 = {2, {0.24, 0.3, 0.55}, 2.2};
+constexpr TileTime kTime64Swiglu = {1, {0.43, 0.47}, 2.3};
+constexpr TileTime kSum128 = {2, {0.6, 0.75, 1.1}, 5}, kSum64 = {5, {0.45, 0.45, 0.55, 0.75, 0.95, 1.15}, 4};  // (two stages in LDS)
 double tiles_time(const TileTime& t, double tiles, double stages) {
   const double slots = 256.0 * t.most, rounds = floor(tiles / slots), r = (tiles - rounds * slots) / 256.0;
   const double whole = rounds * (stages * t.stage[t.most] + t.ends);
@@ -426,10 +427,10 @@ double tiles_time(const TileTime& t, double tiles, double stages) {
 }
 
 // The tile's side, by these times with half a unit more an expert than its rows fill. Rows, experts, width, of 2048 x 2048
-// matrices (us for 64, 128, 256): 1024, 1: 22, 25, 50; 4096, 1: 55, 40, 52; 4096, 16: 89, 78, 64; 16384, 64: 320, 237, 223;
-// of 1024 x 1024: 16384, 16: 63, 51, 60.
+// matrices (us for 64, 128, 256): 1024, 1: 19, 20, 51; 4096, 1: 76, 45, 53; 4096, 16: 93, 70, 64; 16384, 64: 352, 257, 228;
+// 8192, 64, whose weights take 110 us to read: 207, 171, 193 (the rule takes 256); of 1024 x 1024: 16384, 16: 80, 65, 63.
 // fp32: 64 (its products take eight times bf16's time, so that a tile's copies are nothing beside them: 8192 rows,
-// 1024 x 1024, 16 experts 165 us, 104 TFLOP/s; with 128 x 128 197).
+// 1024 x 1024, 16 experts 169 us, 102 TFLOP/s).
 int tile_side(bool bf16, bool swiglu, int64_t M, int N, int k, int n) {
   if (!bf16) return 64;
   int best = 64;
@@ -498,7 +499,7 @@ SumPlan sum_plan(const Shape& s, int k, int n) {
     const int64_t tiles = s.N * cut(k, side) * cut(n, side), wanted = 512 / tiles, most = s.M / s.N / 512;
     const int64_t cuts = wanted < most ? wanted : most;
     const int parts = cuts < 1 ? 1 : cuts > 32 ? 32 : (int)cuts;
-    const TileTime& t = side == 256 ? kTime256 : side == 128 ? kTime128 : kTime64;
+    const TileTime& t = side == 256 ? kTime256 : side == 128 ? kSum128 : kSum64;
     const double stages = (double)s.M / s.N / parts / 64, slots = 256.0 * t.most;
     const double us = tiles * parts / slots * (stages * t.stage[t.most - 1] + t.ends) + stages * t.stage[1] + t.ends +
                       (parts > 1 ? 3 + (2.0 * parts * 4 + 2) * s.N * k * n / 4e6 : 0.0);
