@@ -464,10 +464,10 @@ hipError_t few_launch(const GroupedArgs& p, int64_t units, hipStream_t st) {
   const int64_t groups = cut(p.n, SWIGLU ? 8 * RB : 16 * RB);
   return launch_numbered(grouped_few_kernel<BF16, RB, SWIGLU, W>, units * groups, 64 * W, st, p, (int)groups);
 }
-// Two row blocks a workgroup, one where two would leave compute units idle (a matrix of 2048 x 8192, one token: 13.7 us
-// instead of 19.3); eight waves where each has four steps of its loads in flight (64 experts of 2048 x 2048, 4 and 64
-// tokens: 47 and 121 us, with four waves 54 and 126), else four (16 fp32 experts of 512 x 1024, 8 tokens: 8.4 us, with eight
-// 10.1). Four row blocks: 62 and 144 us.
+// Two row blocks a workgroup, one where two would leave compute units idle (a matrix of 2048 x 8192, one token, before tiles
+// took it: 13.7 us instead of 19.3); eight waves where each has four steps of its loads in flight (64 experts of 2048 x 2048,
+// 4 and 64 tokens: 47 and 121 us, with four waves 54 and 126), else four (16 fp32 experts of 512 x 1024, 8 tokens: 8.4 us,
+// with eight 10.1). Four row blocks: 62 and 144 us.
 template <bool BF16, bool SWIGLU>
 hipError_t few(const GroupedArgs& p, hipStream_t st) {
   const int64_t units = most_units(p.M, p.N, 16), blocks = units * cut((SWIGLU ? 2 : 1) * p.n, 16);
@@ -476,12 +476,22 @@ hipError_t few(const GroupedArgs& p, hipStream_t st) {
   return blocks >= 512 ? few_launch<BF16, SWIGLU, 2, 8>(p, units, st) : few_launch<BF16, SWIGLU, kLeast, 8>(p, units, st);
 }
 
+// Whether a pass over the weights for every sixteen positions is faster than tiles of 64, whose copies bring the weights as
+// fast once there is a workgroup for every other compute unit. us of both, bf16: 2048 x 2048, one expert, 64 positions 8.5 and
+// 10.1, 96 13.8 and 10.3; 16 experts, 32 28 and 20; 64 experts, 8 14.9 and 11.7, 512 113 and 98; one of 2048 x 8192, 64 26 and
+// 10.5. SwiGLU, whose tiles are one a compute unit, 2048 x 1024: one expert, 128 14.0 and 16.1; 16 experts, 128 37 and 31; 64
+// experts, 128 78 and 81, 256 95 and 105. fp32, whose tiles' products take longer: 1024 x 1024, one expert, 192 15.8 and 21.6;
+// 16 experts, 256 27 and 22; 64 experts, 512 75 and 79; 512 x 512, 16 experts, 256 9.0 and 12.4.
+bool few_rows(bool bf16, bool swiglu, int64_t M, int N, int n) {
+  if (!bf16) return M <= 192 || M <= 8 * (int64_t)N || M * n <= 1 << 17;
+  const int64_t units = most_units(M, N, 16);
+  if (swiglu) return units <= 8 || (N >= 32 && M <= 6 * (int64_t)N);
+  return units <= 5 && most_units(M, N, 64) * cut(n, 64) < 128;
+}
+
 template <class T>
 hipError_t forward(const GroupedArgs& p, bool swiglu, hipStream_t st) {
-  // Up to 64 positions, or six an expert, a pass over the weights for every sixteen of them; then tiles. 2048 x 2048: one
-  // expert, 64 positions 8.5 us, as tiles 12.5; 16 experts, 64 35 and 36, 128 44 and 37; 64 experts, 512 118 and 129, 768 137
-  // and 132. (One expert's tiles are few: 128 positions 13.8 and 18.8, 256 25 and 19.)
-  if (p.M <= 64 || p.M <= 6 * (int64_t)p.N) return swiglu ? few<T::kSize == 2, true>(p, st) : few<T::kSize == 2, false>(p, st);
+  if (few_rows(T::kSize == 2, swiglu, p.M, p.N, p.n)) return swiglu ? few<T::kSize == 2, true>(p, st) : few<T::kSize == 2, false>(p, st);
   return swiglu ? tiles<T, false, true>(p, st) : tiles<T, false, false>(p, st);
 }
 
