@@ -8,7 +8,7 @@
 // of 2048 on 64 experts of 2048 x 2048 with SwiGLU 1010 us, 1.09 PFLOP/s, 65536 rows' dx 570 and dW 655 us, 0.96 and 0.84;
 // the library's dense product of 131072 x 2048 x 2048 reaches 1.36. Without its copies the loop runs at 1.34 to 1.54. Two groups
 // of waves that take turns at the products, and workgroups that go from tile to tile, were no faster (1065 and 1074 us).
-// Few rows an expert: the time is that of reading the weights of the experts that have rows, and of little beside it
+// Few rows: the time is that of reading the weights of the experts that have rows, and of little beside it
 // (few_tile.hpp): a unit is up to sixteen rows, a workgroup takes 16 or 32 weight rows and splits the summed index over its
 // waves. 128 rows on 64 experts of 2048 x 2048: 86 us, 5.5 TB/s.
 // Sums are fp32, rounded once; every result has one order of summation, so that it is the same on every run.
