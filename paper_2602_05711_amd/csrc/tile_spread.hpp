@@ -150,8 +150,10 @@ __device__ __forceinline__ void ring_sum(const OA& a, const OB& b, int K, const 
       for (int j = 0; j < NJ; ++j) tile_mma(acc[i][j], fa[ks][i], fb[ks][j]);
   };
   auto stage = [&](unsigned char* cur, unsigned char* last, int s) {
-    // This stage's copies have arrived, and with the barrier everyone's; nobody reads the last stage's (its reads were
-    // waited for by its products). A fence would wait for the copies on their way too, which __syncthreads has.
+    // This stage's copies have arrived, and with the barrier everyone's, and nobody reads the last stage's any more: the wave's
+    // reads are back (lgkmcnt), and the compiler moves no access over the empty statements. A fence, which __syncthreads has,
+    // would wait for the copies on their way too.
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0x0070 | (kTwo & 15) | (kTwo >> 4 << 14));  // vmcnt(kTwo) lgkmcnt(0)
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
