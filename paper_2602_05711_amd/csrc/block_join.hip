@@ -66,8 +66,11 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (&lds)[2][W][N],
   }
 }
 
-// Where a row's squares pass fp32's range they are formed of values times this.
-constexpr float kSmall = 0x1p-70f;
+// Where the sum of a row's squares passes fp32's range they are formed of values times this: of at most 2^56, so that
+// 2^15 squares sum to less than 2^128. (A value is multiplied with the norm's factor first, then with this, which rounds
+// nothing that is not below fp32's normal values in the end.)
+constexpr float kSmall = 0x1p-72f;
+static_assert(kMaxWidth <= 1 << 15, "a row's squares");
 
 __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
 
@@ -138,7 +141,7 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs p) {
       for (int c = 0; c < C; ++c) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float b = a[c][e] * (y[c][e] * pre * inv);
+          float b = a[c][e] * (y[c][e] * inv * pre);
           b *= p.gate_width > 1 ? sigmoid(g[c][e]) : s;
           x[c][e] += b;
         }
@@ -153,7 +156,7 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs p) {
       const int at = c * NT + tid;
       if (at >= q8) continue;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[c][e] = w_in[c][e] * (x[c][e] * pre * inv);
+      for (int e = 0; e < 8; ++e) x[c][e] = w_in[c][e] * (x[c][e] * inv * pre);
       store8<BF16>(p.n, t * p.d + at * 8, x[c]);
     }
   }
@@ -249,11 +252,11 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       if (p.w_in) {
-        const float xh = x[e] * pre_x * ix;
+        const float xh = x[e] * ix * pre_x;
         G[e] += ix * (u[e] - xh * m) * pre_x;
         sum_n[e] = fmaf(dn[e], xh, sum_n[e]);
       }
-      y[e] = y[e] * pre_y * iy;  // yh
+      y[e] = y[e] * iy * pre_y;  // yh
       const float Gs = G[e] * (channel ? sigmoid(g[e], g[e]) : s);
       sum_s[e] = fmaf(Gs, y[e], sum_s[e]);
       x[e] = Gs * a[e];  // q

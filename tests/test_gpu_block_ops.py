@@ -150,6 +150,34 @@ def test_join_extreme_rows(dtype):
     _check_back(i, x_out, "extreme")
 
 
+@pytest.mark.parametrize("gate", ["none", "token", "channel"])
+@pytest.mark.parametrize("d,dtype", [(8192, BF16), (5000, BF16), (4096, F32), (1024, BF16), (512, F32)])
+def test_join_of_the_largest_values(d, dtype, gate):
+    # whole rows of the types' largest values: the sum of their squares, formed of smaller units, is in range at every width
+    i = _join_inputs(4, d, dtype, gate, seed=41)
+    i.y[1] = torch.sign(i.y[1]) * torch.finfo(F32).max
+    i.x[2] = torch.sign(i.x[2]) * torch.finfo(dtype).max
+    i.y[3], i.x[3] = i.y[1], i.x[2] * 0.75
+    i.gate = None if i.gate is None else i.gate.clamp(max=0)  # (the sum of x and the branch stays in range)
+    x_out = _check_join(i, "largest")
+    _check_back(i, x_out, "largest")
+
+
+@pytest.mark.parametrize("d", [8, 520, 2048])
+def test_join_of_small_values_beside_a_large_one(d):
+    # the row's squares pass fp32's range; the norms of its other values, far below them, are still normal numbers (2^-125)
+    i = _join_inputs(3, d, F32, "none", ("scale",), seed=42)
+    some = lambda seed: torch.sign(S.randn(seed, 3, d)) * (1 + S.randn(seed + 1, 3, d).abs().clamp(max=1))  # noqa: E731
+    i.w_out, i.w_in = i.w_out.clamp(0.75, 1.25), i.w_in.clamp(0.75, 1.25)
+    i.x.zero_()
+    i.y = some(43) * 2.0 ** -60
+    i.y[:, 3] = 1.5 * 2.0 ** 64
+    _check_join(i, "beside")
+    i.x, i.dx_out, i.dn = some(45) * 2.0 ** -60, some(47), some(49)
+    i.x[:, 3] = 1.5 * 2.0 ** 64
+    _check_back(i, i.x, "beside")
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=tid)
 def test_join_with_the_largest_eps(dtype):
     # a finite mean square and eps whose sum is past fp32's largest value
