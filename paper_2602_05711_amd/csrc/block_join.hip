@@ -237,7 +237,7 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
         s3[2] = fmaf(vy, vy, s3[2]);
       }
       block_sums<W>(s3, lds3, turn3);
-      s3[0] = s3[0] * d1 + p.eps * pre_x * pre_x, s3[2] = s3[2] * d1 + p.eps * pre_y * pre_y;
+      s3[0] = fmaf(s3[0], d1, p.eps * pre_x * pre_x), s3[2] = fmaf(s3[2], d1, p.eps * pre_y * pre_y);
       if (again || (finite(s3[0]) && finite(s3[2]))) break;  // (the sums are every thread's)
       if (!finite(s3[0])) pre_x = kSmall;
       if (!finite(s3[2])) pre_y = kSmall;
@@ -271,9 +271,9 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
       for (int e = 0; e < 8; ++e) v[e] = g[e] * (x[e] * y[e]);
       store8<BF16>(p.dgate, at, v);
     }
-    if (!p.w_out && !token) {
+    if (!p.w_out) {  // dy = q, whatever y is
       if (in) store8<false>(p.dy, at, x);
-      continue;
+      if (!token) continue;
     }
     block_sums<W>(sq, lds1, turn1);
     if (token && threadIdx.x == 0) {
@@ -281,8 +281,8 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
       if constexpr (BF16) ((uint16_t*)p.dgate)[t] = bf16_rne(v);
       else ((float*)p.dgate)[t] = v;
     }
-    if (!in) continue;
-    const float m2 = p.w_out ? sq[0] * d1 : 0.0f;
+    if (!p.w_out || !in) continue;
+    const float m2 = sq[0] * d1;
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = iy * (x[e] - y[e] * m2) * pre_y;
     store8<false>(p.dy, at, y);

@@ -205,6 +205,20 @@ def test_join_keeps_what_is_not_finite_in_its_row(where, bad):
         assert not bool(torch.isfinite(x_out[4]).all()) and not bool(torch.isfinite(got["dx"][4].float()).all())
 
 
+@pytest.mark.parametrize("gate", ["none", "token", "channel"])
+@pytest.mark.parametrize("dtype", TYPES, ids=tid)
+@pytest.mark.parametrize("bad", [INF, NAN])
+def test_join_without_its_norm_passes_gradients_by_y(bad, dtype, gate):
+    # dy is the branch's factor times the stream's gradient, whatever y holds, with every form of the gate
+    i = _join_inputs(5, 264, dtype, gate, ("w_out",), seed=55)
+    x_out = i.x.clone()
+    clean = _join_back(i, x_out)
+    i.y[2, 100] = bad
+    got = _join_back(i, x_out)
+    assert same_bits(got["dy"], clean["dy"]) and bool(torch.isfinite(got["dy"]).all())
+    assert same_bits(got["dx"], clean["dx"]) and same_bits(got["dw_in"], clean["dw_in"])
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=tid)
 def test_join_in_place(dtype):
     i = _join_inputs(33, 520, dtype, seed=60)
