@@ -168,6 +168,10 @@ struct BackRow {
   Raw8<BF16> x, dn, dx_out, gate;
   Raw8<false> y;
   float token;
+  __device__ __forceinline__ void zero() {
+    x.zero(), dn.zero(), dx_out.zero(), gate.zero(), y.zero();
+    token = 0.0f;
+  }
   __device__ __forceinline__ void load(const JoinArgs& p, int64_t t, int c0, bool in) {
     if (p.y && p.gate_width == 1) token = BF16 ? bf16_lo(((const uint16_t*)p.gate)[t]) : ((const float*)p.gate)[t];
     if (!in) return;
@@ -194,8 +198,7 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
   const float d1 = 1.0f / (float)p.d;
   const bool channel = p.y && p.gate_width > 1, token = p.y && p.gate_width == 1;
   BackRow<BF16> raw;
-  raw.x.zero(), raw.dn.zero(), raw.dx_out.zero(), raw.gate.zero(), raw.y.zero();
-  raw.token = 0.0f;
+  raw.zero();
   const int64_t stride = gridDim.x;
   int64_t t = blockIdx.x;
   constexpr bool kAhead = W < 16;  // (sixteen waves' registers do not hold two rows)
@@ -215,7 +218,10 @@ __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {
   }
   for (; t < p.T; t += stride) {
     float x[8], y[8], u[8], G[8], g[8], dn[8];
-    if (!kAhead) raw.load(p, t, c0, in);
+    if (!kAhead) {
+      raw.zero();  // (whose registers are free between the rows, so that nothing is spilled)
+      raw.load(p, t, c0, in);
+    }
     raw.x.values(x);
     raw.dn.values(dn);
     raw.dx_out.values(G);
