@@ -230,9 +230,20 @@ __global__ __launch_bounds__(64 * WR * WC) void grouped_tile_kernel(GroupedArgs 
     for (int i = 0; i < NI; i += SWIGLU ? 2 : 1) {
       float v[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        v[e] = acc[i][j][e];
-        if constexpr (SWIGLU) v[e] = swiglu<T::kSize == 2>(v[e], acc[i + 1][j][e]);
+      for (int e = 0; e < 16; ++e) v[e] = acc[i][j][e];
+      if constexpr (SWIGLU) {
+        constexpr bool kBf16 = T::kSize == 2;
+        // (the bits of negative values, as whole numbers, are in the order of their magnitude and above all positive ones)
+        uint32_t low = 0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) low = max(low, __float_as_uint(v[e]));
+        if (__any(low > __float_as_uint(kDeepGate))) {  // a gate of the block's is below kDeepGate
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e] = swiglu<kBf16>(v[e], acc[i + 1][j][e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e] = swiglu_near<kBf16>(v[e], acc[i + 1][j][e]);
+        }
       }
       const int f = n0 + (SWIGLU ? a0[i] / 2 : a0[i]);
       put_block<T>(v, lane, (elem*)p.out + (int64_t)row * p.n + f, [&](int c) { return row >= 0 && f + c < p.n; });

@@ -32,13 +32,25 @@ __device__ __forceinline__ void put4(float* p, float a, float b, float c, float 
   *(float4*)p = make_float4(a, b, c, d);
 }
 
-// silu(g) u for a result in the layer's type: bf16's from the hardware's exp2 and reciprocal, whose errors (2^-22 relative,
-// and |g| 2^-24 from the exponent's rounding) are far below its rounding; six instructions instead of forty, of which a
-// tile of 256 x 256 has as many as a quarter of its products' time.
+// silu(g) u for a result in the layer's type, g at least kDeepGate (or NaN): bf16's from the hardware's exp2 and reciprocal,
+// whose errors (2^-22 relative, and |g| 2^-23 from the exponent's roundings) are far below its rounding; six instructions instead
+// of forty, of which a tile of 256 x 256 has as many as a quarter of its products' time.
 template <bool BF16>
-__device__ __forceinline__ float swiglu(float g, float u) {
+__device__ __forceinline__ float swiglu_near(float g, float u) {
   if constexpr (BF16) return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504088896341f)) * u;
   else return activation(1, g) * u;
+}
+
+// Below, e^-g and its reciprocal leave fp32's normal values (from -87 on) before silu(g) u does. There silu(g) = g e^g to fp32's
+// accuracy, formed as g q u q^3 with q = e^(g/4), which is a normal value down to g = -349.
+constexpr float kDeepGate = -80.0f;
+template <bool BF16>
+__device__ __forceinline__ float swiglu(float g, float u) {
+  if (!(g < kDeepGate)) return swiglu_near<BF16>(g, u);
+  float q;
+  if constexpr (BF16) q = __builtin_amdgcn_exp2f(g * (0.25f * 1.44269504088896341f));
+  else q = expf(0.25f * g);
+  return g * q * u * q * q * q;
 }
 
 // (bf16: rounded to nearest even)

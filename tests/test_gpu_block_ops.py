@@ -450,6 +450,56 @@ def test_positions_of_nobody(dtype, M):
     assert bool(torch.isfinite(dw).all())
 
 
+GATES = [-400, -349, -200, -187, -180, -177, -150, -128, -110, -104, -100, -92, -89, -88.5, -88, -87, -80.5, -80, -79.5, -40,
+         -1, 0, 1, 40, 88, 89, 100]
+
+
+def _gated_case(shape, dtype, seed):
+    """Rows of x that pick one value of every weight row, so that gate and up value are known exactly; gates from -400 to 100,
+    up values from 2^-20 to 2^100."""
+    c = _case(*shape, dtype, True, seed=seed)
+    g = torch.Generator().manual_seed(seed)
+    gate = torch.rand((c.N, c.n, c.k), generator=g) * 200 - 100
+    gate.view(-1)[:27 * (gate.numel() // 27 // 3)].view(-1, 27)[:] = torch.tensor(GATES)
+    up = torch.exp2(torch.randint(-20, 101, gate.shape, generator=g).float()) * (torch.rand(gate.shape, generator=g) + 0.5)
+    c.w = torch.cat((gate, up), 1).to(dtype).cuda()
+    c.x = torch.zeros((c.T, c.k), dtype=dtype, device="cuda")
+    c.at = torch.arange(c.T, device="cuda") % c.k
+    c.x[torch.arange(c.T, device="cuda"), c.at] = 1.0
+    return c
+
+
+def _check_gates(c, fn, weights, w):
+    got = _run(c, fn, c.x, *weights, shape=(c.M, c.n), orders=c.orders)
+    expert = torch.repeat_interleave(torch.arange(c.N, device="cuda"), (_ends(c)[1:] - _ends(c)[:-1]).long())
+    rows = w[expert, :, c.at[c.perm.long() // c.hk]].to(F64)
+    g, u = rows[:, :c.n], rows[:, c.n:]
+    want = S.silu(g) * u
+    # bf16's exponents: the constant's and the product's rounding are |g| 2^-24 each of the result; beside them one power (two
+    # units of 2^-24; of the fourth root's four times) and up to five products, or a sum, a division and two products
+    rel = ((2 * g.abs() if c.dtype is BF16 else 0) + 16) * S.U32
+    r = S.unit(c.dtype)
+    within(got, want, want.abs() * (rel * (1 + r) + r) + K.least(c.dtype), fn)
+
+
+# few rows, and tiles of every side
+@pytest.mark.parametrize("dtype", TYPES, ids=tid)
+@pytest.mark.parametrize("shape", [(5, 1, 1, (1, 1), 72, 104), (200, 1, 1, (2, 3), 72, 104), (9000, 1, 1, (2, 4), 264, 776),
+                                   (4000, 1, 1, (4, 4), 264, 1032), (4000, 1, 1, (1, 1), 264, 1032)],
+                         ids=lambda s: f"{s[0]}-{s[3][0] * s[3][1]}-{s[4]}-{s[5]}")
+def test_product_gates_at_their_ends(shape, dtype):
+    c = _gated_case(shape, dtype, 91)
+    _check_gates(c, "omnimoe_grouped_product", (c.w,), c.w)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=tid)
+@pytest.mark.parametrize("shape", [(5, 1, 1, (1, 1), 96, 104), (70, 1, 2, (2, 3), 96, 104)], ids=["one", "six"])
+def test_product4_gates_at_their_ends(shape, dtype):
+    c = _gated_case(shape, dtype, 92)
+    codes, scales, back = _store(c.D, c.q, c.w)
+    _check_gates(c, "omnimoe_grouped_product4", (codes, scales), back)
+
+
 @pytest.mark.parametrize("T", [24, 900])
 @pytest.mark.parametrize("bad", [INF, NAN])
 def test_product_keeps_what_is_not_finite_in_its_row(T, bad):
