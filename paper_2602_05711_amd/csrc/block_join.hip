@@ -359,6 +359,8 @@ int back_groups(int64_t T, int d) {
   return (int)(n < most ? n : most);
 }
 
+static_assert(kMaxWidthF32 <= 4096 && kMaxWidth <= 8192, "the widest kernels");
+
 template <bool BF16>
 hipError_t join(const JoinArgs& p, hipStream_t st) {
   const int q8 = p.d / 8;
@@ -370,7 +372,8 @@ hipError_t join(const JoinArgs& p, hipStream_t st) {
   else if (q8 <= 128) go(join_kernel<BF16, 1, 2>, 4);
   else if (q8 <= 256) go(join_kernel<BF16, 4, 1>, 1);
   else if (q8 <= 512) go(join_kernel<BF16, 4, 2>, 1);
-  else go(join_kernel<BF16, 4, 4>, 1);
+  if constexpr (BF16)
+    if (q8 > 512) go(join_kernel<BF16, 4, 4>, 1);
   return hipGetLastError();
 }
 
@@ -383,7 +386,8 @@ hipError_t join_back(const JoinArgs& p, float* dw_out, float* dscale, float* dw_
     else if (w == 2) go(join_back_kernel<BF16, 2>);
     else if (w == 4) go(join_back_kernel<BF16, 4>);
     else if (w == 8) go(join_back_kernel<BF16, 8>);
-    else go(join_back_kernel<BF16, 16>);
+    if constexpr (BF16)
+      if (w == 16) go(join_back_kernel<BF16, 16>);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   if (!dw_out && !dscale && !dw_in) return hipSuccess;

@@ -466,8 +466,8 @@ hipError_t tiles(const GroupedArgs& p, hipStream_t st) {
     if (side == 256) return go(grouped_tile_kernel<T, 256, 256, 2, 4, TRANSPOSED, SWIGLU>, 256, 256, 512);
     if (side == 128) return go(grouped_tile_kernel<T, 128, 128, 4, 2, TRANSPOSED, SWIGLU>, 128, 128, 512);
   }
-  if constexpr (!SWIGLU) return go(grouped_tile_kernel<T, 64, 64, 2, 2, TRANSPOSED, SWIGLU>, 64, 64, 256);
-  return go(grouped_tile_kernel<T, 64, 128, 2, 2, TRANSPOSED, SWIGLU>, 64, 128, 256);
+  if constexpr (SWIGLU) return go(grouped_tile_kernel<T, 64, 128, 2, 2, TRANSPOSED, SWIGLU>, 64, 128, 256);
+  else return go(grouped_tile_kernel<T, 64, 64, 2, 2, TRANSPOSED, SWIGLU>, 64, 64, 256);
 }
 
 template <bool BF16, bool SWIGLU, int RB, int W>
@@ -475,16 +475,18 @@ hipError_t few_launch(const GroupedArgs& p, int64_t units, hipStream_t st) {
   const int64_t groups = cut(p.n, SWIGLU ? 8 * RB : 16 * RB);
   return launch_numbered(grouped_few_kernel<BF16, RB, SWIGLU, W>, units * groups, 64 * W, st, p, (int)groups);
 }
-// Two row blocks a workgroup, one where two would leave compute units idle (a matrix of 2048 x 8192, one token, before tiles
-// took it: 13.7 us instead of 19.3); eight waves where each has four steps of its loads in flight (64 experts of 2048 x 2048,
-// 4 and 64 tokens: 47 and 121 us, with four waves 54 and 126), else four (16 fp32 experts of 512 x 1024, 8 tokens: 8.4 us,
-// with eight 10.1). Four row blocks: 62 and 144 us.
+// Two row blocks a workgroup (SwiGLU: gate and up rows), one where two would leave compute units idle (a matrix of 2048 x 8192,
+// one token, before tiles took it: 13.7 us instead of 19.3); eight waves where each has four steps of its loads in flight (64
+// experts of 2048 x 2048, 4 and 64 tokens: 47 and 121 us, with four waves 54 and 126), else four (16 fp32 experts of 512 x 1024,
+// 8 tokens: 8.4 us, with eight 10.1). Four row blocks: 62 and 144 us.
 template <bool BF16, bool SWIGLU>
 hipError_t few(const GroupedArgs& p, hipStream_t st) {
-  const int64_t units = most_units(p.M, p.N, 16), blocks = units * cut((SWIGLU ? 2 : 1) * p.n, 16);
-  constexpr int kLeast = SWIGLU ? 2 : 1;
+  const int64_t units = most_units(p.M, p.N, 16);
   if (p.k / Chunk<BF16>::kElems < 256) return few_launch<BF16, SWIGLU, 2, 4>(p, units, st);
-  return blocks >= 512 ? few_launch<BF16, SWIGLU, 2, 8>(p, units, st) : few_launch<BF16, SWIGLU, kLeast, 8>(p, units, st);
+  if constexpr (!SWIGLU) {
+    if (units * cut(p.n, 16) < 512) return few_launch<BF16, SWIGLU, 1, 8>(p, units, st);
+  }
+  return few_launch<BF16, SWIGLU, 2, 8>(p, units, st);
 }
 
 // Whether a pass over the weights for every sixteen positions is faster than tiles of 64, whose copies bring the weights as
