@@ -594,16 +594,18 @@ def omnimoe_block_join_backward(desc, eps, x_out, y, gate, w_out, scale, w_in, d
                                 dw_in, ws=None, stream=None):
     """Gradients of omnimoe_block_join; outputs of inputs that are None may be None."""
     import torch
-    device = (dx if dx is not None else dw_in).device
-    ws = _ffn_workspace(ws, lambda: omnimoe_block_join_backward_workspace_size(desc), device, stream)
+    out = next((t for t in (dx, dw_in, dw_out, dscale, ws) if t is not None), None)  # (without tokens any of them may be None)
+    if out is not None:
+        ws = _ffn_workspace(ws, lambda: omnimoe_block_join_backward_workspace_size(desc), out.device, stream)
+    size = 0 if ws is None else ws.numel()
     T, d, dt, f32 = desc.T, desc.d, _layer_dtype(desc), torch.float32
     width = _gate_width(desc, gate)
     _block_call("omnimoe_block_join_backward", desc, (eps, width), (
         ("x_out", x_out, dt, T * d), ("y", y, f32, T * d), ("gate", gate, dt, T * width), ("w_out", w_out, f32, d),
         ("scale", scale, f32, d), ("w_in", w_in, f32, d), ("dx_out", dx_out, dt, T * d), ("dn", dn, dt, T * d),
         ("dx", dx, dt, T * d), ("dy", dy, f32, T * d), ("dgate", dgate, dt, T * width), ("dw_out", dw_out, f32, d),
-        ("dscale", dscale, f32, d), ("dw_in", dw_in, f32, d), ("ws", ws, torch.uint8, ws.numel())),
-        (ws.numel(),), stream)
+        ("dscale", dscale, f32, d), ("dw_in", dw_in, f32, d), ("ws", ws, torch.uint8, size)),
+        (size,), stream)
 
 
 def make_product(n_in, n_out, swiglu=False, x_order="position", y_order="position") -> OmnimoeProduct:

@@ -242,6 +242,17 @@ def test_join_of_no_tokens():
     assert all(int(got[k].count_nonzero()) == 0 for k in ("dw_out", "dscale", "dw_in"))
 
 
+def test_join_backward_of_no_tokens_with_one_output():
+    # of the sums each may be asked for alone, and nothing else has to be there
+    D = S.desc(0, 64, BF16)
+    for k in ("dw_out", "dscale", "dw_in"):
+        out = dict.fromkeys(("dw_out", "dscale", "dw_in"))
+        out[k] = torch.full((64,), 3.0, device="cuda")
+        P.omnimoe_block_join_backward(D, 1e-6, None, None, None, None, None, None, None, None, None, None, None, **out)
+        assert int(out[k].count_nonzero()) == 0
+    P.omnimoe_block_join_backward(D, 1e-6, *[None] * 14)
+
+
 def test_join_of_a_long_batch():
     # rows past 2^31 values
     T, d = 300000, 8192
