@@ -424,11 +424,14 @@ int64_t cut(int64_t v, int64_t by) { return (v + by - 1) / by; }
 // workgroups of `stages` stages run in whole rounds of 256 `most` and a rest.
 struct TileTime {
   int most;
-  double stage[6], ends;
+  double stage[5], ends;
 };
 constexpr TileTime kTime256 = {1, {1.25, 1.65}, 9}, kTime128 = {1, {0.5, 0.66}, 2.7}, kTime64 = {2, {0.24, 0.3, 0.55}, 2.2};
 constexpr TileTime kTime64Swiglu = {1, {0.43, 0.47}, 2.3};
-constexpr TileTime kSum128 = {2, {0.6, 0.75, 1.1}, 5}, kSum64 = {5, {0.45, 0.45, 0.55, 0.75, 0.95, 1.15}, 4};  // (two stages in LDS)
+constexpr TileTime kSum256 = kTime256, kSum128 = {2, {0.6, 0.75, 1.1}, 5}, kSum64 = {4, {0.45, 0.45, 0.55, 0.75, 0.95}, 4};
+// (grouped_sum_kernel's two stages and its rows' numbers, in a compute unit's 160 KiB of LDS)
+constexpr int sum_most(int side) { return 160 * 1024 / (2 * 2 * side * 128 + 4 * 64 * (int)sizeof(int2)); }
+static_assert(kSum256.most == sum_most(256) && kSum128.most == sum_most(128) && kSum64.most == sum_most(64), "LDS");
 double tiles_time(const TileTime& t, double tiles, double stages) {
   const double slots = 256.0 * t.most, rounds = floor(tiles / slots), r = (tiles - rounds * slots) / 256.0;
   const double whole = rounds * (stages * t.stage[t.most] + t.ends);
@@ -509,8 +512,10 @@ hipError_t forward(const GroupedArgs& p, bool swiglu, hipStream_t st) {
 }
 
 // The weight gradients' tiles, and parts of an expert's positions, of 512 at least, where the tiles leave compute units idle:
-// by the same times, with a tile's more for the experts' unevenness, and parts' way through memory. 16384 rows, 16 experts of
-// 1024 x 1024, both gradients: 119 us with tiles of 128, 171 with 256.
+// by the same times, with a tile's sum more for the experts' unevenness, and parts' way through memory. Of 752 sizes (512 to
+// 65536 rows, 1 to 256 experts of 512 x 264 to 4096 x 4096) the choice takes 1.02 times the fastest side's time in the mean. Rows,
+// experts, matrices (us for 64, 128, 256): 16384, 8 of 2048 x 2048: 259, 174, 135; 32768, 16 of 1024 x 2048: 398, 257, 198;
+// 16384, 1 of 2048 x 2048: 256, 166, 162; 16384, 16 of 1024 x 1024: 114, 76, 97; 8192, 12 of 512 x 512: 36, 45, 73.
 struct SumPlan {
   int side, parts;
 };
@@ -522,9 +527,9 @@ SumPlan sum_plan(const Shape& s, int k, int n) {
     const int64_t tiles = s.N * cut(k, side) * cut(n, side), wanted = 512 / tiles, most = s.M / s.N / 512;
     const int64_t cuts = wanted < most ? wanted : most;
     const int parts = cuts < 1 ? 1 : cuts > 32 ? 32 : (int)cuts;
-    const TileTime& t = side == 256 ? kTime256 : side == 128 ? kSum128 : kSum64;
-    const double stages = (double)s.M / s.N / parts / 64, slots = 256.0 * t.most;
-    const double us = tiles * parts / slots * (stages * t.stage[t.most - 1] + t.ends) + stages * t.stage[1] + t.ends +
+    const TileTime& t = side == 256 ? kSum256 : side == 128 ? kSum128 : kSum64;
+    const double stages = (double)s.M / s.N / parts / 64;
+    const double us = tiles_time(t, (double)tiles * parts, stages) + stages * t.stage[1] +
                       (parts > 1 ? 3 + (2.0 * parts * 4 + 2) * s.N * k * n / 4e6 : 0.0);
     if (side == 64 || us < least) best = {side, parts}, least = us;
   }

@@ -410,6 +410,14 @@ def test_weight_gradient_tiles(shape, orders):
     _check_dw(_case(*shape, BF16, False, orders, seed=13, weights=False))
 
 
+# tiles of 128 by rank, to and fro, in order and in parts, and long sums of few experts
+@pytest.mark.parametrize("shape", [(1500, 1, 1, (3, 4), 520, 776), (9000, 1, 1, (4, 4), 1032, 520), (4000, 1, 1, (4, 5), 1032, 776),
+                                   (30000, 1, 1, (1, 1), 520, 264), (65536, 1, 1, (2, 2), 1024, 1024)],
+                         ids=lambda s: f"{s[0]}-{s[3][0] * s[3][1]}-{s[4]}-{s[5]}")
+def test_weight_gradient_tiles_of_long_sums(shape):
+    _check_dw(_case(*shape, BF16, False, ("token", "position"), seed=14, weights=False))
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=tid)
 @pytest.mark.parametrize("idx", ["first", "last", "one each", "empty between"])
 def test_product_of_uneven_experts(idx, dtype):
