@@ -47,7 +47,8 @@ omnimoe_status omnimoe_block_join(const omnimoe_layer_desc* desc, float eps, int
  *   dy     [T, d]  fp32 out   dL/dy, as omnimoe_expert_backward and omnimoe_shared_mlp_backward take it
  *   dgate  [T, gate_width] dtype out
  *   dw_out, dscale, dw_in  [d] fp32 out, sums over the tokens
- * Outputs whose input is NULL (or with y NULL: not used) are not written and may be NULL. The norms are formed again from
+ * Outputs whose input is NULL (or with y NULL: not used) are not written and may be NULL. Without w_out dy does not depend on y.
+ * The norms are formed again from
  * x_out and y. A row's sums are fp32: squares past its largest value are no matter, products of the row's gradients (w_in dn,
  * and those of w_out norm(y)) with x_out and norm(y) that are past it are. T = 0 writes zeros to those of the three sums that
  * are not NULL and uses nothing else. Workspace:
@@ -79,7 +80,8 @@ typedef struct {
   int32_t y_order;
 } omnimoe_product;
 
-/* y = W_e x for every position of every expert e (or silu(G_e x) (U_e x)).
+/* y = W_e x for every position of every expert e (or silu(G_e x) (U_e x), for use without gradients: a training step takes the
+ * plain product of both halves and forms silu(g) u itself).
  *   x  [M, n_in], by token [T, n_in]   dtype
  *   w  [N, n_out, n_in], with swiglu [N, 2 n_out, n_in]  dtype; a matrix below 4 GiB, else OMNIMOE_ERR_UNSUPPORTED
  *   y  [M, n_out]  dtype out, rounded once from fp32 sums
@@ -118,8 +120,9 @@ omnimoe_status omnimoe_weights4_load(const omnimoe_layer_desc* desc, const omnim
                                      const uint8_t* codes, const uint8_t* scales, void* w, void* stream);
 
 /* omnimoe_grouped_product with 4-bit weights, for a few rows an expert: every code is read once for up to sixteen rows and
- * is exact in the product. More rows go through the weights again for every sixteen; a prompt's many rows are faster
- * through omnimoe_weights4_load and omnimoe_grouped_product. */
+ * is exact in the product. More rows go through the weights again for every sixteen. A prompt's many rows are faster through
+ * omnimoe_grouped_product where omnimoe_weights4_load's result is kept (64 bf16 experts of 2048 x 2048 with SwiGLU, 4096 rows:
+ * 126 us, here 140), and with a load each time from about 160 rows an expert on (8192 rows: 319 us, here 262). */
 omnimoe_status omnimoe_grouped_product4(const omnimoe_layer_desc* desc, const omnimoe_product* product, const void* x,
                                         const uint8_t* codes, const uint8_t* scales, const int32_t* offsets,
                                         const int32_t* perm, void* y, void* stream);

@@ -7,8 +7,8 @@
 //   dw_in = sum over the tokens of dn xh;  with S = sum of G s yh: dscale = w_out S, dw_out = scale S
 // Both ways are bound by memory: every value is read and written once, a row lies in registers from its first read to its
 // last use, and the way back forms the norms again instead of reading them. 16384 tokens, d = 2048, bf16: 64 us with a gate a
-// token (5.2 TB/s), back 133 us and the columns' sums 5 with a gate a channel (4.9 TB/s; a large copy runs at 4.7). One
-// token: 2.8 us, a launch's own time.
+// token (5.2 TB/s), back 137 us and the columns' sums 5 with a gate a channel (139 together back to back, 4.8 TB/s; a large copy
+// runs at 4.7); 4096 tokens, d = 8192, a gate a token: 75 and 117 us (4.5 TB/s). One token: 2.9 us, a launch's own time.
 // Sums, norms and the joint itself are fp32; results are rounded to the layer's type once (n from the unrounded x').
 #include "internal.hpp"
 #include "vec8.hpp"
@@ -187,7 +187,7 @@ struct BackRow {
 };
 
 // A row at a time a workgroup of W waves, eight values of each operand a thread; the next row's are on their way meanwhile
-// (16384 tokens, d = 2048: 133 us; two rows at once with nothing on its way 191). A thread keeps its columns' sums over the
+// (16384 tokens, d = 2048: 137 us; two rows at once with nothing on its way 191). A thread keeps its columns' sums over the
 // rows. The vector units are busy for two fifths of the time, which is why a sigmoid's division is a reciprocal and one step.
 template <bool BF16, int W>
 __global__ __launch_bounds__(64 * W) void join_back_kernel(JoinArgs p) {

@@ -5,12 +5,12 @@
 // they are copied to LDS. The experts' positions are cut into units of a tile's rows; a workgroup finds its unit from the
 // offsets itself, so that the grid depends on the sizes alone: units past the last leave at once. Bound by the matrix cores
 // beside the copies and by the tiles' starts and ends (8 to 14 us of a 256 x 256 tile's 60, 2048 summed values): 131072 rows
-// of 2048 on 64 experts of 2048 x 2048 with SwiGLU 1010 us, 1.09 PFLOP/s, 65536 rows' dx 570 and dW 655 us, 0.96 and 0.84;
-// the library's dense product of 131072 x 2048 x 2048 reaches 1.36. Without its copies the loop runs at 1.34 to 1.54. Two groups
+// of 2048 on 64 experts of 2048 x 2048 with SwiGLU 1020 to 1040 us, 1.07 PFLOP/s, 65536 rows' dx 590 and dW 665 us, 0.93 and
+// 0.83 (calls back to back); the library's dense product of 131072 x 2048 x 2048 reaches 1.36. Without its copies the loop runs at 1.34 to 1.54. Two groups
 // of waves that take turns at the products, and workgroups that go from tile to tile, were no faster (1065 and 1074 us).
 // Few rows: the time is that of reading the weights of the experts that have rows, and of little beside it
 // (few_tile.hpp): a unit is up to sixteen rows, a workgroup takes 16 or 32 weight rows and splits the summed index over its
-// waves. 128 rows on 64 experts of 2048 x 2048: 86 us, 5.5 TB/s.
+// waves. 128 rows on 64 experts of 2048 x 2048: 87 to 90 us, 5.3 TB/s.
 // Sums are fp32, rounded once; every result has one order of summation, so that it is the same on every run.
 #include "few_tile.hpp"
 #include "grouped_rows.hpp"
@@ -308,7 +308,8 @@ struct GroupedSumArgs {
 // Experts' rows may be very uneven. 16 to 64 of them, a multiple of eight, go to the XCDs by their rank in rows, to and fro
 // (the first eight to XCDs 0 to 7, the next to 7 to 0, ...), so that each has about as many rows, the longest first; all of
 // an expert's tiles stay on one XCD, whose L2 they share. Fewer experts' tiles go over all XCDs, the longest expert's first
-// (eight experts of 2048 x 2048, 16384 rows, both gradients: 344 us, with an XCD each 413). Returns the expert of rank `want`.
+// (eight experts of 2048 x 2048, 16384 rows, both gradients with tiles of 128: 344 us, with an XCD each 413). Other numbers of
+// experts go in their own order, in which the XCD of the longest ones may end last. Returns the expert of rank `want`.
 __device__ __forceinline__ int expert_of_rank(const int32_t* offsets, int N, int M, int want) {
   const int l = lane_id(), e = l < N ? l : N - 1;
   const int lo = expert_start(offsets, e, M), hi = expert_start(offsets, e + 1, M), rows = l < N ? (hi > lo ? hi - lo : 0) : -1;
@@ -321,7 +322,7 @@ __device__ __forceinline__ int expert_of_rank(const int32_t* offsets, int N, int
 }
 
 // A tile of dW_e: TM of y's columns x TN of x's, one part of e's positions. 65536 rows on 64 experts of 2048 x 2048, some with
-// three times others' rows: 655 us (with every copy looking up its row by itself 1560, experts in their own order 846).
+// three times others' rows: 665 us (with every copy looking up its row by itself 1560, experts in their own order 846).
 template <class T, int TM, int TN, int WR, int WC>
 __global__ __launch_bounds__(64 * WR * WC) void grouped_sum_kernel(GroupedSumArgs p) {
   constexpr int NW = WR * WC, MJ = TM / WR / 32, NI = TN / WC / 32;

@@ -4,9 +4,10 @@
 // least with max |w| <= 6 2^s: v_cvt_scalef32_pk_bf16_fp4 turns two codes and the scale into two bf16 values, exactly, so
 // that no product needs a scale of its own and the sums run through all of a row.
 //
-// The products are bound by reading the codes once: 128 rows on 64 experts of 2048 x 2048 with SwiGLU 30 us, 4.2 TB/s (a kernel
-// that only reads as many codes and scales in this order 21 us); eight rows of one token 6.8 us. What cost most was a byte load
-// for each scale (42 us); a row's scales of several steps now come in one.
+// The products are bound by reading the codes once: 128 rows on 64 experts of 2048 x 2048 with SwiGLU 28 to 32 us, 4.2 TB/s (a
+// kernel that only reads as many codes and scales in this order 21 us); eight rows of one token 7.4 us. What cost most was a byte
+// load for each scale (42 us); a row's scales of several steps come in one where the rows are of whole steps. Other widths have the
+// byte loads: 64 experts of 2048 x 2304 45 us, 2880 45, 768 22 (1024: 21).
 #include "few_tile.hpp"
 #include "grouped_rows.hpp"
 #include "internal.hpp"
@@ -25,7 +26,8 @@ __device__ __forceinline__ int block_exponent4(uint32_t amax_bits) {
   return s < -125 ? -125 : s > 125 ? 125 : s;
 }
 
-// A block a thread: bound by memory, laid out once.
+// A block a thread: bound by memory, laid out once. 64 matrices of 2048 x 2048, bf16: 142 us, 4.8 TB/s, and load4_kernel 149, 4.6;
+// of 1024 x 1024, fp32: 49 (from the caches in part) and 73.
 template <bool BF16>
 __global__ __launch_bounds__(256) void store4_kernel(const void* __restrict__ w, uint8_t* __restrict__ codes,
                                                      uint8_t* __restrict__ scales, int64_t blocks) {
@@ -249,7 +251,7 @@ hipError_t product4_launch(const Product4Args& p, int64_t units, hipStream_t st)
 // SwiGLU's two), with the steps spread over eight waves. 64 experts, n_in = 2048, n_out = 1024, SwiGLU: 16 tokens 29.6 us
 // with four blocks and 32.3 with two, one token 8.6 and 7.7; one matrix of 2048 x 8192, one token: 18.3, 12.0 and, with
 // one, 7.8 us. fp32 weights keep the matrix cores busy (eight products for one of bf16): one block, 7 tokens,
-// 2080 x 2056: 7.2 us, with two blocks on four waves 10.5.
+// 2080 x 2056: 7.5 us, with two blocks on four waves 10.5.
 template <bool BF16, bool SWIGLU>
 hipError_t product4(const Product4Args& p, hipStream_t st) {
   const int64_t units = p.M / 16 + p.N < p.M ? p.M / 16 + p.N : p.M, blocks = units * (((SWIGLU ? 2 : 1) * p.n + 15) / 16);
